@@ -47,7 +47,8 @@ typedef enum {
     FTK_EUNCORRECTABLE = 5 /* reserved: never returned; see ftk_ft_stats.uncorrectable   */
 } ftk_status;
 
-typedef enum { FTK_F32 = 0, FTK_F64 = 1 } ftk_dtype;
+/* FTK_BF16 and FTK_F16 are taken by the ftk_route_* and ftk_mx4_* calls alone. */
+typedef enum { FTK_F32 = 0, FTK_F64 = 1, FTK_BF16 = 2, FTK_F16 = 3 } ftk_dtype;
 
 /* Fault-tolerance mode of the contraction (Section 4).
  *   OFF     : no checksums.
@@ -323,6 +324,113 @@ ftk_status ftk_kmeans_fit_fast(ftk_dtype dtype, const void *X, int64_t N, int32_
 
 /* (host) K distinct indices in [0, N) by the seeded procedure ftk_kmeans_fit uses. */
 ftk_status ftk_seeded_indices(uint64_t seed, int64_t N, int32_t K, int64_t *idx_host);
+
+/* ---- rows sorted by label and back ---------------------------------------------------------
+ * An assignment labels every row with its nearest centroid; a gate labels every token with the k experts it
+ * likes best.  These calls bring the rows of one label together, so that what belongs to the label (an
+ * inverted list, an expert's matrix) can be applied to them, bring the results back with weights, and
+ * give the gradients of both.
+ *   N tokens of D elements with k slots each, E experts; slot s = t * k + j belongs to token t.
+ *   labels [N x k] int32: a slot whose label lies outside [0, E) is dropped: it takes no row and adds
+ *   nothing anywhere, whatever its weight.  N = 0 is a valid, empty call.
+ * Sorted rows: expert e has the rows [offsets[e], offsets[e + 1]), its slots in ascending order first, then
+ * fill up to a multiple of `align`; rows beyond offsets[E] hold nothing either.  `rows` is the number of
+ * sorted rows that the caller's arrays have, at least ftk_route_rows(N, k, E, align).
+ *   order [rows] int32  : slot of a sorted row, -1 where it holds none
+ *   pos [N x k] int32   : sorted row of a slot, -1 where it was dropped
+ * Index arrays are device data that a call cannot check first: entries outside their range count as -1.
+ * dtype: any.  Row arrays have unit stride along a row and a row stride (ldx, ... in elements, >= D).
+ * Weights are float, for FTK_F64 double.  Sums are held in 32 bits (FTK_F64: 64), in ascending j, and rounded
+ * once.  Everything is bitwise reproducible.
+ * Limits: N * k + E * (align - 1) < 2^31, 1 <= E <= 8192, 1 <= k <= 64, 1 <= align <= 65536. */
+int64_t ftk_route_rows(int64_t N, int32_t k, int32_t E, int32_t align); /* -1: bad arguments */
+size_t ftk_route_workspace_bytes(int64_t N, int32_t k, int32_t E);      /* 0: bad arguments */
+
+/* Where every slot goes: offsets [E + 1], counts [E] (slots of every expert without the fill; may be NULL),
+ * order [rows], pos [N x k], all int32 and out. */
+ftk_status ftk_route_plan(const int32_t *labels, int64_t N, int32_t k, int32_t E, int32_t align,
+                          int64_t rows, int32_t *offsets, int32_t *counts /* nullable */, int32_t *order,
+                          int32_t *pos, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* out[p] = X[order[p] / k], times weights[order[p]] where weights are given; zero where order[p] is -1.
+ *   X [N x D], out [rows x D].  out must not overlap X. */
+ftk_status ftk_route_gather(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N, int32_t k, int32_t D,
+                            const int32_t *order, const int32_t *pos, int64_t rows,
+                            const void *weights /* nullable */, void *out, int64_t ldo, void *hip_stream);
+
+/* ftk_route_plan and ftk_route_gather (without weights) in one call, for few slots in one launch. */
+ftk_status ftk_route_dispatch(ftk_dtype dtype, const void *X, int64_t ldx, int32_t D, const int32_t *labels,
+                              int64_t N, int32_t k, int32_t E, int32_t align, int64_t rows, int32_t *offsets,
+                              int32_t *counts /* nullable */, int32_t *order, int32_t *pos, void *out,
+                              int64_t ldo, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* out[t] = sum over the slots of t of weights[t, j] * Y[pos[t, j]] (weights NULL: 1; then this is the gradient
+ * of ftk_route_gather without weights).  A token all of whose slots were dropped gets zeros.
+ *   Y [rows x D], out [N x D].  out must not overlap Y. */
+ftk_status ftk_route_combine(ftk_dtype dtype, const void *Y, int64_t ldy, int64_t rows, const int32_t *pos,
+                             const void *weights /* nullable */, int64_t N, int32_t k, int32_t D, void *out,
+                             int64_t ldo, void *hip_stream);
+
+/* Gradients of ftk_route_combine with weights: dY[pos[t, j]] = weights[t, j] * dOut[t] (zero in rows without a slot),
+ * dweights[t, j] = <dOut[t], Y[pos[t, j]]> (zero for dropped slots; type of the weights).
+ *   dOut [N x D], Y and dY [rows x D] (dY must not overlap Y or dOut). */
+ftk_status ftk_route_combine_grad(ftk_dtype dtype, const void *dOut, int64_t ldg, const void *Y, int64_t ldy,
+                                  const int32_t *order, const int32_t *pos, int64_t rows, const void *weights,
+                                  int64_t N, int32_t k, int32_t D, void *dY, int64_t ldd, void *dweights,
+                                  void *hip_stream);
+
+/* ---- rows in microscaled 4-bit floating point, and products of them ---------------------------
+ * The MXFP4 format of the OCP Microscaling Formats specification 1.0: 32 consecutive elements of a row share a power of two
+ * 2^b, b = max(floor(log2 max|x|) - 2, -127), held as the byte b + 127; an element is sign, two bits of
+ * exponent and one of mantissa, one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives: x / 2^b rounded
+ * to the nearest, ties to the even code, beyond 6 to 6.  A block that holds an infinity or NaN gets the byte
+ * 255 and stands for 32 NaN.
+ * Packed rows are padded with zeros to Dp = D rounded up to 128 elements:
+ *   codes [N x Dp / 2] bytes, 16-byte aligned: element 2i in the low half of byte i, 2i + 1 in the high half
+ *   scales [N x Dp / 32] bytes, 4-byte aligned
+ * dtype of dense rows: FTK_F32, FTK_BF16 or FTK_F16. */
+
+/* Packs the N rows of X [N x D]; transpose != 0: the D columns, i.e. the rows of X^T (codes [D x Np / 2], scales
+ * [D x Np / 32], Np = N rounded up to 128). */
+ftk_status ftk_mx4_quantize(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N, int32_t D, int32_t transpose,
+                            void *codes, void *scales, void *hip_stream);
+
+/* out [N x D] of `dtype` from N packed rows of D elements, each value rounded once (FTK_F32, FTK_BF16: exact but for the
+ * type's range). */
+ftk_status ftk_mx4_dequantize(ftk_dtype dtype, const void *codes, const void *scales, int64_t N, int32_t D,
+                              void *out, int64_t ldo, void *hip_stream);
+
+/* The experts' products on packed rows: out[m, f] = sum_d A[src(m), d] * B[g(m) * F + f, d].
+ *   A : N packed rows of D elements; B : E * F packed rows of D elements, E matrices of F rows.
+ *   offsets [E + 1]  : expert e has the output rows [offsets[e], offsets[e + 1]) (device data, ascending, within
+ *                      [0, M]); rows outside all of them become zero.  NULL: E must be 1 and has all rows.
+ *   order [M], k     : src(m) = order[m] / k, and an output row whose order[m] is -1 becomes zero; NULL: src(m) = m.
+ *   out [M x F]      : FTK_F32, FTK_BF16 or FTK_F16, row stride ldo.  N must be at least M where order is NULL.
+ * Products of 4-bit elements are exact, sums are held in 32 bits and rounded once to out's type.
+ * workspace: ftk_mx4_workspace_bytes(0, 0, M, F) bytes (may be 0: then NULL is allowed).
+ * Limits: M < 2^31, F and D < 2^24, E <= 8192, E * F < 2^31. */
+ftk_status ftk_mx4_matmul(ftk_dtype out_dtype, const void *a_codes, const void *a_scales, int64_t N,
+                          const void *b_codes, const void *b_scales, int64_t M, int32_t F, int32_t D, int32_t E,
+                          const int32_t *offsets /* nullable */, const int32_t *order /* nullable */, int32_t k,
+                          void *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* The same from dense rows X [N x D] of `dtype`, packed on the way exactly as ftk_mx4_quantize does; out has
+ * their type.  workspace: ftk_mx4_workspace_bytes(N, D, M, F) bytes. */
+ftk_status ftk_mx4_linear(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N, const void *b_codes,
+                          const void *b_scales, int64_t M, int32_t F, int32_t D, int32_t E,
+                          const int32_t *offsets /* nullable */, const int32_t *order /* nullable */, int32_t k,
+                          void *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t ftk_mx4_workspace_bytes(int64_t N, int32_t D, int64_t M, int32_t F);
+
+/* Sums over the rows of every expert, the gradient of the experts' matrices:
+ *   out[e][f, d] = sum over p in [offsets[e], offsets[e + 1]) of A[f, p] * B[d, p]
+ *   A : F packed rows of `rows` elements, B : D packed rows of `rows` elements (ftk_mx4_quantize with transpose of sorted
+ *       rows, those without a slot zero); offsets on multiples of 128 (ftk_route_plan with align = 128 or a multiple; others
+ *       are rounded down); NULL: E must be 1 and has all rows.
+ *   out [E x F x D] contiguous, FTK_F32, FTK_BF16 or FTK_F16; experts without rows get zeros. */
+ftk_status ftk_mx4_outer(ftk_dtype out_dtype, const void *a_codes, const void *a_scales, const void *b_codes,
+                         const void *b_scales, int64_t rows, int32_t F, int32_t D, int32_t E,
+                         const int32_t *offsets /* nullable */, void *out, void *hip_stream);
 
 /* Profiling aid for benchmarks.  While enabled, every ftk_kmeans_assign call brackets its main
  * contraction kernel (not the small norm / refine kernels around it; on the scan path: the scan with

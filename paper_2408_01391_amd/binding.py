@@ -12,7 +12,7 @@ from pathlib import Path
 import torch
 
 FT_OFF, FT_DETECT, FT_CORRECT, FT_STRICT = 0, 1, 2, 3
-F32, F64 = 0, 1
+F32, F64, BF16, F16 = 0, 1, 2, 3
 
 _LIB_PATH = Path(__file__).resolve().parent / "libftkmeans.so"
 _lib = None
@@ -84,6 +84,32 @@ def load():
     L.ftk_profile_read.restype = i32
     L.ftk_tuning_override.argtypes = [i32, i32, i32]
     L.ftk_tuning_override.restype = i32
+    L.ftk_route_rows.argtypes = [i64, i32, i32, i32]
+    L.ftk_route_rows.restype = i64
+    L.ftk_route_workspace_bytes.argtypes = [i64, i32, i32]
+    L.ftk_route_workspace_bytes.restype = sz
+    L.ftk_route_plan.argtypes = [vp, i64, i32, i32, i32, i64, vp, vp, vp, vp, vp, sz, vp]
+    L.ftk_route_plan.restype = i32
+    L.ftk_route_gather.argtypes = [i32, vp, i64, i64, i32, i32, vp, vp, i64, vp, vp, i64, vp]
+    L.ftk_route_gather.restype = i32
+    L.ftk_route_dispatch.argtypes = [i32, vp, i64, i32, vp, i64, i32, i32, i32, i64, vp, vp, vp, vp, vp, i64, vp, sz, vp]
+    L.ftk_route_dispatch.restype = i32
+    L.ftk_route_combine.argtypes = [i32, vp, i64, i64, vp, vp, i64, i32, i32, vp, i64, vp]
+    L.ftk_route_combine.restype = i32
+    L.ftk_route_combine_grad.argtypes = [i32, vp, i64, vp, i64, vp, vp, i64, vp, i64, i32, i32, vp, i64, vp, vp]
+    L.ftk_route_combine_grad.restype = i32
+    L.ftk_mx4_quantize.argtypes = [i32, vp, i64, i64, i32, i32, vp, vp, vp]
+    L.ftk_mx4_quantize.restype = i32
+    L.ftk_mx4_dequantize.argtypes = [i32, vp, vp, i64, i32, vp, i64, vp]
+    L.ftk_mx4_dequantize.restype = i32
+    L.ftk_mx4_matmul.argtypes = [i32, vp, vp, i64, vp, vp, i64, i32, i32, i32, vp, vp, i32, vp, i64, vp, sz, vp]
+    L.ftk_mx4_matmul.restype = i32
+    L.ftk_mx4_linear.argtypes = [i32, vp, i64, i64, vp, vp, i64, i32, i32, i32, vp, vp, i32, vp, i64, vp, sz, vp]
+    L.ftk_mx4_linear.restype = i32
+    L.ftk_mx4_workspace_bytes.argtypes = [i64, i32, i64, i32]
+    L.ftk_mx4_workspace_bytes.restype = sz
+    L.ftk_mx4_outer.argtypes = [i32, vp, vp, vp, vp, i64, i32, i32, i32, vp, vp, vp]
+    L.ftk_mx4_outer.restype = i32
     L.ftk_last_error.restype = ctypes.c_char_p
     L.ftk_version.restype = ctypes.c_char_p
     _lib = L
@@ -92,6 +118,9 @@ def load():
 
 EXPORTS = ("ftk_workspace_bytes", "ftk_assign_geometry", "ftk_plan_padded_rows", "ftk_ft_thresholds", "ftk_kmeans_assign_static", "ftk_static_scratch_bytes", "ftk_kmeans_assign", "ftk_kmeans_assign_fast", "ftk_fast_plan", "ftk_absmax",
            "ftk_kmeans_update", "ftk_kmeans_update_ft", "ftk_kmeans_step_batched", "ftk_update_geometry", "ftk_kmeans_fit", "ftk_kmeans_fit_fast", "ftk_seeded_indices", "ftk_profile_enable",
+           "ftk_route_rows", "ftk_route_workspace_bytes", "ftk_route_plan", "ftk_route_gather", "ftk_route_dispatch",
+           "ftk_route_combine", "ftk_route_combine_grad", "ftk_mx4_quantize", "ftk_mx4_dequantize", "ftk_mx4_matmul",
+           "ftk_mx4_linear", "ftk_mx4_workspace_bytes", "ftk_mx4_outer",
            "ftk_profile_read", "ftk_tuning_override", "ftk_last_error", "ftk_version")
 
 
@@ -367,3 +396,302 @@ def kmeans_fit(X, K, iters, seed=0, C_init=None, ft_mode=FT_OFF, stats=None, wor
                                  None if inertia is None else inertia.ctypes.data, ft_mode,
                                  _ptr(stats), wp, wn, _stream()))
     return dict(C=C, labels=labels, counts=counts, inertia=inertia)
+
+
+# ---- rows sorted by label and back -----------------------------------------------------------
+
+_ROW_DTYPES = {torch.float32: F32, torch.float64: F64, torch.bfloat16: BF16, torch.float16: F16}
+_MX_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+def _row_code(t: torch.Tensor, name: str, dtypes=_ROW_DTYPES) -> int:
+    code = dtypes.get(t.dtype)
+    if code is None:
+        raise TypeError("%s: %s is not one of %s" % (name, t.dtype, ", ".join(str(d)[6:] for d in dtypes)))
+    return code
+
+
+def _row_stride(t: torch.Tensor, name: str) -> int:
+    """Row stride of a 2-D device tensor whose rows are contiguous."""
+    if not t.is_cuda:
+        raise ValueError("%s must live on the GPU" % name)
+    if t.dim() != 2 or (t.shape[0] > 0 and t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s must be a 2-D tensor of contiguous rows" % name)
+    if t.shape[0] <= 1:
+        return t.shape[1]
+    if t.stride(0) < t.shape[1]:
+        raise ValueError("%s: its rows overlap" % name)
+    return t.stride(0)
+
+
+def _index(t: torch.Tensor, name: str, *shape) -> torch.Tensor:
+    if not t.is_cuda or t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous int32 device tensor of shape %s" % (name, list(shape)))
+    return t
+
+
+def _new_rows(out, rows, D, like, name, dtype=None):
+    dtype = like.dtype if dtype is None else dtype
+    if out is None:
+        return torch.empty(rows, D, dtype=dtype, device=like.device)
+    if out.shape != (rows, D) or out.dtype != dtype:
+        raise ValueError("%s must be [%d, %d] of %s" % (name, rows, D, dtype))
+    return out
+
+
+class Route:
+    """Where every slot's row goes (device tensors, int32): offsets [E + 1], counts [E], order [rows], pos [N, k]."""
+
+    __slots__ = ("offsets", "counts", "order", "pos", "align")
+
+    def __init__(self, offsets, counts, order, pos, align=1):
+        self.offsets, self.counts, self.order, self.pos, self.align = offsets, counts, order, pos, align
+
+    @property
+    def experts(self):
+        return self.offsets.shape[0] - 1
+
+    @property
+    def rows(self):
+        return self.order.shape[0]
+
+    def check(self):
+        N, k = self.pos.shape
+        _index(self.offsets, "offsets", self.experts + 1), _index(self.order, "order", self.rows)
+        _index(self.pos, "pos", N, k)
+        return N, k
+
+
+def route_rows(N: int, k: int, E: int, align: int = 1) -> int:
+    """Sorted rows that N tokens of k slots may need."""
+    n = load().ftk_route_rows(N, k, E, align)
+    if n < 0:
+        raise FtkError(1, load().ftk_last_error().decode())
+    return n
+
+
+def route_workspace_bytes(N: int, k: int, E: int) -> int:
+    n = load().ftk_route_workspace_bytes(N, k, E)
+    if n == 0:
+        raise FtkError(1, load().ftk_last_error().decode())
+    return n
+
+
+def _route_args(labels, E, align, route, workspace):
+    if labels.dim() == 1:
+        labels = labels.unsqueeze(1)
+    if labels.dim() != 2:
+        raise ValueError("labels must be [N] or [N, k]")
+    N, k = labels.shape
+    _index(labels, "labels", N, k)
+    if route is None:
+        rows, dev = route_rows(N, k, E, align), labels.device
+        whole = torch.empty(2 * E + 1 + rows + N * k, dtype=torch.int32, device=dev)
+        offsets, counts, order, pos = whole.split((E + 1, E, rows, N * k))
+        route = Route(offsets, counts, order, pos.view(N, k), align)
+    else:
+        if route.check() != (N, k) or route.experts != E or route.align != align:
+            raise ValueError("route is not one of %d x %d slots, %d experts and align %d" % (N, k, E, align))
+        _index(route.counts, "counts", E)
+    need = route_workspace_bytes(N, k, E)
+    if workspace is None:
+        workspace = torch.empty(need + 256, dtype=torch.uint8, device=labels.device)
+    return labels, N, k, route, workspace
+
+
+def route_plan(labels, E, align=1, route=None, workspace=None):
+    """Sorts the slots of labels (int32 [N] or [N, k]; outside [0, E): dropped) by expert.  Returns a Route."""
+    labels, N, k, route, workspace = _route_args(labels, E, align, route, workspace)
+    wp, wn = _ws_args(workspace)
+    _check(load().ftk_route_plan(labels.data_ptr(), N, k, E, align, route.rows, route.offsets.data_ptr(),
+                                 route.counts.data_ptr(), route.order.data_ptr(), route.pos.data_ptr(), wp, wn, _stream()))
+    return route
+
+
+def route_dispatch(X, labels, E, align=1, out=None, route=None, workspace=None):
+    """route_plan and route_gather in one call.  Returns (sorted rows [rows, D], Route)."""
+    labels, N, k, route, workspace = _route_args(labels, E, align, route, workspace)
+    ld = _row_stride(X, "X")
+    if X.shape[0] != N:
+        raise ValueError("X must have a row for each of the %d tokens" % N)
+    out = _new_rows(out, route.rows, X.shape[1], X, "out")
+    wp, wn = _ws_args(workspace)
+    _check(load().ftk_route_dispatch(_row_code(X, "X"), X.data_ptr(), ld, X.shape[1], labels.data_ptr(), N, k, E, align,
+                                     route.rows, route.offsets.data_ptr(), route.counts.data_ptr(),
+                                     route.order.data_ptr(), route.pos.data_ptr(), out.data_ptr(),
+                                     _row_stride(out, "out"), wp, wn, _stream()))
+    return out, route
+
+
+def _weights(weights, like, N, k):
+    dtype = torch.float64 if like.dtype == torch.float64 else torch.float32
+    if weights is not None and (not weights.is_cuda or weights.dtype != dtype or tuple(weights.shape) != (N, k)
+                                or not weights.is_contiguous()):
+        raise ValueError("weights must be a contiguous device tensor [%d, %d] of %s" % (N, k, dtype))
+    return weights
+
+
+def route_gather(X, route, weights=None, out=None):
+    """Tokens' rows X [N, D], times weights [N, k] if given, to their sorted places [rows, D]; rows without a slot are zero."""
+    N, k = route.check()
+    ld = _row_stride(X, "X")
+    if X.shape[0] != N:
+        raise ValueError("X must have a row for each of the %d tokens" % N)
+    out = _new_rows(out, route.rows, X.shape[1], X, "out")
+    _check(load().ftk_route_gather(_row_code(X, "X"), X.data_ptr(), ld, N, k, X.shape[1], route.order.data_ptr(),
+                                   route.pos.data_ptr(), route.rows, _ptr(_weights(weights, X, N, k)), out.data_ptr(),
+                                   _row_stride(out, "out"), _stream()))
+    return out
+
+
+def route_combine(Y, route, weights=None, out=None):
+    """Sorted rows Y [rows, D] back to their tokens [N, D]: the sum over a token's slots, times weights [N, k] if given."""
+    N, k = route.check()
+    ld = _row_stride(Y, "Y")
+    if Y.shape[0] != route.rows:
+        raise ValueError("Y must have the %d sorted rows" % route.rows)
+    out = _new_rows(out, N, Y.shape[1], Y, "out")
+    _check(load().ftk_route_combine(_row_code(Y, "Y"), Y.data_ptr(), ld, route.rows, route.pos.data_ptr(),
+                                    _ptr(_weights(weights, Y, N, k)), N, k, Y.shape[1], out.data_ptr(),
+                                    _row_stride(out, "out"), _stream()))
+    return out
+
+
+def route_combine_grad(dOut, Y, route, weights, dY=None, dweights=None):
+    """Gradients of route_combine(Y, route, weights) for dOut [N, D].  Returns (dY [rows, D], dweights [N, k]).
+    (The gradient of route_gather without weights is route_combine without weights.)"""
+    N, k = route.check()
+    D = dOut.shape[1]
+    ldg, ldy = _row_stride(dOut, "dOut"), _row_stride(Y, "Y")
+    if dOut.shape[0] != N or tuple(Y.shape) != (route.rows, D) or Y.dtype != dOut.dtype:
+        raise ValueError("dOut [N, D] and Y [rows, D] must share type and D")
+    _weights(weights, Y, N, k)
+    dY = _new_rows(dY, route.rows, D, Y, "dY")
+    dweights = torch.empty_like(weights) if dweights is None else _weights(dweights, Y, N, k)
+    _check(load().ftk_route_combine_grad(_row_code(Y, "Y"), dOut.data_ptr(), ldg, Y.data_ptr(), ldy,
+                                         route.order.data_ptr(), route.pos.data_ptr(), route.rows, weights.data_ptr(),
+                                         N, k, D, dY.data_ptr(), _row_stride(dY, "dY"), dweights.data_ptr(), _stream()))
+    return dY, dweights
+
+
+# ---- rows in microscaled 4-bit floating point ------------------------------------------------
+
+
+class Mx4:
+    """Packed rows (device tensors, uint8): codes [N, Dp / 2], scales [N, Dp / 32]; D elements a row, Dp = D rounded up
+    to 128."""
+
+    __slots__ = ("codes", "scales", "D")
+
+    def __init__(self, codes, scales, D):
+        self.codes, self.scales, self.D = codes, scales, D
+
+    @property
+    def N(self):
+        return self.codes.shape[0]
+
+    def check(self, name):
+        Dp = -(-self.D // 128) * 128
+        for t, width, part in ((self.codes, Dp // 2, "codes"), (self.scales, Dp // 32, "scales")):
+            if (not t.is_cuda or t.dtype != torch.uint8 or tuple(t.shape) != (self.codes.shape[0], width)
+                    or not t.is_contiguous()):
+                raise ValueError("%s.%s must be a contiguous uint8 device tensor [N, %d]" % (name, part, width))
+        return self
+
+
+def mx4_quantize(X, transpose=False, out=None):
+    """Packs the rows of X [N, D] (transpose: its columns, as rows of N elements).  Returns an Mx4."""
+    ld = _row_stride(X, "X")
+    N, D = X.shape
+    n, d = (D, N) if transpose else (N, D)
+    if out is None:
+        Dp = -(-d // 128) * 128
+        out = Mx4(torch.empty(n, Dp // 2, dtype=torch.uint8, device=X.device),
+                  torch.empty(n, Dp // 32, dtype=torch.uint8, device=X.device), d)
+    elif out.N != n or out.D != d:
+        raise ValueError("out must hold %d rows of %d elements" % (n, d))
+    else:
+        out.check("out")
+    _check(load().ftk_mx4_quantize(_row_code(X, "X", _MX_DTYPES), X.data_ptr(), ld, N, D, 1 if transpose else 0,
+                                   out.codes.data_ptr(), out.scales.data_ptr(), _stream()))
+    return out
+
+
+def mx4_dequantize(q, dtype=torch.float32, out=None):
+    """The values of packed rows, [N, D]."""
+    q.check("q")
+    out = _new_rows(out, q.N, q.D, q.codes, "out", dtype)
+    if q.D == 0:
+        return out
+    _check(load().ftk_mx4_dequantize(_row_code(out, "out", _MX_DTYPES), q.codes.data_ptr(), q.scales.data_ptr(), q.N, q.D,
+                                     out.data_ptr(), _row_stride(out, "out"), _stream()))
+    return out
+
+
+def _groups(B, route, gather, sources):
+    """(E, F, M, offsets, order, k) of a product."""
+    B.check("B")
+    if route is None:
+        return 1, B.N, sources, None, None, 1
+    N, k = route.check()
+    E = route.experts
+    if B.N % E:
+        raise ValueError("%d rows of B are not %d matrices of equal height" % (B.N, E))
+    if sources != (N if gather else route.rows):
+        raise ValueError("%d rows given, the route has %d %s" % (sources, N if gather else route.rows,
+                                                                 "tokens" if gather else "sorted rows"))
+    return E, B.N // E, route.rows, route.offsets, route.order if gather else None, k
+
+
+def mx4_matmul(A, B, route=None, gather=False, out=None, out_dtype=torch.bfloat16):
+    """Products of packed rows: [A.N, B.N] without a route.  With one, B holds the experts' matrices one after the other and a
+    sorted row meets its expert's: A holds sorted rows, or with gather=True the tokens' rows; [rows, F]."""
+    A.check("A")
+    if A.D != B.D:
+        raise ValueError("A and B must share D (got %d and %d)" % (A.D, B.D))
+    E, F, M, offsets, order, k = _groups(B, route, gather, A.N)
+    out = _new_rows(out, M, F, A.codes, "out", out_dtype if out is None else out.dtype)
+    _check(load().ftk_mx4_matmul(_row_code(out, "out", _MX_DTYPES), A.codes.data_ptr(), A.scales.data_ptr(), A.N,
+                                 B.codes.data_ptr(), B.scales.data_ptr(), M, F, A.D, E, _ptr(offsets), _ptr(order), k,
+                                 out.data_ptr(), _row_stride(out, "out"), None, 0, _stream()))
+    return out
+
+
+def mx4_linear(X, B, route=None, gather=False, out=None, workspace=None):
+    """mx4_matmul of dense rows X, packed on the way; the result has their type."""
+    ld = _row_stride(X, "X")
+    N, D = X.shape
+    if D != B.D:
+        raise ValueError("X and B must share D (got %d and %d)" % (D, B.D))
+    E, F, M, offsets, order, k = _groups(B, route, gather, N)
+    out = _new_rows(out, M, F, X, "out")
+    if workspace is None:
+        need = load().ftk_mx4_workspace_bytes(N, D, M, F)
+        workspace = torch.empty(need + 256, dtype=torch.uint8, device=X.device)
+    wp, wn = _ws_args(workspace)
+    _check(load().ftk_mx4_linear(_row_code(X, "X", _MX_DTYPES), X.data_ptr(), ld, N, B.codes.data_ptr(),
+                                 B.scales.data_ptr(), M, F, D, E, _ptr(offsets), _ptr(order), k, out.data_ptr(),
+                                 _row_stride(out, "out"), wp, wn, _stream()))
+    return out
+
+
+def mx4_outer(A, B, route=None, out=None, out_dtype=torch.float32):
+    """Sums over the rows of every expert, [E, F, D]: A holds F and B holds D packed rows across all sorted rows
+    (mx4_quantize(..., transpose=True)); the route's align must be a multiple of 128."""
+    A.check("A"), B.check("B")
+    if A.D != B.D:
+        raise ValueError("A and B must have equally many elements a row (got %d and %d)" % (A.D, B.D))
+    E = 1
+    if route is not None:
+        route.check()
+        E = route.experts
+        if route.align % 128 or A.D != route.rows:
+            raise ValueError("mx4_outer takes all sorted rows, and a route whose align is a multiple of 128")
+    if out is None:
+        out = torch.empty(E, A.N, B.N, dtype=out_dtype, device=A.codes.device)
+    elif tuple(out.shape) != (E, A.N, B.N) or not out.is_contiguous():
+        raise ValueError("out must be a contiguous tensor [%d, %d, %d]" % (E, A.N, B.N))
+    _check(load().ftk_mx4_outer(_row_code(out, "out", _MX_DTYPES), A.codes.data_ptr(), A.scales.data_ptr(),
+                                B.codes.data_ptr(), B.scales.data_ptr(), A.D, A.N, B.N, E,
+                                None if route is None else route.offsets.data_ptr(), out.data_ptr(), _stream()))
+    return out

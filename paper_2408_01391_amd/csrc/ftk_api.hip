@@ -310,7 +310,7 @@ static ftk_status check_problem(ftk_dtype dtype, int64_t N, int D, int K, int ft
     return FTK_OK;
 }
 
-static ftk_status check_ptr(const void *p, size_t align, const char *name)
+ftk_status check_ptr(const void *p, size_t align, const char *name)
 {
     if (!p) {
         set_error("%s is NULL", name);
@@ -323,7 +323,7 @@ static ftk_status check_ptr(const void *p, size_t align, const char *name)
     return FTK_OK;
 }
 
-static ftk_status check_workspace(void *ws, size_t bytes, size_t need)
+ftk_status check_workspace(void *ws, size_t bytes, size_t need)
 {
     if (!ws || bytes < need) {
         set_error("workspace of %zu bytes given, %zu needed", ws ? bytes : (size_t)0, need);
@@ -336,7 +336,7 @@ static ftk_status check_workspace(void *ws, size_t bytes, size_t need)
     return FTK_OK;
 }
 
-static ftk_status check_device()
+ftk_status check_device()
 {
     static thread_local int checked_dev = -1;
     int dev = 0;

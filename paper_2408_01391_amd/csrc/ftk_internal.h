@@ -24,6 +24,11 @@ ftk_status hip_failed(hipError_t e, const char *what);
         if (s_ != FTK_OK) return s_;   \
     } while (0)
 
+// argument checks shared by the entry points
+ftk_status check_ptr(const void *p, size_t align, const char *name);
+ftk_status check_workspace(void *ws, size_t bytes, size_t need);
+ftk_status check_device();
+
 static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
