@@ -105,6 +105,29 @@ __device__ __forceinline__ float4v mx_mma(uint4 b, uint32_t bs, uint4 a, uint32_
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(frag(b), frag(a), c, 4, 4, 0, (int)bs, 0, (int)as);
 }
 
+// The same onto accumulators that stay where they are, with byte BYTE of the scales.  256 of them fill the AGPRs, and the compiler,
+// which may give the result other registers than the summand, would move them about.  What it would
+// otherwise see to is in the text: two wait states after a vector instruction that wrote an operand.  (Before the sums are
+// read, the caller waits for the last ones.)
+template <int BYTE>
+__device__ __forceinline__ void mx_mma_in_place(float4v &c, uint4 b, uint32_t bs, uint4 a, uint32_t as)
+{
+    typedef uint32_t four __attribute__((ext_vector_type(4)));
+    const four x = {b.x, b.y, b.z, b.w}, y = {a.x, a.y, a.z, a.w};
+    if constexpr (BYTE == 0)
+        asm("s_nop 1\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] cbsz:4 blgp:4"
+            : "+a"(c) : "v"(x), "v"(y), "v"(bs), "v"(as));
+    else
+        asm("s_nop 1\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[1,1,0] op_sel_hi:[0,0,0] cbsz:4 blgp:4"
+            : "+a"(c) : "v"(x), "v"(y), "v"(bs), "v"(as));
+}
+__device__ __forceinline__ void mx_sums_done()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // Few rows: 16 output rows by 16 * CT columns a workgroup, whose four waves share the steps of 128 elements out between
 // them and add their sums up in LDS.  Operands go from memory straight to registers; a dense row is packed on
 // the way, the whole block of 32 within a lane.
@@ -200,6 +223,293 @@ static ftk_status launch_direct(MxProduct a, hipStream_t st)
     return FTK_OK;
 }
 
+// Many rows: TM = 32 * MT rows by TN = 32 * NT columns a workgroup, a quarter of them a wave.  k goes in stages of 256
+// elements, one 128-byte line of codes a row, copied straight to LDS a stage ahead of their use; scales go two
+// stages (16 bytes a row) at a time.  A stage is two steps of the instruction.  Which 128 of its elements a step takes is
+// free as long as both operands agree: lane quarter q takes blocks 2q and 2q + 1, so that the scales of both steps
+// are one 16-bit word, out of which the instruction picks the byte.
+//
+// LDS rows are lines of eight 16-byte pieces, piece p of row r at place p ^ key(r): the eight lanes that LDS serves
+// at once then read eight different places.  The copy keeps the order of its lanes, so it is the lanes' addresses
+// that are permuted, within a line.
+// Column tile j of a wave has, for lane row r, column 32 * (j / 2) + 8 * (r / 4) + 4 * (j % 2) + r % 4: two
+// tiles together give a lane eight consecutive columns to store.
+//
+// While one step's fragments are multiplied the next one's are read.
+// Copies as to_lds16 (ftk_mma.h), to an LDS address; the second from a common base and 32-bit offsets of the lanes.
+__device__ __forceinline__ void to_lds16_at(const uint8_t *g, uint32_t at)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(g) : "memory");
+}
+__device__ __forceinline__ void to_lds16_from(const uint8_t *base, uint32_t offset, uint32_t at)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(base) : "memory");
+}
+
+template <int MT, int NT>
+struct TileShape {
+    static constexpr int TM = 32 * MT, TN = 32 * NT, ROWS = TM + TN;
+    static constexpr int STAGE = ROWS * 128, SCALES = ROWS * 16;
+    static constexpr int LDS = 2 * STAGE + 2 * SCALES + TM * 4;
+};
+
+template <int MT, int NT, typename Out, bool OUTER>
+__global__ __launch_bounds__(256, MT* NT >= 64 ? 1 : 2) void mx_tile_kernel(MxProduct a)
+{
+    using S = TileShape<MT, NT>;
+    extern __shared__ __align__(16) uint8_t lds[];
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
+    uint8_t *const sc = lds + 2 * S::STAGE;
+    int *const source = reinterpret_cast<int *>(sc + 2 * S::SCALES);
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, q = lane >> 4;
+    const int64_t t = blockIdx.x / a.ntiles;
+    const int n0 = (int)(blockIdx.x - t * a.ntiles) * S::TN;
+    int64_t m0, end;
+    int e, k0 = 0, k1 = (int)(a.pitch / 4);
+    if constexpr (OUTER) {
+        const int64_t mt = (a.M + S::TM - 1) / S::TM;
+        e = (int)(t / mt);
+        m0 = (t - (int64_t)e * mt) * S::TM;
+        end = a.M;
+        if (a.offsets) {
+            k0 = min(k1, max(0, a.offsets[e]) / 128);
+            k1 = min(k1, max(0, a.offsets[e + 1]) / 128);
+        }
+    } else {
+        RowTile tile;
+        if (!find_tile<S::TM>(a, t, tile)) return;
+        e = tile.e;
+        m0 = tile.m0;
+        end = tile.end;
+        if (e >= a.E) k1 = 0;
+    }
+    float4v acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = float4v{0, 0, 0, 0};
+    const int wm = (w >> 1) * 16 * MT, wn = (w & 1) * 16 * NT;
+
+    const int steps = max(0, k1 - k0), stages = (steps + 1) / 2;
+    // rows of A, -1 where an output row has none
+    for (int row = tid; row < S::TM; row += 256) {
+        const int64_t m = m0 + row;
+        source[row] = (int)(m >= end ? -1 : OUTER ? m : source_row(a, m));
+    }
+    __syncthreads();
+    if (steps > 0) {
+        // What this lane copies: rows lane / 8 of eights of rows, one piece of each.  The key of A's rows goes with the row, that
+        // of B's with the lane row that reads them.
+        const uint32_t pitch = (uint32_t)a.pitch * 16;
+        const int slot = lane & 7, l8 = lane >> 3;
+        const uint8_t *abase = a.a_codes + (int64_t)k0 * 64, *bbase = a.b_codes + ((int64_t)k0 * 64 + (int64_t)n0 * pitch);
+        const uint8_t *const ascales = a.a_scales + k0 * 4, *bscales = a.b_scales + (k0 * 4 + (int64_t)n0 * a.pitch);
+        if constexpr (!OUTER) {
+            bbase += (int64_t)e * a.F * pitch;
+            bscales += (int64_t)e * a.F * a.pitch;
+        }
+        const int blast = a.F - 1 - n0;
+        uint32_t arow[MT], boff[NT];  // row of A; offset from the column tile's first line
+#pragma unroll
+        for (int i = 0; i < MT; ++i) arow[i] = (uint32_t)max(0, source[(w * MT + i) * 8 + l8]);
+        const int pa = slot ^ l8, pb = slot ^ (l8 & 3);  // pieces; of B ^ 4 in every second eight
+#pragma unroll
+        for (int i = 0; i < NT; ++i) boff[i] = min((w * NT + i) * 8 + l8, blast) * pitch + (pb ^ (i & 1) * 4) * 16;
+        const bool small = a.pitch < 16;  // all scales of a row at once, and the next row may not be there to be read
+        constexpr int SN = (S::ROWS / 64 + 3) / 4;
+        if (small) {
+            for (int row = tid; row < S::ROWS; row += 256) {
+                const int64_t at = row < S::TM ? max(0, source[row]) : min(row - S::TM, blast);
+                const uint32_t *g = reinterpret_cast<const uint32_t *>((row < S::TM ? ascales : bscales) + at * a.pitch);
+                for (int c = 0; c < steps; ++c) reinterpret_cast<uint32_t *>(sc + row * 16)[c] = g[c];
+            }
+        }
+        const int64_t last = a.pitch - 16 - (int64_t)k0 * 4;  // the last 16 scales of a row
+        // Copy number c of a stage (MT + NT of them).  In half a stage the line's second half lies beyond the range, maybe beyond
+        // the array: the first is read twice.
+        auto copy = [&](int st, int c) __attribute__((always_inline)) {
+            const uint32_t to = lds0 + (st & 1) * S::STAGE;
+            const bool half = 2 * st + 2 > steps;
+            if (c < MT) {
+                uint32_t row = arow[c];
+                asm volatile("" : "+v"(row));  // (the product would be kept for all stages in two registers a row)
+                const int p = half ? pa & 3 : pa;
+                to_lds16_at(abase + (int64_t)st * 128 + p * 16 + (uint64_t)row * pitch, to + (w * MT + c) * 1024);
+            } else {
+                const int i = c - MT;
+                uint32_t o = boff[i];
+                if (half) o -= ((pb ^ (i & 1) * 4) & 4) * 16;
+                to_lds16_from(bbase + (int64_t)st * 128, o, to + S::TM * 128 + (w * NT + i) * 1024);
+            }
+        };
+        // the scales of stages st and st + 1
+        auto copy_scales = [&](int st) __attribute__((always_inline)) {
+            const int64_t o = st * 8, at = o < last ? o : last;
+#pragma unroll
+            for (int i = 0; i < SN; ++i) {
+                const int first = (i * 4 + w) * 64, row = first + lane;
+                if (first >= S::ROWS) break;
+                const uint32_t src = first < S::TM ? max(0, source[min(row, S::TM - 1)]) : min(row - S::TM, blast);
+                to_lds16_at((first < S::TM ? ascales : bscales) + at + (uint64_t)src * (uint32_t)a.pitch,
+                            lds0 + 2 * S::STAGE + ((st >> 1) & 1) * S::SCALES + first * 16);
+            }
+        };
+        // where a stage's scales of a row begin in its 16 bytes
+        auto scale_at = [&](int st) __attribute__((always_inline)) {
+            const int64_t o = (st & ~1) * 8, at = small || o < last ? o : last;
+            return (int)((st & 1) * 8 + (o - at)) + ((st >> 1) & 1) * S::SCALES;
+        };
+        const int lrow = wm + r, lcol = wn + (r >> 2) * 8 + (r & 3), key = r & 7;
+        const uint8_t *const fa = lds + lrow * 128, *const fb = lds + (S::TM + lcol) * 128;
+        const uint8_t *const sa = sc + lrow * 16, *const sb = sc + (S::TM + lcol) * 16;
+        uint4 fra[MT], frb[2][NT];
+        uint32_t xa[MT], xb[2][NT];
+        auto read_a = [&](int at, int i) __attribute__((always_inline)) { fra[i] = *reinterpret_cast<const uint4 *>(fa + at + i * 16 * 128); };
+        auto read_b = [&](int at, int j, int set) __attribute__((always_inline)) {
+            frb[set][j] = *reinterpret_cast<const uint4 *>(fb + at + (j >> 1) * 32 * 128 + (j & 1) * 4 * 128);
+        };
+        auto read_xa = [&](int at, int i) __attribute__((always_inline)) { xa[i] = *reinterpret_cast<const uint16_t *>(sa + at + i * 16 * 16); };
+        auto read_xb = [&](int at, int j, int set) __attribute__((always_inline)) {
+            xb[set][j] = *reinterpret_cast<const uint16_t *>(sb + at + (j >> 1) * 32 * 16 + (j & 1) * 4 * 16);
+        };
+        // One step's products, row tile by row tile; behind each the next step's fragments of that number are read, the A
+        // fragment into the registers just used.  BYTE: of the scales, and the set of B fragments.
+        auto step = [&](auto byte, auto copies, int cst, int at, int sat) __attribute__((always_inline)) {
+            constexpr int B = decltype(byte)::value, C = decltype(copies)::value;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+                    mx_mma_in_place<B>(acc[i][j], frb[B][j], xb[0][j], fra[i], xa[i]);
+                read_a(at, i);
+                if (B) read_xa(sat, i);
+#pragma unroll
+                for (int j = i * NT / MT; j < (i + 1) * NT / MT; ++j) {
+                    read_b(at, j, 1 - B);
+                    if (B) read_xb(sat, j, 1);
+                }
+                if constexpr (C > 0) {
+#pragma unroll
+                    for (int c = i * C / MT; c < (i + 1) * C / MT; ++c) copy(cst, c);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        const int whole = steps / 2;
+#pragma unroll
+        for (int c = 0; c < MT + NT; ++c) copy(0, c);
+        if (!small) copy_scales(0);
+        wait_loads<0>();
+        __syncthreads();
+        if (stages > 1) {
+#pragma unroll
+            for (int c = 0; c < MT + NT; ++c) copy(1, c);
+        }
+        {
+            const int at = ((2 * q) ^ key) * 16, sat = scale_at(0) + 2 * q;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                read_b(at, j, 0);
+                read_xb(sat, j, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                read_a(at, i);
+                read_xa(sat, i);
+            }
+        }
+        using Zero = std::integral_constant<int, 0>;
+        using One = std::integral_constant<int, 1>;
+        using All = std::integral_constant<int, MT + NT>;
+        auto stage = [&](auto copies, int st) __attribute__((always_inline)) {
+            step(Zero{}, Zero{}, 0, (st & 1) * S::STAGE + ((2 * q + 1) ^ key) * 16, 0);
+            // this stage is in registers and the next one has arrived, in all waves
+            wait_loads<0>();
+            __syncthreads();
+            if constexpr (decltype(copies)::value > 0) {
+                if (!small && (st & 1) == 0) copy_scales(st + 2);
+            }
+            // (behind the last stage this reads what is not used)
+            step(One{}, copies, st + 2, ((st + 1) & 1) * S::STAGE + ((2 * q) ^ key) * 16, scale_at(st + 1) + 2 * q);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) xb[0][j] = xb[1][j];
+        };
+        int st = 0;
+        for (; st + 2 < stages; ++st) stage(All{}, st);
+        for (; st < whole; ++st) stage(Zero{}, st);
+        if (steps & 1) {  // half a stage: blocks 0 to 3 of the line
+            const int at = (whole & 1) * S::STAGE + (q ^ key) * 16, sat = scale_at(whole) + q;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                read_b(at, j, 0);
+                read_xb(sat, j, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                read_a(at, i);
+                read_xa(sat, i);
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+                    mx_mma_in_place<0>(acc[i][j], frb[0][j], xb[0][j], fra[i], xa[i]);
+        }
+    }
+    mx_sums_done();
+    typedef Out Eight __attribute__((ext_vector_type(8), aligned(sizeof(Out))));
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int64_t m = m0 + wm + i * 16 + r;
+        if (m >= end) continue;
+        const bool held = source[wm + i * 16 + r] >= 0;
+        Out *o = (Out *)a.out + (OUTER ? (int64_t)e * a.M + m : m) * a.ldo;
+#pragma unroll
+        for (int j = 0; j < NT; j += 2) {
+            const int n = n0 + wn + (j >> 1) * 32 + q * 8;
+            Eight v;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) v[c] = held ? (Out)acc[i][j + (c >> 2)][c & 3] : (Out)0.f;
+            if (n + 8 <= a.F) {
+                *reinterpret_cast<Eight *>(o + n) = v;
+            } else {
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    if (n + c < a.F) o[n + c] = v[c];
+            }
+        }
+    }
+}
+
+template <int MT, int NT, typename Out, bool OUTER>
+static ftk_status launch_tile(MxProduct a, hipStream_t st)
+{
+    using S = TileShape<MT, NT>;
+    a.ntiles = (int)ceil_div(a.F, S::TN);
+    int64_t mtiles = OUTER ? ceil_div(a.M, S::TM) * a.E : a.M / S::TM + a.E + 1;
+    if (!OUTER) {
+        a.by_row = a.M < mtiles;
+        if (a.by_row) mtiles = a.M;
+    }
+    if (mtiles * a.ntiles > 0x7fffffffLL) {
+        set_error("too many tiles: M=%lld F=%d E=%d", (long long)a.M, a.F, a.E);
+        return FTK_EINVAL;
+    }
+    FTK_TRY_HIP(hipFuncSetAttribute((const void *)mx_tile_kernel<MT, NT, Out, OUTER>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                    S::LDS));
+    mx_tile_kernel<MT, NT, Out, OUTER><<<(unsigned)(mtiles * a.ntiles), 256, S::LDS, st>>>(a);
+    FTK_TRY_HIP(hipGetLastError());
+    return FTK_OK;
+}
+
+// Which kernel for packed rows.
+template <typename Out, bool OUTER>
+static ftk_status launch_packed(const MxProduct &a, hipStream_t st)
+{
+    if (a.N > 0 && a.M >= 256 && a.pitch < (1 << 20)) return launch_tile<8, 8, Out, OUTER>(a, st);
+    return launch_direct<uint8_t, Out, OUTER>(a, st);
+}
+
 static size_t packed_bytes(int64_t N, int D, size_t *codes)
 {
     const size_t c = align_up((size_t)N * mx_padded(D) / 2, 256);
@@ -267,7 +577,7 @@ ftk_status ftk_mx4_matmul(ftk_dtype out_dtype, const void *a_codes, const void *
     const MxProduct a{(const uint8_t *)a_codes, (const uint8_t *)a_scales, nullptr, 0, N, D, mx_padded(D) / MX_BLOCK,
                       (const uint8_t *)b_codes, (const uint8_t *)b_scales, M, F, E, offsets, order, k, out, ldo, 0, 0};
     return with_mx_type(out_dtype, [&](auto tag) {
-        return launch_direct<uint8_t, typename decltype(tag)::type, false>(a, (hipStream_t)hip_stream);
+        return launch_packed<typename decltype(tag)::type, false>(a, (hipStream_t)hip_stream);
     });
 }
 
@@ -285,11 +595,21 @@ ftk_status ftk_mx4_linear(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N
     const size_t need = packed_bytes(N, D, nullptr);
     if (need) FTK_TRY(check_workspace(workspace, workspace_bytes, need));
     FTK_TRY(check_device());
-    const MxProduct a{nullptr, nullptr, X, ldx, N, D, mx_padded(D) / MX_BLOCK, (const uint8_t *)b_codes,
-                      (const uint8_t *)b_scales, M, F, E, offsets, order, k, out, ldo, 0, 0};
+    hipStream_t st = (hipStream_t)hip_stream;
+    MxProduct a{nullptr, nullptr, X, ldx, N, D, mx_padded(D) / MX_BLOCK, (const uint8_t *)b_codes,
+                (const uint8_t *)b_scales, M, F, E, offsets, order, k, out, ldo, 0, 0};
+    const bool few = N == 0 || M < 256;
+    if (!few) {
+        size_t codes = 0;
+        packed_bytes(N, D, &codes);
+        uint8_t *p = (uint8_t *)workspace;
+        FTK_TRY(launch_mx_quantize(dtype, X, ldx, N, D, p, p + codes, st));
+        a.a_codes = p;
+        a.a_scales = p + codes;
+    }
     return with_mx_type(dtype, [&](auto tag) {
         using T = typename decltype(tag)::type;
-        return launch_direct<T, T, false>(a, (hipStream_t)hip_stream);
+        return few ? launch_direct<T, T, false>(a, st) : launch_packed<T, false>(a, st);
     });
 }
 
@@ -319,7 +639,7 @@ ftk_status ftk_mx4_outer(ftk_dtype out_dtype, const void *a_codes, const void *a
     MxProduct a{(const uint8_t *)a_codes, (const uint8_t *)a_scales, nullptr, 0, F, (int)rows, mx_padded(rows) / MX_BLOCK,
                 (const uint8_t *)b_codes, (const uint8_t *)b_scales, F, D, E, rows ? offsets : nullptr, nullptr, 1, out, D, 0, 0};
     return with_mx_type(out_dtype, [&](auto tag) {
-        return launch_direct<uint8_t, typename decltype(tag)::type, true>(a, (hipStream_t)hip_stream);
+        return launch_packed<typename decltype(tag)::type, true>(a, (hipStream_t)hip_stream);
     });
 }
 
