@@ -7,113 +7,148 @@
 
 namespace ftk {
 
+// Threads of both row kernels take eights of the padded rows in order, 256 at a time and MX_UNITS times a workgroup.  The
+// row of a workgroup's first one is found by one wide division, what lies between by a narrow one: a wide one for every
+// eight cost as much as the conversion (65536 x 2048 bf16 back: 98 us).
+constexpr int MX_UNITS = 4;
+struct MxUnit {
+    int64_t row;
+    int piece;  // eight of the row
+};
+template <typename F>
+__device__ __forceinline__ void for_units(int64_t N, uint32_t pieces, F &&f)
+{
+    const int64_t u0 = (int64_t)blockIdx.x * (256 * MX_UNITS), row0 = u0 / pieces;
+    const uint32_t first = (uint32_t)(u0 - row0 * pieces) + threadIdx.x;
+    const int64_t left = N * pieces - u0;
+#pragma unroll
+    for (int k = 0; k < MX_UNITS; ++k) {
+        if (k * 256 + threadIdx.x >= left) break;
+        const uint32_t at = first + k * 256, rows = at / pieces;
+        f(MxUnit{row0 + rows, (int)(at - rows * pieces)}, u0 + k * 256 + threadIdx.x);
+    }
+}
+
 // Eight elements a thread, four threads a block: the largest magnitude passes between them by two lane
 // moves.  A thread's codes are one dword, so a wave writes 256 consecutive bytes.
 template <typename T>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(const T *__restrict__ X, int64_t ldx, int64_t N, int D, int pieces,
                                                           uint32_t *__restrict__ codes, uint8_t *__restrict__ scales)
 {
-    const int64_t total = N * pieces;  // pieces: eights of a padded row, a multiple of 16
-    for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
-        const int64_t row = u / pieces;
-        const int c = (int)(u - row * pieces);
+    for_units(N, pieces, [&](MxUnit t, int64_t u) {  // (pieces: a multiple of 16)
         T v[8];
-        load8(X + row * ldx, (int64_t)c * 8, D, v);
+        load8(X + t.row * ldx, (int64_t)t.piece * 8, D, v);
         uint32_t m = max8(v);
         m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0xB1, 0xf, 0xf, true));
         m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x4E, 0xf, 0xf, true));
         const uint32_t b = mx_scale_byte(m);
         codes[u] = mx_pack8(v, mx_scale_float(b));
-        if ((c & 3) == 0) scales[u >> 2] = (uint8_t)b;
-    }
+        if ((t.piece & 3) == 0) scales[u >> 2] = (uint8_t)b;
+    });
 }
 
-// Across the rows: a lane has the 32 rows of a block in two neighbouring columns, a wave 128 columns.
-// Workgroup: four blocks (128 rows), the 64 bytes of codes and four scales that a column has of them.
+// Across the rows: a lane has the 32 rows of a block in two neighbouring columns, a wave 128 columns and two
+// blocks, a workgroup 256 rows: 128 bytes of codes and eight scales of every column, brought together in LDS so that
+// they leave by whole lines (written by the lanes that made them, 16 bytes at a time: 33792 x 4096 bf16 171 us).  Workgroups that
+// share a line of scales run near each other on one XCD.
+constexpr int ACROSS_ROWS = 256, ACROSS_COLS = 128;
 template <typename T>
 __global__ __launch_bounds__(256) void mx_quantize_across_kernel(const T *__restrict__ X, int64_t ldx, int64_t N, int D,
-                                                                 int64_t nblocks, uint4 *__restrict__ codes,
+                                                                 int64_t nblocks, int rowgroups, uint32_t *__restrict__ codes,
                                                                  uint8_t *__restrict__ scales)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t blk = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);  // of 32 rows; nblocks is a multiple of 4
-    const int d = ((int)blockIdx.y * 64 + lane) * 2;
-    if (d >= D) return;
+    // a column's 32 dwords of codes and two of scales, and one more against bank conflicts
+    constexpr int LINE = 35;
+    __shared__ uint32_t line[ACROSS_COLS * LINE];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    uint32_t id = blockIdx.x;
+    if (gridDim.x % 8 == 0) id = (id & 7) * (gridDim.x / 8) + id / 8;
+    const int rg = id % rowgroups, c0 = (int)(id / rowgroups) * ACROSS_COLS;
+    const int d = c0 + lane * 2;
     typedef T Pair __attribute__((ext_vector_type(2), aligned(sizeof(T))));
     const bool both = d + 1 < D;
-    T v[2][32];
-    const int64_t r0 = blk * 32;
 #pragma unroll
-    for (int r = 0; r < 32; ++r) {
-        v[0][r] = v[1][r] = (T)0.f;
-        if (r0 + r < N) {
-            const T *x = X + (r0 + r) * ldx + d;
-            if (both) {
-                const Pair p = *reinterpret_cast<const Pair *>(x);
+    for (int h = 0; h < 2; ++h) {
+        const int b = w * 2 + h;
+        const int64_t r0 = (int64_t)rg * ACROSS_ROWS + b * 32;
+        T v[2][32];
+        if (r0 + 32 <= N && both) {
+            const T *x = X + r0 * ldx + d;
+#pragma unroll
+            for (int r = 0; r < 32; ++r) {
+                const Pair p = *reinterpret_cast<const Pair *>(x + r * ldx);
                 v[0][r] = p[0];
                 v[1][r] = p[1];
-            } else {
-                v[0][r] = *x;
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < 32; ++r) {
+                v[0][r] = r0 + r < N && d < D ? X[(r0 + r) * ldx + d] : (T)0.f;
+                v[1][r] = r0 + r < N && both ? X[(r0 + r) * ldx + d + 1] : (T)0.f;
             }
         }
-    }
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        if (c && !both) break;
-        uint32_t m = 0;
+        for (int c = 0; c < 2; ++c) {
+            uint32_t m = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) m = max(m, max8(&v[c][8 * i]));
-        const uint32_t b = mx_scale_byte(m);
-        const float s = mx_scale_float(b);
-        codes[(int64_t)(d + c) * nblocks + blk] =
-            make_uint4(mx_pack8(&v[c][0], s), mx_pack8(&v[c][8], s), mx_pack8(&v[c][16], s), mx_pack8(&v[c][24], s));
-        scales[(int64_t)(d + c) * nblocks + blk] = (uint8_t)b;
+            for (int i = 0; i < 4; ++i) m = max(m, max8(&v[c][8 * i]));
+            const uint32_t s = mx_scale_byte(m);
+            const float f = mx_scale_float(s);
+            uint32_t *l = line + (lane * 2 + c) * LINE;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) l[b * 4 + i] = mx_pack8(&v[c][8 * i], f);
+            reinterpret_cast<uint8_t *>(l + 32)[b] = (uint8_t)s;
+        }
     }
-}
-
-__device__ __forceinline__ float mx_value(uint32_t code, uint32_t byte)
-{
-    // magnitude by its two bits of exponent and one of mantissa: twice it is 0, 1, 2, 3, 4, 6, 8, 12
-    const uint32_t i = code & 7;
-    const float twice = i < 2 ? (float)i : (float)((2 + (i & 1)) << ((i >> 1) - 1));
-    const float v = ldexpf(twice, (int)byte - 128);
-    return byte == 255 ? __uint_as_float(0x7fc00000u) : code & 8 ? -v : v;
+    __syncthreads();
+    const int blocks = (int)(nblocks - (int64_t)rg * 8 < 8 ? nblocks - (int64_t)rg * 8 : 8);  // 4 or 8
+    for (int i = threadIdx.x; i < ACROSS_COLS * 8; i += 256) {
+        const int col = i >> 3, piece = i & 7;
+        if (c0 + col >= D || piece >= blocks) continue;
+        const uint32_t *l = line + col * LINE;
+        const int64_t at = (int64_t)(c0 + col) * nblocks + (int64_t)rg * 8;
+        *reinterpret_cast<uint4 *>(codes + (at + piece) * 4) = make_uint4(l[piece * 4], l[piece * 4 + 1], l[piece * 4 + 2], l[piece * 4 + 3]);
+        if ((piece & 3) == 0) *reinterpret_cast<uint32_t *>(scales + at + piece) = l[32 + (piece >> 2)];
+    }
 }
 
 template <typename T>
 __global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint32_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                                                             int64_t N, int D, int pieces, T *__restrict__ out, int64_t ldo)
 {
-    const int64_t total = N * pieces;
-    for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
-        const int64_t row = u / pieces;
-        const int c = (int)(u - row * pieces) * 8;
-        if (c >= D) continue;
+    typedef float pair __attribute__((ext_vector_type(2)));
+    for_units(N, pieces, [&](MxUnit t, int64_t u) {
+        const int c = t.piece * 8;
+        if (c >= D) return;
         const uint32_t q = codes[u], b = scales[u >> 2];
+        const float s = mx_scale_float(b);
+        const pair p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, s, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, s, 1),
+                           __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, s, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, s, 3)};
         T v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = (T)mx_value(q >> (4 * e), b);
-        T *o = out + row * ldo + c;
+        for (int e = 0; e < 8; ++e) v[e] = (T)(b == 255 ? __uint_as_float(0x7fc00000u) : p[e >> 1][e & 1]);
+        T *o = out + t.row * ldo + c;
         if (c + 8 <= D) {
 #pragma unroll
-            for (int p = 0; p < 8 / PIECE<T>; ++p) {
+            for (int k = 0; k < 8 / PIECE<T>; ++k) {
                 PieceOf<T> w;
 #pragma unroll
-                for (int e = 0; e < PIECE<T>; ++e) w[e] = v[p * PIECE<T> + e];
-                put_piece(o + p * PIECE<T>, w);
+                for (int e = 0; e < PIECE<T>; ++e) w[e] = v[k * PIECE<T> + e];
+                put_piece(o + k * PIECE<T>, w);
             }
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 if (c + e < D) o[e] = v[e];
         }
-    }
+    });
 }
 
-static int mx_grid(int64_t threads)
+// workgroups of a row kernel, 0 where there are too many
+static unsigned mx_grid(int64_t units)
 {
-    const int64_t g = ceil_div(threads, 256);
-    return (int)(g < 65536 ? g : 65536);
+    const int64_t g = ceil_div(units, 256 * MX_UNITS);
+    return g <= 0x7fffffffLL ? (unsigned)g : 0;
 }
 
 ftk_status launch_mx_quantize(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N, int D, void *codes, void *scales,
@@ -122,6 +157,10 @@ ftk_status launch_mx_quantize(ftk_dtype dtype, const void *X, int64_t ldx, int64
     return with_mx_type(dtype, [&](auto tag) {
         using T = typename decltype(tag)::type;
         const int pieces = (int)(mx_padded(D) / 8);
+        if (!mx_grid(N * pieces)) {
+            set_error("too many elements (N=%lld D=%d)", (long long)N, D);
+            return FTK_EINVAL;
+        }
         mx_quantize_kernel<T><<<mx_grid(N * pieces), 256, 0, st>>>((const T *)X, ldx, N, D, pieces, (uint32_t *)codes,
                                                                    (uint8_t *)scales);
         FTK_TRY_HIP(hipGetLastError());
@@ -161,15 +200,15 @@ ftk_status ftk_mx4_quantize(ftk_dtype dtype, const void *X, int64_t ldx, int64_t
     if (N == 0) return FTK_OK;
     hipStream_t st = (hipStream_t)hip_stream;
     if (!transpose) return launch_mx_quantize(dtype, X, ldx, N, D, codes, scales, st);
-    const int64_t nblocks = mx_padded(N) / MX_BLOCK, wgs = nblocks / 4;
-    if (ceil_div(D, 128) > 65535) {
-        set_error("transpose: D = %d is too large (at most %d)", D, 128 * 65535);
+    const int64_t nblocks = mx_padded(N) / MX_BLOCK, rowgroups = ceil_div(N, ACROSS_ROWS), wgs = rowgroups * ceil_div(D, ACROSS_COLS);
+    if (wgs > 0x7fffffffLL) {
+        set_error("transpose: too many elements (N=%lld D=%d)", (long long)N, D);
         return FTK_EINVAL;
     }
     return with_mx_type(dtype, [&](auto tag) {
         using T = typename decltype(tag)::type;
-        mx_quantize_across_kernel<T><<<dim3((unsigned)wgs, (unsigned)ceil_div(D, 128)), 256, 0, st>>>(
-            (const T *)X, ldx, N, D, nblocks, (uint4 *)codes, (uint8_t *)scales);
+        mx_quantize_across_kernel<T><<<(unsigned)wgs, 256, 0, st>>>((const T *)X, ldx, N, D, nblocks, (int)rowgroups,
+                                                                     (uint32_t *)codes, (uint8_t *)scales);
         FTK_TRY_HIP(hipGetLastError());
         return FTK_OK;
     });
@@ -183,6 +222,10 @@ ftk_status ftk_mx4_dequantize(ftk_dtype dtype, const void *codes, const void *sc
     return with_mx_type(dtype, [&](auto tag) {
         using T = typename decltype(tag)::type;
         const int pieces = (int)(mx_padded(D) / 8);
+        if (!mx_grid(N * pieces)) {
+            set_error("too many elements (N=%lld D=%d)", (long long)N, D);
+            return FTK_EINVAL;
+        }
         mx_dequantize_kernel<T><<<mx_grid(N * pieces), 256, 0, (hipStream_t)hip_stream>>>(
             (const uint32_t *)codes, (const uint8_t *)scales, N, D, pieces, (T *)out, ldo);
         FTK_TRY_HIP(hipGetLastError());

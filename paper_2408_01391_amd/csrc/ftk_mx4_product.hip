@@ -229,8 +229,8 @@ static ftk_status launch_direct(MxProduct a, hipStream_t st)
 // free as long as both operands agree: lane quarter q takes blocks 2q and 2q + 1, so that the scales of both steps
 // are one 16-bit word, out of which the instruction picks the byte.
 //
-// LDS rows are lines of eight 16-byte pieces, piece p of row r at place p ^ key(r): the eight lanes that LDS serves
-// at once then read eight different places.  The copy keeps the order of its lanes, so it is the lanes' addresses
+// LDS rows are lines of eight 16-byte pieces, piece p at place p ^ key: the key is half the lane row that reads the line, so
+// that the sixteen lanes that LDS serves at once read sixteen different places of its 256 bytes.  The copy keeps the order of its lanes, so it is the lanes' addresses
 // that are permuted, within a line.
 // Column tile j of a wave has, for lane row r, column 32 * (j / 2) + 8 * (r / 4) + 4 * (j % 2) + r % 4: two
 // tiles together give a lane eight consecutive columns to store.
@@ -298,8 +298,7 @@ __global__ __launch_bounds__(256, MT* NT >= 64 ? 1 : 2) void mx_tile_kernel(MxPr
     }
     __syncthreads();
     if (steps > 0) {
-        // What this lane copies: rows lane / 8 of eights of rows, one piece of each.  The key of A's rows goes with the row, that
-        // of B's with the lane row that reads them.
+        // What this lane copies: rows lane / 8 of eights of rows, one piece of each.
         const uint32_t pitch = (uint32_t)a.pitch * 16;
         const int slot = lane & 7, l8 = lane >> 3;
         const uint8_t *abase = a.a_codes + (int64_t)k0 * 64, *bbase = a.b_codes + ((int64_t)k0 * 64 + (int64_t)n0 * pitch);
@@ -312,9 +311,11 @@ __global__ __launch_bounds__(256, MT* NT >= 64 ? 1 : 2) void mx_tile_kernel(MxPr
         uint32_t arow[MT], boff[NT];  // row of A; offset from the column tile's first line
 #pragma unroll
         for (int i = 0; i < MT; ++i) arow[i] = (uint32_t)max(0, source[(w * MT + i) * 8 + l8]);
-        const int pa = slot ^ l8, pb = slot ^ (l8 & 3);  // pieces; of B ^ 4 in every second eight
+        // the piece of copy i of A or B
+        auto piece_a = [&](int i) __attribute__((always_inline)) { return slot ^ (l8 >> 1) ^ (i & 1) * 4; };
+        auto piece_b = [&](int i) __attribute__((always_inline)) { return slot ^ ((l8 >> 1) & 1) ^ ((w * NT + i) & 3) * 2; };
 #pragma unroll
-        for (int i = 0; i < NT; ++i) boff[i] = min((w * NT + i) * 8 + l8, blast) * pitch + (pb ^ (i & 1) * 4) * 16;
+        for (int i = 0; i < NT; ++i) boff[i] = __umul24(min((w * NT + i) * 8 + l8, blast), pitch) + piece_b(i) * 16;
         const bool small = a.pitch < 16;  // all scales of a row at once, and the next row may not be there to be read
         constexpr int SN = (S::ROWS / 64 + 3) / 4;
         if (small) {
@@ -333,12 +334,12 @@ __global__ __launch_bounds__(256, MT* NT >= 64 ? 1 : 2) void mx_tile_kernel(MxPr
             if (c < MT) {
                 uint32_t row = arow[c];
                 asm volatile("" : "+v"(row));  // (the product would be kept for all stages in two registers a row)
-                const int p = half ? pa & 3 : pa;
+                const int p = half ? piece_a(c) & 3 : piece_a(c);
                 to_lds16_at(abase + (int64_t)st * 128 + p * 16 + (uint64_t)row * pitch, to + (w * MT + c) * 1024);
             } else {
                 const int i = c - MT;
                 uint32_t o = boff[i];
-                if (half) o -= ((pb ^ (i & 1) * 4) & 4) * 16;
+                if (half) o -= (piece_b(i) & 4) * 16;
                 to_lds16_from(bbase + (int64_t)st * 128, o, to + S::TM * 128 + (w * NT + i) * 1024);
             }
         };
@@ -359,7 +360,7 @@ __global__ __launch_bounds__(256, MT* NT >= 64 ? 1 : 2) void mx_tile_kernel(MxPr
             const int64_t o = (st & ~1) * 8, at = small || o < last ? o : last;
             return (int)((st & 1) * 8 + (o - at)) + ((st >> 1) & 1) * S::SCALES;
         };
-        const int lrow = wm + r, lcol = wn + (r >> 2) * 8 + (r & 3), key = r & 7;
+        const int lrow = wm + r, lcol = wn + (r >> 2) * 8 + (r & 3), key = r >> 1;
         const uint8_t *const fa = lds + lrow * 128, *const fb = lds + (S::TM + lcol) * 128;
         const uint8_t *const sa = sc + lrow * 16, *const sb = sc + (S::TM + lcol) * 16;
         uint4 fra[MT], frb[2][NT];
