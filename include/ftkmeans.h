@@ -342,7 +342,9 @@ ftk_status ftk_seeded_indices(uint64_t seed, int64_t N, int32_t K, int64_t *idx_
  * dtype: any.  Row arrays have unit stride along a row and a row stride (ldx, ... in elements, >= D).
  * Weights are float, for FTK_F64 double.  Sums are held in 32 bits (FTK_F64: 64), in ascending j, and rounded
  * once.  Everything is bitwise reproducible.
- * Limits: N * k + E * (align - 1) < 2^31, 1 <= E <= 8192, 1 <= k <= 64, 1 <= align <= 65536. */
+ * Limits: N * k + E * (align - 1) < 2^31, 1 <= E <= 8192, 1 <= k <= 64, 1 <= align <= 65536.
+ * Up to FTK_ROUTE_FEW slots (N * k) no workspace is needed: NULL will do. */
+#define FTK_ROUTE_FEW 1024
 int64_t ftk_route_rows(int64_t N, int32_t k, int32_t E, int32_t align); /* -1: bad arguments */
 size_t ftk_route_workspace_bytes(int64_t N, int32_t k, int32_t E);      /* 0: bad arguments */
 
@@ -407,20 +409,19 @@ ftk_status ftk_mx4_dequantize(ftk_dtype dtype, const void *codes, const void *sc
  *   order [M], k     : src(m) = order[m] / k, and an output row whose order[m] is -1 becomes zero; NULL: src(m) = m.
  *   out [M x F]      : FTK_F32, FTK_BF16 or FTK_F16, row stride ldo.  N must be at least M where order is NULL.
  * Products of 4-bit elements are exact, sums are held in 32 bits and rounded once to out's type.
- * workspace: ftk_mx4_workspace_bytes(0, 0, M, F) bytes (may be 0: then NULL is allowed).
  * Limits: M < 2^31, F and D < 2^24, E <= 8192, E * F < 2^31. */
 ftk_status ftk_mx4_matmul(ftk_dtype out_dtype, const void *a_codes, const void *a_scales, int64_t N,
                           const void *b_codes, const void *b_scales, int64_t M, int32_t F, int32_t D, int32_t E,
                           const int32_t *offsets /* nullable */, const int32_t *order /* nullable */, int32_t k,
-                          void *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *hip_stream);
+                          void *out, int64_t ldo, void *hip_stream);
 
 /* The same from dense rows X [N x D] of `dtype`, packed on the way exactly as ftk_mx4_quantize does; out has
- * their type.  workspace: ftk_mx4_workspace_bytes(N, D, M, F) bytes. */
+ * their type.  workspace: ftk_mx4_workspace_bytes(N, D, M) bytes; where that is 0, as for few rows, NULL will do. */
 ftk_status ftk_mx4_linear(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N, const void *b_codes,
                           const void *b_scales, int64_t M, int32_t F, int32_t D, int32_t E,
                           const int32_t *offsets /* nullable */, const int32_t *order /* nullable */, int32_t k,
                           void *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *hip_stream);
-size_t ftk_mx4_workspace_bytes(int64_t N, int32_t D, int64_t M, int32_t F);
+int64_t ftk_mx4_workspace_bytes(int64_t N, int32_t D, int64_t M); /* -1: bad arguments */
 
 /* Sums over the rows of every expert, the gradient of the experts' matrices:
  *   out[e][f, d] = sum over p in [offsets[e], offsets[e + 1]) of A[f, p] * B[d, p]

@@ -102,12 +102,12 @@ def load():
     L.ftk_mx4_quantize.restype = i32
     L.ftk_mx4_dequantize.argtypes = [i32, vp, vp, i64, i32, vp, i64, vp]
     L.ftk_mx4_dequantize.restype = i32
-    L.ftk_mx4_matmul.argtypes = [i32, vp, vp, i64, vp, vp, i64, i32, i32, i32, vp, vp, i32, vp, i64, vp, sz, vp]
+    L.ftk_mx4_matmul.argtypes = [i32, vp, vp, i64, vp, vp, i64, i32, i32, i32, vp, vp, i32, vp, i64, vp]
     L.ftk_mx4_matmul.restype = i32
     L.ftk_mx4_linear.argtypes = [i32, vp, i64, i64, vp, vp, i64, i32, i32, i32, vp, vp, i32, vp, i64, vp, sz, vp]
     L.ftk_mx4_linear.restype = i32
-    L.ftk_mx4_workspace_bytes.argtypes = [i64, i32, i64, i32]
-    L.ftk_mx4_workspace_bytes.restype = sz
+    L.ftk_mx4_workspace_bytes.argtypes = [i64, i32, i64]
+    L.ftk_mx4_workspace_bytes.restype = i64
     L.ftk_mx4_outer.argtypes = [i32, vp, vp, vp, vp, i64, i32, i32, i32, vp, vp, vp]
     L.ftk_mx4_outer.restype = i32
     L.ftk_last_error.restype = ctypes.c_char_p
@@ -146,7 +146,8 @@ def _dev2d(t: torch.Tensor, name: str) -> torch.Tensor:
 
 
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    # the current stream's handle, without the Stream object that torch.cuda.current_stream() makes (3 of 12 us of a small call)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _ptr(t):
@@ -401,6 +402,7 @@ def kmeans_fit(X, K, iters, seed=0, C_init=None, ft_mode=FT_OFF, stats=None, wor
 # ---- rows sorted by label and back -----------------------------------------------------------
 
 _ROW_DTYPES = {torch.float32: F32, torch.float64: F64, torch.bfloat16: BF16, torch.float16: F16}
+ROUTE_FEW = 1024  # slots that are sorted without a workspace
 _MX_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
 
@@ -415,13 +417,26 @@ def _row_stride(t: torch.Tensor, name: str) -> int:
     """Row stride of a 2-D device tensor whose rows are contiguous."""
     if not t.is_cuda:
         raise ValueError("%s must live on the GPU" % name)
-    if t.dim() != 2 or (t.shape[0] > 0 and t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("%s must be a 2-D tensor of contiguous rows" % name)
-    if t.shape[0] <= 1:
-        return t.shape[1]
-    if t.stride(0) < t.shape[1]:
-        raise ValueError("%s: its rows overlap" % name)
-    return t.stride(0)
+    strides = t.stride()
+    if len(strides) == 2:
+        rows, D = t.shape
+        ld, unit = strides
+        if rows <= 1:
+            ld = D
+        if unit == 1 or D <= 1 or rows == 0:
+            if ld < D:
+                raise ValueError("%s: its rows overlap" % name)
+            return ld
+    raise ValueError("%s must be a 2-D tensor of contiguous rows" % name)
+
+
+def _workspace(workspace, need, device):
+    """(workspace, address, bytes): the caller's workspace, or a new one where any is needed, to be held until the call is enqueued."""
+    if workspace is None:
+        if not need:
+            return None, None, 0
+        workspace = torch.empty(need + 256, dtype=torch.uint8, device=device)
+    return workspace, *_ws_args(workspace)
 
 
 def _index(t: torch.Tensor, name: str, *shape) -> torch.Tensor:
@@ -431,12 +446,13 @@ def _index(t: torch.Tensor, name: str, *shape) -> torch.Tensor:
 
 
 def _new_rows(out, rows, D, like, name, dtype=None):
+    """(out, its row stride): the caller's, or a new one."""
     dtype = like.dtype if dtype is None else dtype
     if out is None:
-        return torch.empty(rows, D, dtype=dtype, device=like.device)
+        return torch.empty((rows, D), dtype=dtype, device=like.device), D
     if out.shape != (rows, D) or out.dtype != dtype:
         raise ValueError("%s must be [%d, %d] of %s" % (name, rows, D, dtype))
-    return out
+    return out, _row_stride(out, name)
 
 
 class Route:
@@ -487,22 +503,19 @@ def _route_args(labels, E, align, route, workspace):
     if route is None:
         rows, dev = route_rows(N, k, E, align), labels.device
         whole = torch.empty(2 * E + 1 + rows + N * k, dtype=torch.int32, device=dev)
-        offsets, counts, order, pos = whole.split((E + 1, E, rows, N * k))
+        offsets, counts, order, pos = whole.split_with_sizes((E + 1, E, rows, N * k))
         route = Route(offsets, counts, order, pos.view(N, k), align)
     else:
         if route.check() != (N, k) or route.experts != E or route.align != align:
             raise ValueError("route is not one of %d x %d slots, %d experts and align %d" % (N, k, E, align))
         _index(route.counts, "counts", E)
-    need = route_workspace_bytes(N, k, E)
-    if workspace is None:
-        workspace = torch.empty(need + 256, dtype=torch.uint8, device=labels.device)
-    return labels, N, k, route, workspace
+    need = route_workspace_bytes(N, k, E) if N * k > ROUTE_FEW else 0
+    return labels, N, k, route, *_workspace(workspace, need, labels.device)
 
 
 def route_plan(labels, E, align=1, route=None, workspace=None):
     """Sorts the slots of labels (int32 [N] or [N, k]; outside [0, E): dropped) by expert.  Returns a Route."""
-    labels, N, k, route, workspace = _route_args(labels, E, align, route, workspace)
-    wp, wn = _ws_args(workspace)
+    labels, N, k, route, workspace, wp, wn = _route_args(labels, E, align, route, workspace)
     _check(load().ftk_route_plan(labels.data_ptr(), N, k, E, align, route.rows, route.offsets.data_ptr(),
                                  route.counts.data_ptr(), route.order.data_ptr(), route.pos.data_ptr(), wp, wn, _stream()))
     return route
@@ -510,16 +523,15 @@ def route_plan(labels, E, align=1, route=None, workspace=None):
 
 def route_dispatch(X, labels, E, align=1, out=None, route=None, workspace=None):
     """route_plan and route_gather in one call.  Returns (sorted rows [rows, D], Route)."""
-    labels, N, k, route, workspace = _route_args(labels, E, align, route, workspace)
+    labels, N, k, route, workspace, wp, wn = _route_args(labels, E, align, route, workspace)
     ld = _row_stride(X, "X")
     if X.shape[0] != N:
         raise ValueError("X must have a row for each of the %d tokens" % N)
-    out = _new_rows(out, route.rows, X.shape[1], X, "out")
-    wp, wn = _ws_args(workspace)
+    out, ldo = _new_rows(out, route.rows, X.shape[1], X, "out")
     _check(load().ftk_route_dispatch(_row_code(X, "X"), X.data_ptr(), ld, X.shape[1], labels.data_ptr(), N, k, E, align,
                                      route.rows, route.offsets.data_ptr(), route.counts.data_ptr(),
                                      route.order.data_ptr(), route.pos.data_ptr(), out.data_ptr(),
-                                     _row_stride(out, "out"), wp, wn, _stream()))
+                                     ldo, wp, wn, _stream()))
     return out, route
 
 
@@ -537,10 +549,10 @@ def route_gather(X, route, weights=None, out=None):
     ld = _row_stride(X, "X")
     if X.shape[0] != N:
         raise ValueError("X must have a row for each of the %d tokens" % N)
-    out = _new_rows(out, route.rows, X.shape[1], X, "out")
+    out, ldo = _new_rows(out, route.rows, X.shape[1], X, "out")
     _check(load().ftk_route_gather(_row_code(X, "X"), X.data_ptr(), ld, N, k, X.shape[1], route.order.data_ptr(),
                                    route.pos.data_ptr(), route.rows, _ptr(_weights(weights, X, N, k)), out.data_ptr(),
-                                   _row_stride(out, "out"), _stream()))
+                                   ldo, _stream()))
     return out
 
 
@@ -550,10 +562,10 @@ def route_combine(Y, route, weights=None, out=None):
     ld = _row_stride(Y, "Y")
     if Y.shape[0] != route.rows:
         raise ValueError("Y must have the %d sorted rows" % route.rows)
-    out = _new_rows(out, N, Y.shape[1], Y, "out")
+    out, ldo = _new_rows(out, N, Y.shape[1], Y, "out")
     _check(load().ftk_route_combine(_row_code(Y, "Y"), Y.data_ptr(), ld, route.rows, route.pos.data_ptr(),
                                     _ptr(_weights(weights, Y, N, k)), N, k, Y.shape[1], out.data_ptr(),
-                                    _row_stride(out, "out"), _stream()))
+                                    ldo, _stream()))
     return out
 
 
@@ -566,11 +578,11 @@ def route_combine_grad(dOut, Y, route, weights, dY=None, dweights=None):
     if dOut.shape[0] != N or tuple(Y.shape) != (route.rows, D) or Y.dtype != dOut.dtype:
         raise ValueError("dOut [N, D] and Y [rows, D] must share type and D")
     _weights(weights, Y, N, k)
-    dY = _new_rows(dY, route.rows, D, Y, "dY")
+    dY, ldo = _new_rows(dY, route.rows, D, Y, "dY")
     dweights = torch.empty_like(weights) if dweights is None else _weights(dweights, Y, N, k)
     _check(load().ftk_route_combine_grad(_row_code(Y, "Y"), dOut.data_ptr(), ldg, Y.data_ptr(), ldy,
                                          route.order.data_ptr(), route.pos.data_ptr(), route.rows, weights.data_ptr(),
-                                         N, k, D, dY.data_ptr(), _row_stride(dY, "dY"), dweights.data_ptr(), _stream()))
+                                         N, k, D, dY.data_ptr(), ldo, dweights.data_ptr(), _stream()))
     return dY, dweights
 
 
@@ -620,11 +632,11 @@ def mx4_quantize(X, transpose=False, out=None):
 def mx4_dequantize(q, dtype=torch.float32, out=None):
     """The values of packed rows, [N, D]."""
     q.check("q")
-    out = _new_rows(out, q.N, q.D, q.codes, "out", dtype)
+    out, ldo = _new_rows(out, q.N, q.D, q.codes, "out", dtype)
     if q.D == 0:
         return out
     _check(load().ftk_mx4_dequantize(_row_code(out, "out", _MX_DTYPES), q.codes.data_ptr(), q.scales.data_ptr(), q.N, q.D,
-                                     out.data_ptr(), _row_stride(out, "out"), _stream()))
+                                     out.data_ptr(), ldo, _stream()))
     return out
 
 
@@ -650,11 +662,18 @@ def mx4_matmul(A, B, route=None, gather=False, out=None, out_dtype=torch.bfloat1
     if A.D != B.D:
         raise ValueError("A and B must share D (got %d and %d)" % (A.D, B.D))
     E, F, M, offsets, order, k = _groups(B, route, gather, A.N)
-    out = _new_rows(out, M, F, A.codes, "out", out_dtype if out is None else out.dtype)
+    out, ldo = _new_rows(out, M, F, A.codes, "out", out_dtype if out is None else out.dtype)
     _check(load().ftk_mx4_matmul(_row_code(out, "out", _MX_DTYPES), A.codes.data_ptr(), A.scales.data_ptr(), A.N,
                                  B.codes.data_ptr(), B.scales.data_ptr(), M, F, A.D, E, _ptr(offsets), _ptr(order), k,
-                                 out.data_ptr(), _row_stride(out, "out"), None, 0, _stream()))
+                                 out.data_ptr(), ldo, _stream()))
     return out
+
+
+def mx4_workspace_bytes(N: int, D: int, M: int) -> int:
+    n = load().ftk_mx4_workspace_bytes(N, D, M)
+    if n < 0:
+        raise FtkError(1, load().ftk_last_error().decode())
+    return n
 
 
 def mx4_linear(X, B, route=None, gather=False, out=None, workspace=None):
@@ -664,14 +683,11 @@ def mx4_linear(X, B, route=None, gather=False, out=None, workspace=None):
     if D != B.D:
         raise ValueError("X and B must share D (got %d and %d)" % (D, B.D))
     E, F, M, offsets, order, k = _groups(B, route, gather, N)
-    out = _new_rows(out, M, F, X, "out")
-    if workspace is None:
-        need = load().ftk_mx4_workspace_bytes(N, D, M, F)
-        workspace = torch.empty(need + 256, dtype=torch.uint8, device=X.device)
-    wp, wn = _ws_args(workspace)
+    out, ldo = _new_rows(out, M, F, X, "out")
+    workspace, wp, wn = _workspace(workspace, mx4_workspace_bytes(N, D, M), X.device)
     _check(load().ftk_mx4_linear(_row_code(X, "X", _MX_DTYPES), X.data_ptr(), ld, N, B.codes.data_ptr(),
                                  B.scales.data_ptr(), M, F, D, E, _ptr(offsets), _ptr(order), k, out.data_ptr(),
-                                 _row_stride(out, "out"), wp, wn, _stream()))
+                                 ldo, wp, wn, _stream()))
     return out
 
 

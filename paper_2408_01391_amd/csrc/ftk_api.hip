@@ -352,6 +352,13 @@ ftk_status check_device()
     return FTK_OK;
 }
 
+ftk_status allow_lds(const void *kernel, size_t bytes)
+{
+    if (bytes > 65536)
+        FTK_TRY_HIP(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    return FTK_OK;
+}
+
 static bool g_profile = false;
 static std::vector<std::pair<hipEvent_t, hipEvent_t>> g_profile_events;
 

@@ -28,6 +28,8 @@ ftk_status hip_failed(hipError_t e, const char *what);
 ftk_status check_ptr(const void *p, size_t align, const char *name);
 ftk_status check_workspace(void *ws, size_t bytes, size_t need);
 ftk_status check_device();
+// lets a kernel have more than 64 KB of dynamic LDS on the current device
+ftk_status allow_lds(const void *kernel, size_t bytes);
 
 static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }

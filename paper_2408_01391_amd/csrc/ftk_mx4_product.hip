@@ -55,23 +55,26 @@ template <int TM>
 __device__ __forceinline__ bool find_tile(const MxProduct &a, int64_t t, RowTile &r)
 {
     const int lane = threadIdx.x & 63;
+    auto number = [&](int64_t first, int e) { return a.by_row ? first : first / TM + e; };
     int lo = 0, hi = a.E;
-    while (lo < hi) {
+    while (hi - lo > 62) {
         const int step = (hi - lo + 63) / 64, e = lo + (lane + 1) * step;
-        bool below = false;
-        if (e <= hi) below = a.by_row ? first_row(a, e) <= t : first_row(a, e) / TM + e <= t;
-        lo += __popcll(__ballot(below)) * step;
+        lo += __popcll(__ballot(e <= hi && number(first_row(a, e), e) <= t)) * step;
         hi = min(hi, lo + step - 1);
     }
+    // lane i: expert lo + i, up to the end of hi (rows are less than 2^31)
     lo = __builtin_amdgcn_readfirstlane(lo);
-    const int64_t first = first_row(a, lo);
-    r.e = lo;
-    r.end = first_row(a, lo + 1);
+    const int f = (int)first_row(a, lo + lane);
+    const int below = __builtin_amdgcn_readfirstlane(
+        (int)__popcll(__ballot(lane > 0 && lo + lane <= hi && number((int64_t)f, lo + lane) <= t)));
+    const int64_t first = __builtin_amdgcn_readlane(f, below);
+    r.e = lo + below;
+    r.end = __builtin_amdgcn_readlane(f, below + 1);
     if (a.by_row) {
         if (t < first || (t - first) % TM) return false;
         r.m0 = t;
     } else {
-        r.m0 = first + (t - (first / TM + lo)) * TM;
+        r.m0 = first + (t - (first / TM + r.e)) * TM;
     }
     return r.m0 >= first && r.m0 < r.end;
 }
@@ -121,21 +124,32 @@ __device__ __forceinline__ void mx_mma_in_place(float4v &c, uint4 b, uint32_t bs
         asm("s_nop 1\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[1,1,0] op_sel_hi:[0,0,0] cbsz:4 blgp:4"
             : "+a"(c) : "v"(x), "v"(y), "v"(bs), "v"(as));
 }
-__device__ __forceinline__ void mx_sums_done()
+// Waits for the last of them.  The sums pass through empty statements before and behind the wait, so that no product is moved
+// behind it and no look at a sum before it.
+template <int MT, int NT>
+__device__ __forceinline__ void mx_sums_done(float4v (&c)[MT][NT])
 {
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) asm volatile("" : "+a"(c[i][j]));
+    asm volatile("s_nop 15\n\ts_nop 15");
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) asm volatile("" : "+a"(c[i][j]));
 }
 
-// Few rows: 16 output rows by 16 * CT columns a workgroup, whose four waves share the steps of 128 elements out between
-// them and add their sums up in LDS.  Operands go from memory straight to registers; a dense row is packed on
-// the way, the whole block of 32 within a lane.
-template <typename Src, typename Out, int CT, bool OUTER>
-__global__ __launch_bounds__(256) void mx_direct_kernel(MxProduct a)
+// Few rows: 16 output rows by 16 * CT columns a workgroup, whose WAVES waves share the steps of 128 elements out between
+// them, a run each, and add their sums up in LDS.  Operands go from memory straight to registers, UNROLL steps
+// at a time, all requested before the first is used: with one row the weights' way from memory is all the time there
+// is.  A dense row is packed on the way, the whole block of 32 within a lane.
+template <typename Src, typename Out, int CT, int WAVES, bool OUTER>
+__global__ __launch_bounds__(64 * WAVES) void mx_direct_kernel(MxProduct a)
 {
     constexpr bool DENSE = !std::is_same<Src, uint8_t>::value;
-    __shared__ float4v part[4][CT][64];
+    constexpr int UNROLL = 4 / CT > 1 ? 4 / CT : 1;
+    __shared__ float4v part[WAVES][CT][64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, row = lane & 15, q = lane >> 4;
     const int64_t t = blockIdx.x / a.ntiles;
     const int n0 = (int)(blockIdx.x - t * a.ntiles) * 16 * CT;
@@ -164,47 +178,80 @@ __global__ __launch_bounds__(256) void mx_direct_kernel(MxProduct a)
 #pragma unroll
     for (int i = 0; i < CT; ++i) acc[i] = float4v{0, 0, 0, 0};
     const int64_t brow = OUTER ? 0 : (int64_t)e * a.F;
-    for (int s = k0 + w; s < k1; s += 4) {
+    const uint8_t *bc[CT], *bs[CT];
+#pragma unroll
+    for (int i = 0; i < CT; ++i) {
+        const int64_t at = (brow + min(n0 + 16 * i + row, a.F - 1)) * a.pitch + q;
+        bc[i] = a.b_codes + at * 16;
+        bs[i] = a.b_scales + at;
+    }
+    auto read_b = [&](int s, int i, uint4 &c, uint32_t &x) {
+        c = *reinterpret_cast<const uint4 *>(bc[i] + (int64_t)s * 64);
+        x = bs[i][(int64_t)s * 4];
+    };
+    auto read_a = [&](int s, uint4 &x, uint32_t &xs) {
         const int64_t blk = (int64_t)s * 4 + q;
-        uint4 x = make_uint4(0, 0, 0, 0);
-        uint32_t xs = 0;
-        if (src >= 0) {
-            if constexpr (DENSE) {
-                const Src *p = (const Src *)a.X + src * a.ldx;
-                Src v[32];
-                uint32_t top = 0;
+        x = make_uint4(0, 0, 0, 0);
+        xs = 0;
+        if (src < 0) return;
+        if constexpr (DENSE) {
+            const Src *p = (const Src *)a.X + src * a.ldx;
+            Src v[32];
+            uint32_t top = 0;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    load8(p, blk * 32 + 8 * i, a.K, v + 8 * i);
-                    top = max(top, max8(v + 8 * i));
-                }
-                xs = mx_scale_byte(top);
-                const float f = mx_scale_float(xs);
-                x = make_uint4(mx_pack8(v, f), mx_pack8(v + 8, f), mx_pack8(v + 16, f), mx_pack8(v + 24, f));
-            } else {
-                x = *reinterpret_cast<const uint4 *>(a.a_codes + (src * a.pitch + blk) * 16);
-                xs = a.a_scales[src * a.pitch + blk];
+            for (int i = 0; i < 4; ++i) {
+                load8(p, blk * 32 + 8 * i, a.K, v + 8 * i);
+                top = max(top, max8(v + 8 * i));
             }
+            xs = mx_scale_byte(top);
+            const float f = mx_scale_float(xs);
+            x = make_uint4(mx_pack8(v, f), mx_pack8(v + 8, f), mx_pack8(v + 16, f), mx_pack8(v + 24, f));
+        } else {
+            x = *reinterpret_cast<const uint4 *>(a.a_codes + (src * a.pitch + blk) * 16);
+            xs = a.a_scales[src * a.pitch + blk];
         }
+    };
+    const int run = (k1 - k0 + WAVES - 1) / WAVES, last = min(k1, k0 + (w + 1) * run);
+    int s = k0 + w * run;
+    for (; s + UNROLL <= last; s += UNROLL) {
+        uint4 x[UNROLL], b[UNROLL][CT];
+        uint32_t xs[UNROLL], bx[UNROLL][CT];
 #pragma unroll
-        for (int i = 0; i < CT; ++i) {
-            const int64_t at = (brow + min(n0 + 16 * i + row, a.F - 1)) * a.pitch + blk;
-            acc[i] = mx_mma(*reinterpret_cast<const uint4 *>(a.b_codes + at * 16), a.b_scales[at], x, xs, acc[i]);
-        }
+        for (int u = 0; u < UNROLL; ++u)
+#pragma unroll
+            for (int i = 0; i < CT; ++i) read_b(s + u, i, b[u][i], bx[u][i]);
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) read_a(s + u, x[u], xs[u]);
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u)
+#pragma unroll
+            for (int i = 0; i < CT; ++i) acc[i] = mx_mma(b[u][i], bx[u][i], x[u], xs[u], acc[i]);
+    }
+    for (; s < last; ++s) {
+        uint4 x, b[CT];
+        uint32_t xs, bx[CT];
+#pragma unroll
+        for (int i = 0; i < CT; ++i) read_b(s, i, b[i], bx[i]);
+        read_a(s, x, xs);
+#pragma unroll
+        for (int i = 0; i < CT; ++i) acc[i] = mx_mma(b[i], bx[i], x, xs, acc[i]);
     }
 #pragma unroll
     for (int i = 0; i < CT; ++i) part[w][i][lane] = acc[i];
     __syncthreads();
     if (m >= end) return;
     Out *o = (Out *)a.out + (OUTER ? ((int64_t)e * a.M + m) * a.ldo : m * a.ldo);
-    for (int i = w; i < CT; i += 4)
-        store4(o, n0 + 16 * i + 4 * q, a.F, part[0][i][lane] + part[1][i][lane] + part[2][i][lane] + part[3][i][lane]);
+    for (int i = w; i < CT; i += WAVES) {
+        float4v sum = part[0][i][lane];
+#pragma unroll
+        for (int v = 1; v < WAVES; ++v) sum += part[v][i][lane];
+        store4(o, n0 + 16 * i + 4 * q, a.F, sum);
+    }
 }
 
-template <typename Src, typename Out, bool OUTER>
+template <typename Src, typename Out, int CT, int WAVES, bool OUTER>
 static ftk_status launch_direct(MxProduct a, hipStream_t st)
 {
-    constexpr int CT = 4;
     a.ntiles = (int)ceil_div(a.F, 16 * CT);
     int64_t mtiles;
     if (OUTER) {
@@ -218,7 +265,7 @@ static ftk_status launch_direct(MxProduct a, hipStream_t st)
         set_error("too many tiles: M=%lld F=%d E=%d", (long long)a.M, a.F, a.E);
         return FTK_EINVAL;
     }
-    mx_direct_kernel<Src, Out, CT, OUTER><<<(unsigned)(mtiles * a.ntiles), 256, 0, st>>>(a);
+    mx_direct_kernel<Src, Out, CT, WAVES, OUTER><<<(unsigned)(mtiles * a.ntiles), 64 * WAVES, 0, st>>>(a);
     FTK_TRY_HIP(hipGetLastError());
     return FTK_OK;
 }
@@ -244,6 +291,14 @@ __device__ __forceinline__ void to_lds16_at(const uint8_t *g, uint32_t at)
 __device__ __forceinline__ void to_lds16_from(const uint8_t *base, uint32_t offset, uint32_t at)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(base) : "memory");
+}
+
+// A pointer that is the same in all lanes, where the compiler cannot see it.
+__device__ __forceinline__ const uint8_t *uniform(const uint8_t *p)
+{
+    const uint64_t b = (uint64_t)p;
+    return (const uint8_t *)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)b) |
+                             (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) << 32);
 }
 
 template <int MT, int NT>
@@ -307,6 +362,7 @@ __global__ __launch_bounds__(256, MT* NT >= 64 ? 1 : 2) void mx_tile_kernel(MxPr
             bbase += (int64_t)e * a.F * pitch;
             bscales += (int64_t)e * a.F * a.pitch;
         }
+        bbase = uniform(bbase);
         const int blast = a.F - 1 - n0;
         uint32_t arow[MT], boff[NT];  // row of A; offset from the column tile's first line
 #pragma unroll
@@ -457,7 +513,7 @@ __global__ __launch_bounds__(256, MT* NT >= 64 ? 1 : 2) void mx_tile_kernel(MxPr
                     mx_mma_in_place<0>(acc[i][j], frb[0][j], xb[0][j], fra[i], xa[i]);
         }
     }
-    mx_sums_done();
+    mx_sums_done(acc);
     typedef Out Eight __attribute__((ext_vector_type(8), aligned(sizeof(Out))));
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
@@ -496,20 +552,31 @@ static ftk_status launch_tile(MxProduct a, hipStream_t st)
         set_error("too many tiles: M=%lld F=%d E=%d", (long long)a.M, a.F, a.E);
         return FTK_EINVAL;
     }
-    FTK_TRY_HIP(hipFuncSetAttribute((const void *)mx_tile_kernel<MT, NT, Out, OUTER>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                    S::LDS));
+    FTK_TRY(allow_lds((const void *)mx_tile_kernel<MT, NT, Out, OUTER>, S::LDS));
     mx_tile_kernel<MT, NT, Out, OUTER><<<(unsigned)(mtiles * a.ntiles), 256, S::LDS, st>>>(a);
     FTK_TRY_HIP(hipGetLastError());
     return FTK_OK;
 }
 
-// Which kernel for packed rows.
+// Tiles that a problem is cut into, at most (rows of experts that are no multiple of a tile leave a broken one each).
+static int64_t count_tiles(const MxProduct &a, bool outer, int64_t tm, int64_t tn)
+{
+    const int64_t rows = outer ? ceil_div(a.M, tm) * a.E : a.M / tm + (a.M < a.E ? a.M : a.E);
+    return rows * ceil_div(a.F, tn);
+}
+
 template <typename Out, bool OUTER>
 static ftk_status launch_packed(const MxProduct &a, hipStream_t st)
 {
-    if (a.N > 0 && a.M >= 256 && a.pitch < (1 << 20)) return launch_tile<8, 8, Out, OUTER>(a, st);
-    return launch_direct<uint8_t, Out, OUTER>(a, st);
+    // offsets within a column tile are 32 bits wide
+    if (a.N == 0 || a.pitch >= 1 << 20) return launch_direct<uint8_t, Out, 4, 4, OUTER>(a, st);
+    if (count_tiles(a, OUTER, 256, 256) >= 1536) return launch_tile<8, 8, Out, OUTER>(a, st);
+    if (count_tiles(a, OUTER, 64, 64) > 1536) return launch_tile<4, 4, Out, OUTER>(a, st);
+    return launch_tile<2, 2, Out, OUTER>(a, st);
 }
+
+// Whether dense rows are packed by every workgroup that needs them rather than once beforehand.
+static bool few_rows(int64_t M) { return M <= 16; }
 
 static size_t packed_bytes(int64_t N, int D, size_t *codes)
 {
@@ -555,16 +622,18 @@ using namespace ftk;
 
 extern "C" {
 
-size_t ftk_mx4_workspace_bytes(int64_t N, int32_t D, int64_t M, int32_t F)
+int64_t ftk_mx4_workspace_bytes(int64_t N, int32_t D, int64_t M)
 {
-    if (N < 0 || M < 0 || D < 0 || F < 0 || N > 0x7fffffffLL || D > MX_MAX) return 0;
-    return packed_bytes(N, D, nullptr);
+    if (N < 0 || M < 0 || D < 1 || N > 0x7fffffffLL || M > 0x7fffffffLL || D > MX_MAX) {
+        set_error("need 0 <= N, M < 2^31, 1 <= D <= %d (got N=%lld M=%lld D=%d)", MX_MAX, (long long)N, (long long)M, D);
+        return -1;
+    }
+    return N == 0 || few_rows(M) ? 0 : (int64_t)packed_bytes(N, D, nullptr);
 }
 
 ftk_status ftk_mx4_matmul(ftk_dtype out_dtype, const void *a_codes, const void *a_scales, int64_t N, const void *b_codes,
                           const void *b_scales, int64_t M, int32_t F, int32_t D, int32_t E, const int32_t *offsets,
-                          const int32_t *order, int32_t k, void *out, int64_t ldo, void *workspace, size_t workspace_bytes,
-                          void *hip_stream)
+                          const int32_t *order, int32_t k, void *out, int64_t ldo, void *hip_stream)
 {
     FTK_TRY(check_product(out_dtype, N, b_codes, b_scales, M, F, D, E, offsets, order, k, out, ldo));
     if (M == 0) return FTK_OK;
@@ -572,8 +641,6 @@ ftk_status ftk_mx4_matmul(ftk_dtype out_dtype, const void *a_codes, const void *
         FTK_TRY(check_ptr(a_codes, 16, "a_codes"));
         FTK_TRY(check_ptr(a_scales, 4, "a_scales"));
     }
-    (void)workspace;
-    (void)workspace_bytes;
     FTK_TRY(check_device());
     const MxProduct a{(const uint8_t *)a_codes, (const uint8_t *)a_scales, nullptr, 0, N, D, mx_padded(D) / MX_BLOCK,
                       (const uint8_t *)b_codes, (const uint8_t *)b_scales, M, F, E, offsets, order, k, out, ldo, 0, 0};
@@ -593,13 +660,12 @@ ftk_status ftk_mx4_linear(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N
         return FTK_EINVAL;
     }
     if (N > 0) FTK_TRY(check_ptr(X, dtype_size(dtype), "X"));
-    const size_t need = packed_bytes(N, D, nullptr);
-    if (need) FTK_TRY(check_workspace(workspace, workspace_bytes, need));
+    const bool few = N == 0 || few_rows(M);
+    if (!few) FTK_TRY(check_workspace(workspace, workspace_bytes, packed_bytes(N, D, nullptr)));
     FTK_TRY(check_device());
     hipStream_t st = (hipStream_t)hip_stream;
     MxProduct a{nullptr, nullptr, X, ldx, N, D, mx_padded(D) / MX_BLOCK, (const uint8_t *)b_codes,
                 (const uint8_t *)b_scales, M, F, E, offsets, order, k, out, ldo, 0, 0};
-    const bool few = N == 0 || M < 256;
     if (!few) {
         size_t codes = 0;
         packed_bytes(N, D, &codes);
@@ -610,7 +676,7 @@ ftk_status ftk_mx4_linear(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N
     }
     return with_mx_type(dtype, [&](auto tag) {
         using T = typename decltype(tag)::type;
-        return few ? launch_direct<T, T, false>(a, st) : launch_packed<T, false>(a, st);
+        return few ? launch_direct<T, T, 1, 8, false>(a, st) : launch_packed<T, false>(a, st);
     });
 }
 

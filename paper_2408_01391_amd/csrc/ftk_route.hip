@@ -10,7 +10,7 @@ namespace ftk {
 
 constexpr int ROUTE_THREADS = 256, ROUTE_WAVES = ROUTE_THREADS / 64;
 constexpr int ROUTE_MAX_EXPERTS = 8192;  // one counter per wave and expert: 128 KB of a compute unit's 160
-constexpr int ROUTE_CHUNK = 1024;        // slots of a workgroup, at least
+constexpr int ROUTE_CHUNK = FTK_ROUTE_FEW;  // slots of a workgroup, at least
 constexpr int ROUTE_MAX_CHUNKS = 256;
 
 struct RoutePlan {
@@ -237,7 +237,28 @@ __device__ __forceinline__ void fill_rows(const int32_t *order, const RowShape &
     }
 }
 
-// Token's row to its k sorted places; the last `fill` workgroups clear the rows without a slot.
+// A piece of a token's row to its k sorted places.
+template <typename T, typename W>
+__device__ __forceinline__ void copy_piece(const T *x, const int32_t *p, const W *w, int i, const RowShape &h, T *out, int64_t ldo)
+{
+    using Acc = typename RowType<T>::Acc;
+    if (h.D < PIECE<T>) {
+        const T v = x[i];
+        for (int j = 0; j < h.k; ++j) {
+            const int32_t r = p[j];
+            if ((uint32_t)r < (uint64_t)h.rows) out[r * ldo + i] = w ? (T)((Acc)v * (Acc)w[j]) : v;
+        }
+    } else {
+        const int c = min(i * PIECE<T>, h.D - PIECE<T>);
+        const PieceOf<T> v = row_piece(x + c);
+        for (int j = 0; j < h.k; ++j) {
+            const int32_t r = p[j];
+            if ((uint32_t)r < (uint64_t)h.rows) put_piece(out + r * ldo + c, w ? scale_piece<T>(v, w[j]) : v);
+        }
+    }
+}
+
+// Tokens' rows to their places; the last `fill` workgroups clear the rows without a slot.
 template <typename T, typename W, int L>
 __global__ __launch_bounds__(256) void route_gather_kernel(const T *__restrict__ X, int64_t ldx, RowShape h,
                                                            const int32_t *__restrict__ order,
@@ -252,29 +273,33 @@ __global__ __launch_bounds__(256) void route_gather_kernel(const T *__restrict__
     }
     const int lane = threadIdx.x % L;
     const int64_t groups = (int64_t)movers * (256 / L);
-    for (int64_t t = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L; t < h.N; t += groups) {
-        const T *x = X + t * ldx;
-        const int32_t *p = pos + t * h.k;
+    for (int64_t t = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L; t < h.N; t += groups)
+        for (int i = lane; i < h.np; i += L)
+            copy_piece(X + t * ldx, pos + t * h.k, weights ? weights + t * h.k : nullptr, i, h, out, ldo);
+}
+
+// Few slots and no fill between experts: every workgroup works all places out by itself, which takes it less time than
+// a second launch does, and copies its share of the rows.
+template <typename T, int L>
+__global__ __launch_bounds__(ROUTE_THREADS) void route_few_kernel(PlaceArgs a, const T *__restrict__ X, int64_t ldx, RowShape h,
+                                                                  T *__restrict__ out, int64_t ldo)
+{
+    extern __shared__ int cnt[];
+    __shared__ int sums[ROUTE_WAVES], places[FTK_ROUTE_FEW];
+    place_slots(a, 0, 1, blockIdx.x == 0, cnt, sums, places);
+    __syncthreads();
+    const int lane = threadIdx.x % L, groups = gridDim.x * (256 / L), group = blockIdx.x * (256 / L) + threadIdx.x / L;
+    for (int t = group; t < (int)h.N; t += groups)
+        for (int i = lane; i < h.np; i += L)
+            copy_piece(X + t * ldx, places + t * h.k, (const float *)nullptr, i, h, out, ldo);
+    for (int64_t r = sums[0] + group; r < h.rows; r += groups)
         for (int i = lane; i < h.np; i += L) {
-            if (h.D < PIECE<T>) {
-                const T v = x[i];
-                for (int j = 0; j < h.k; ++j) {
-                    const int32_t r = p[j];
-                    if ((uint32_t)r >= (uint64_t)h.rows) continue;
-                    using Acc = typename RowType<T>::Acc;
-                    out[r * ldo + i] = weights ? (T)((Acc)v * (Acc)weights[t * h.k + j]) : v;
-                }
-            } else {
-                const int c = min(i * PIECE<T>, h.D - PIECE<T>);
-                const PieceOf<T> v = row_piece(x + c);
-                for (int j = 0; j < h.k; ++j) {
-                    const int32_t r = p[j];
-                    if ((uint32_t)r >= (uint64_t)h.rows) continue;
-                    put_piece(out + r * ldo + c, weights ? scale_piece<T>(v, weights[t * h.k + j]) : v);
-                }
-            }
+            T *o = out + r * ldo;
+            if (h.D < PIECE<T>)
+                o[i] = (T)0.f;
+            else
+                put_piece(o + min(i * PIECE<T>, h.D - PIECE<T>), PieceOf<T>{});
         }
-    }
 }
 
 // A token's sorted rows, times their weights, added up.  J slots at a time, whose loads are all under way before the
@@ -496,21 +521,22 @@ static ftk_status check_plan(const int32_t *labels, int64_t N, int32_t k, int32_
     return check_device();
 }
 
-static ftk_status launch_plan(const int32_t *labels, int64_t N, int k, int E, int align, int64_t rows, int32_t *offsets,
-                              int32_t *counts, int32_t *order, int32_t *pos, void *ws, hipStream_t st)
+static PlaceArgs place_args(const RoutePlan &p, const int32_t *labels, int E, int align, int64_t rows, int32_t *offsets,
+                            int32_t *counts, int32_t *order, int32_t *pos)
 {
-    const RoutePlan p = plan_route(N * k);
     int ebits = 0;
     while ((1 << ebits) < E) ++ebits;
-    PlaceArgs a{labels, p.S, p.chunk, E, align, ebits, rows, nullptr, nullptr, offsets, counts, order, pos};
-    const size_t lds = (size_t)ROUTE_WAVES * E * 4;
-    if (lds > 65536) {
-        FTK_TRY_HIP(hipFuncSetAttribute((const void *)route_place_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    }
+    return PlaceArgs{labels, p.S, p.chunk, E, align, ebits, rows, nullptr, nullptr, offsets, counts, order, pos};
+}
+
+static ftk_status launch_plan(const RoutePlan &p, PlaceArgs a, void *ws, hipStream_t st)
+{
+    const size_t lds = (size_t)ROUTE_WAVES * a.E * 4;
+    FTK_TRY(allow_lds((const void *)route_place_kernel, lds));
     if (p.chunks > 1) {
-        int32_t *totals = (int32_t *)ws, *table = totals + E;
-        route_count_kernel<<<p.chunks, ROUTE_THREADS, (size_t)E * 4, st>>>(labels, p.S, p.chunk, E, table);
-        route_prefix_kernel<<<(E + 63) / 64, ROUTE_THREADS, 0, st>>>(table, p.chunks, E, totals);
+        int32_t *totals = (int32_t *)ws, *table = totals + a.E;
+        route_count_kernel<<<p.chunks, ROUTE_THREADS, (size_t)a.E * 4, st>>>(a.labels, p.S, p.chunk, a.E, table);
+        route_prefix_kernel<<<(a.E + 63) / 64, ROUTE_THREADS, 0, st>>>(table, p.chunks, a.E, totals);
         a.table = table;
         a.totals = totals;
     }
@@ -564,7 +590,8 @@ ftk_status ftk_route_plan(const int32_t *labels, int64_t N, int32_t k, int32_t E
                           size_t workspace_bytes, void *hip_stream)
 {
     FTK_TRY(check_plan(labels, N, k, E, align, rows, offsets, counts, order, pos, workspace, workspace_bytes));
-    return launch_plan(labels, N, k, E, align, rows, offsets, counts, order, pos, workspace, (hipStream_t)hip_stream);
+    const RoutePlan p = plan_route(N * k);
+    return launch_plan(p, place_args(p, labels, E, align, rows, offsets, counts, order, pos), workspace, (hipStream_t)hip_stream);
 }
 
 ftk_status ftk_route_gather(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N, int32_t k, int32_t D,
@@ -596,7 +623,21 @@ ftk_status ftk_route_dispatch(ftk_dtype dtype, const void *X, int64_t ldx, int32
     if (N > 0) FTK_TRY(check_matrix(X, esz, ldx, D, "X"));
     FTK_TRY(check_plan(labels, N, k, E, align, rows, offsets, counts, order, pos, workspace, workspace_bytes));
     hipStream_t st = (hipStream_t)hip_stream;
-    FTK_TRY(launch_plan(labels, N, k, E, align, rows, offsets, counts, order, pos, workspace, st));
+    const RoutePlan p = plan_route(N * k);
+    const PlaceArgs a = place_args(p, labels, E, align, rows, offsets, counts, order, pos);
+    const size_t lds = (size_t)ROUTE_WAVES * E * 4;
+    if (rows > 0 && N * k <= FTK_ROUTE_FEW && align == 1 && lds <= 32768)
+        return with_type(dtype, [&](auto tag) {
+            using T = typename decltype(tag)::type;
+            const RowShape h{N, rows, k, D, row_pieces<T>(D)};
+            return with_lanes(h.np, [&](auto lanes) {
+                constexpr int L = decltype(lanes)::value;
+                route_few_kernel<T, L><<<row_grid(N, L), ROUTE_THREADS, lds, st>>>(a, (const T *)X, ldx, h, (T *)out, ldo);
+                FTK_TRY_HIP(hipGetLastError());
+                return FTK_OK;
+            });
+        });
+    FTK_TRY(launch_plan(p, a, workspace, st));
     if (rows == 0) return FTK_OK;
     return launch_gather(dtype, X, ldx, RowShape{N, rows, k, D, 0}, order, pos, nullptr, out, ldo, st);
 }

@@ -27,8 +27,11 @@ def test_sizes():
             ftk.route_rows(*bad)
     with pytest.raises(ftk.FtkError):
         ftk.route_workspace_bytes(1, 1, 0)
-    assert ftk.load().ftk_mx4_workspace_bytes(100, 1000, 10, 10) >= 100 * 1024 * 17 // 32
-    assert ftk.load().ftk_mx4_workspace_bytes(-1, 10, 1, 1) == 0
+    assert ftk.mx4_workspace_bytes(100, 1000, 10000) >= 100 * 1024 * 17 // 32
+    assert ftk.mx4_workspace_bytes(0, 1000, 10000) == 0
+    for bad in ((-1, 10, 1), (1, 0, 1), (1, 10, -1), (1, 1 << 25, 1), (1 << 31, 10, 1)):
+        with pytest.raises(ftk.FtkError):
+            ftk.mx4_workspace_bytes(*bad)
 
 
 def test_plan():
@@ -66,12 +69,12 @@ def test_mx4():
     ok = [ftk.F16, P, P, 10, 64, P, 64, None]
     for at, value, code in ((0, ftk.F64, 1), (1, P + 4, 2), (2, None, 1), (3, -1, 1), (4, 0, 1), (5, None, 1), (6, 1, 1)):
         refused(code, "ftk_mx4_dequantize", *(ok[:at] + [value] + ok[at + 1:]))
-    ok = [ftk.F32, P, P, 10, P, P, 20, 64, 128, 4, P, P, 2, P, 64, None, 0, None]
+    ok = [ftk.F32, P, P, 10, P, P, 20, 64, 128, 4, P, P, 2, P, 64, None]
     for at, value, code in ((0, ftk.F64, 1), (1, P + 8, 2), (2, None, 1), (3, -1, 1), (4, None, 1), (5, P + 1, 2), (6, -1, 1), (7, 0, 1),
                             (8, 0, 1), (8, (1 << 24) + 1, 1), (9, 0, 1), (9, 8193, 1), (10, None, 1), (11, None, 1), (12, 0, 1), (13, P + 2, 2),
                             (14, 63, 1)):
         refused(code, "ftk_mx4_matmul", *(ok[:at] + [value] + ok[at + 1:]))
-    ok = [ftk.F32, P, 128, 10, P, P, 20, 64, 128, 4, P, P, 2, P, 64, P, 1 << 20, None]
+    ok = [ftk.F32, P, 128, 10, P, P, 20000, 64, 128, 4, P, P, 2, P, 64, P, 1 << 20, None]
     for at, value, code in ((0, ftk.F64, 1), (1, None, 1), (2, 127, 1), (3, -1, 1), (4, None, 1), (7, 0, 1), (9, 0, 1), (10, None, 1),
                             (12, 0, 1), (13, None, 1), (14, 0, 1), (15, None, 3), (16, 100, 3), (15, P + 16, 2)):
         refused(code, "ftk_mx4_linear", *(ok[:at] + [value] + ok[at + 1:]))
