@@ -10,19 +10,20 @@ namespace ftk {
 // Threads of both row kernels take eights of the padded rows in order, 256 at a time and MX_UNITS times a workgroup.  The
 // row of a workgroup's first one is found by one wide division, what lies between by a narrow one: a wide one for every
 // eight cost as much as the conversion (65536 x 2048 bf16 back: 98 us).
-constexpr int MX_UNITS = 4;
+// (Few eights, for which there is a compute unit each: one at a time.)
+constexpr int MX_UNITS = 4, MX_FEW_UNITS = 256 * 256 * 4;
 struct MxUnit {
     int64_t row;
     int piece;  // eight of the row
 };
-template <typename F>
+template <int UNITS, typename F>
 __device__ __forceinline__ void for_units(int64_t N, uint32_t pieces, F &&f)
 {
-    const int64_t u0 = (int64_t)blockIdx.x * (256 * MX_UNITS), row0 = u0 / pieces;
+    const int64_t u0 = (int64_t)blockIdx.x * (256 * UNITS), row0 = u0 / pieces;
     const uint32_t first = (uint32_t)(u0 - row0 * pieces) + threadIdx.x;
     const int64_t left = N * pieces - u0;
 #pragma unroll
-    for (int k = 0; k < MX_UNITS; ++k) {
+    for (int k = 0; k < UNITS; ++k) {
         if (k * 256 + threadIdx.x >= left) break;
         const uint32_t at = first + k * 256, rows = at / pieces;
         f(MxUnit{row0 + rows, (int)(at - rows * pieces)}, u0 + k * 256 + threadIdx.x);
@@ -31,11 +32,11 @@ __device__ __forceinline__ void for_units(int64_t N, uint32_t pieces, F &&f)
 
 // Eight elements a thread, four threads a block: the largest magnitude passes between them by two lane
 // moves.  A thread's codes are one dword, so a wave writes 256 consecutive bytes.
-template <typename T>
+template <typename T, int UNITS>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(const T *__restrict__ X, int64_t ldx, int64_t N, int D, int pieces,
                                                           uint32_t *__restrict__ codes, uint8_t *__restrict__ scales)
 {
-    for_units(N, pieces, [&](MxUnit t, int64_t u) {  // (pieces: a multiple of 16)
+    for_units<UNITS>(N, pieces, [&](MxUnit t, int64_t u) {  // (pieces: a multiple of 16)
         T v[8];
         load8(X + t.row * ldx, (int64_t)t.piece * 8, D, v);
         uint32_t m = max8(v);
@@ -51,14 +52,15 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(const T *__restrict__ 
 // blocks, a workgroup 256 rows: 128 bytes of codes and eight scales of every column, brought together in LDS so that
 // they leave by whole lines (written by the lanes that made them, 16 bytes at a time: 33792 x 4096 bf16 171 us).  Workgroups that
 // share a line of scales run near each other on one XCD.
-constexpr int ACROSS_ROWS = 256, ACROSS_COLS = 128;
-template <typename T>
+// Few rows and columns: half as many rows a workgroup (HALVES = 1), for twice the workgroups (30007 x 333 fp32 15.9 us with 256).
+constexpr int ACROSS_COLS = 128;
+template <typename T, int HALVES>
 __global__ __launch_bounds__(256) void mx_quantize_across_kernel(const T *__restrict__ X, int64_t ldx, int64_t N, int D,
                                                                  int64_t nblocks, int rowgroups, uint32_t *__restrict__ codes,
                                                                  uint8_t *__restrict__ scales)
 {
-    // a column's 32 dwords of codes and two of scales, and one more against bank conflicts
-    constexpr int LINE = 35;
+    // a column's dwords of codes and of scales, an odd number against bank conflicts
+    constexpr int BLOCKS = 4 * HALVES, ROWS = 32 * BLOCKS, CODES = 4 * BLOCKS, LINE = CODES + HALVES + (HALVES == 2 ? 1 : 0);
     __shared__ uint32_t line[ACROSS_COLS * LINE];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     uint32_t id = blockIdx.x;
@@ -68,9 +70,9 @@ __global__ __launch_bounds__(256) void mx_quantize_across_kernel(const T *__rest
     typedef T Pair __attribute__((ext_vector_type(2), aligned(sizeof(T))));
     const bool both = d + 1 < D;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int b = w * 2 + h;
-        const int64_t r0 = (int64_t)rg * ACROSS_ROWS + b * 32;
+    for (int h = 0; h < HALVES; ++h) {
+        const int b = w * HALVES + h;
+        const int64_t r0 = (int64_t)rg * ROWS + b * 32;
         T v[2][32];
         if (r0 + 32 <= N && both) {
             const T *x = X + r0 * ldx + d;
@@ -97,27 +99,27 @@ __global__ __launch_bounds__(256) void mx_quantize_across_kernel(const T *__rest
             uint32_t *l = line + (lane * 2 + c) * LINE;
 #pragma unroll
             for (int i = 0; i < 4; ++i) l[b * 4 + i] = mx_pack8(&v[c][8 * i], f);
-            reinterpret_cast<uint8_t *>(l + 32)[b] = (uint8_t)s;
+            reinterpret_cast<uint8_t *>(l + CODES)[b] = (uint8_t)s;
         }
     }
     __syncthreads();
-    const int blocks = (int)(nblocks - (int64_t)rg * 8 < 8 ? nblocks - (int64_t)rg * 8 : 8);  // 4 or 8
-    for (int i = threadIdx.x; i < ACROSS_COLS * 8; i += 256) {
-        const int col = i >> 3, piece = i & 7;
+    const int blocks = (int)(nblocks - (int64_t)rg * BLOCKS < BLOCKS ? nblocks - (int64_t)rg * BLOCKS : BLOCKS);  // 4 or 8
+    for (int i = threadIdx.x; i < ACROSS_COLS * BLOCKS; i += 256) {
+        const int col = i / BLOCKS, piece = i % BLOCKS;
         if (c0 + col >= D || piece >= blocks) continue;
         const uint32_t *l = line + col * LINE;
-        const int64_t at = (int64_t)(c0 + col) * nblocks + (int64_t)rg * 8;
+        const int64_t at = (int64_t)(c0 + col) * nblocks + (int64_t)rg * BLOCKS;
         *reinterpret_cast<uint4 *>(codes + (at + piece) * 4) = make_uint4(l[piece * 4], l[piece * 4 + 1], l[piece * 4 + 2], l[piece * 4 + 3]);
-        if ((piece & 3) == 0) *reinterpret_cast<uint32_t *>(scales + at + piece) = l[32 + (piece >> 2)];
+        if ((piece & 3) == 0) *reinterpret_cast<uint32_t *>(scales + at + piece) = l[CODES + (piece >> 2)];
     }
 }
 
-template <typename T>
+template <typename T, int UNITS>
 __global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint32_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                                                             int64_t N, int D, int pieces, T *__restrict__ out, int64_t ldo)
 {
     typedef float pair __attribute__((ext_vector_type(2)));
-    for_units(N, pieces, [&](MxUnit t, int64_t u) {
+    for_units<UNITS>(N, pieces, [&](MxUnit t, int64_t u) {
         const int c = t.piece * 8;
         if (c >= D) return;
         const uint32_t q = codes[u], b = scales[u >> 2];
@@ -144,11 +146,18 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint32_t *__re
     });
 }
 
-// workgroups of a row kernel, 0 where there are too many
-static unsigned mx_grid(int64_t units)
+// calls f(units of a thread, workgroups) for a row kernel
+template <typename F>
+static ftk_status with_units(int64_t N, int D, F &&f)
 {
+    const int64_t units = N * (mx_padded(D) / 8);
+    if (units <= MX_FEW_UNITS) return f(std::integral_constant<int, 1>{}, (unsigned)ceil_div(units, 256));
     const int64_t g = ceil_div(units, 256 * MX_UNITS);
-    return g <= 0x7fffffffLL ? (unsigned)g : 0;
+    if (g > 0x7fffffffLL) {
+        set_error("too many elements (N=%lld D=%d)", (long long)N, D);
+        return FTK_EINVAL;
+    }
+    return f(std::integral_constant<int, MX_UNITS>{}, (unsigned)g);
 }
 
 ftk_status launch_mx_quantize(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N, int D, void *codes, void *scales,
@@ -156,15 +165,12 @@ ftk_status launch_mx_quantize(ftk_dtype dtype, const void *X, int64_t ldx, int64
 {
     return with_mx_type(dtype, [&](auto tag) {
         using T = typename decltype(tag)::type;
-        const int pieces = (int)(mx_padded(D) / 8);
-        if (!mx_grid(N * pieces)) {
-            set_error("too many elements (N=%lld D=%d)", (long long)N, D);
-            return FTK_EINVAL;
-        }
-        mx_quantize_kernel<T><<<mx_grid(N * pieces), 256, 0, st>>>((const T *)X, ldx, N, D, pieces, (uint32_t *)codes,
-                                                                   (uint8_t *)scales);
-        FTK_TRY_HIP(hipGetLastError());
-        return FTK_OK;
+        return with_units(N, D, [&](auto units, unsigned grid) {
+            mx_quantize_kernel<T, decltype(units)::value><<<grid, 256, 0, st>>>(
+                (const T *)X, ldx, N, D, (int)(mx_padded(D) / 8), (uint32_t *)codes, (uint8_t *)scales);
+            FTK_TRY_HIP(hipGetLastError());
+            return FTK_OK;
+        });
     });
 }
 
@@ -200,15 +206,17 @@ ftk_status ftk_mx4_quantize(ftk_dtype dtype, const void *X, int64_t ldx, int64_t
     if (N == 0) return FTK_OK;
     hipStream_t st = (hipStream_t)hip_stream;
     if (!transpose) return launch_mx_quantize(dtype, X, ldx, N, D, codes, scales, st);
-    const int64_t nblocks = mx_padded(N) / MX_BLOCK, rowgroups = ceil_div(N, ACROSS_ROWS), wgs = rowgroups * ceil_div(D, ACROSS_COLS);
+    const int64_t nblocks = mx_padded(N) / MX_BLOCK, colgroups = ceil_div(D, ACROSS_COLS);
+    const bool few = ceil_div(N, 256) * colgroups < 1024;
+    const int64_t rowgroups = ceil_div(N, few ? 128 : 256), wgs = rowgroups * colgroups;
     if (wgs > 0x7fffffffLL) {
         set_error("transpose: too many elements (N=%lld D=%d)", (long long)N, D);
         return FTK_EINVAL;
     }
     return with_mx_type(dtype, [&](auto tag) {
         using T = typename decltype(tag)::type;
-        mx_quantize_across_kernel<T><<<(unsigned)wgs, 256, 0, st>>>((const T *)X, ldx, N, D, nblocks, (int)rowgroups,
-                                                                     (uint32_t *)codes, (uint8_t *)scales);
+        const auto kernel = few ? mx_quantize_across_kernel<T, 1> : mx_quantize_across_kernel<T, 2>;
+        kernel<<<(unsigned)wgs, 256, 0, st>>>((const T *)X, ldx, N, D, nblocks, (int)rowgroups, (uint32_t *)codes, (uint8_t *)scales);
         FTK_TRY_HIP(hipGetLastError());
         return FTK_OK;
     });
@@ -221,15 +229,12 @@ ftk_status ftk_mx4_dequantize(ftk_dtype dtype, const void *codes, const void *sc
     if (N == 0) return FTK_OK;
     return with_mx_type(dtype, [&](auto tag) {
         using T = typename decltype(tag)::type;
-        const int pieces = (int)(mx_padded(D) / 8);
-        if (!mx_grid(N * pieces)) {
-            set_error("too many elements (N=%lld D=%d)", (long long)N, D);
-            return FTK_EINVAL;
-        }
-        mx_dequantize_kernel<T><<<mx_grid(N * pieces), 256, 0, (hipStream_t)hip_stream>>>(
-            (const uint32_t *)codes, (const uint8_t *)scales, N, D, pieces, (T *)out, ldo);
-        FTK_TRY_HIP(hipGetLastError());
-        return FTK_OK;
+        return with_units(N, D, [&](auto units, unsigned grid) {
+            mx_dequantize_kernel<T, decltype(units)::value><<<grid, 256, 0, (hipStream_t)hip_stream>>>(
+                (const uint32_t *)codes, (const uint8_t *)scales, N, D, (int)(mx_padded(D) / 8), (T *)out, ldo);
+            FTK_TRY_HIP(hipGetLastError());
+            return FTK_OK;
+        });
     });
 }
 

@@ -79,15 +79,12 @@ __device__ __forceinline__ bool find_tile(const MxProduct &a, int64_t t, RowTile
     return r.m0 >= first && r.m0 < r.end;
 }
 
-__device__ __forceinline__ int64_t source_row(const MxProduct &a, int64_t m)
+__device__ __forceinline__ int64_t source_of(const MxProduct &a, int64_t m, int32_t slot)
 {
-    int64_t s = m;
-    if (a.order) {
-        const int32_t o = a.order[m];
-        s = o < 0 ? -1 : o / a.k;
-    }
+    const int64_t s = !a.order ? m : slot < 0 ? -1 : slot / a.k;
     return s < a.N ? s : -1;
 }
+__device__ __forceinline__ int64_t source_row(const MxProduct &a, int64_t m) { return source_of(a, m, a.order ? a.order[m] : 0); }
 
 template <typename Out>
 __device__ __forceinline__ void store4(Out *o, int n, int F, float4v v)
@@ -153,7 +150,7 @@ __global__ __launch_bounds__(64 * WAVES) void mx_direct_kernel(MxProduct a)
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, row = lane & 15, q = lane >> 4;
     const int64_t t = blockIdx.x / a.ntiles;
     const int n0 = (int)(blockIdx.x - t * a.ntiles) * 16 * CT;
-    int64_t m, end;
+    int64_t m, end, src;
     int e;
     int k0 = 0, k1 = (int)(((int64_t)a.K + 127) / 128);
     if constexpr (OUTER) {
@@ -161,19 +158,23 @@ __global__ __launch_bounds__(64 * WAVES) void mx_direct_kernel(MxProduct a)
         e = (int)(t / mt);
         m = (t - (int64_t)e * mt) * 16 + row;
         end = a.M;
+        src = m < end ? m : -1;
         if (a.offsets) {
             k0 = min(k1, max(0, a.offsets[e]) / 128);
             k1 = min(k1, max(0, a.offsets[e + 1]) / 128);
         }
     } else {
+        // (numbered by rows, the tile's first row is known, and the rows of A need not wait for the expert)
+        const bool early = a.by_row && a.order;
+        const int32_t slot = early && t + row < a.M ? a.order[t + row] : -1;
         RowTile r;
         if (!find_tile<16>(a, t, r)) return;
         e = r.e;
         m = r.m0 + row;
         end = r.end;
         if (e >= a.E) k1 = 0;
+        src = m >= end ? -1 : early ? source_of(a, m, slot) : source_row(a, m);
     }
-    const int64_t src = m >= end ? -1 : OUTER ? m : source_row(a, m);
     float4v acc[CT];
 #pragma unroll
     for (int i = 0; i < CT; ++i) acc[i] = float4v{0, 0, 0, 0};
@@ -558,11 +559,16 @@ static ftk_status launch_tile(MxProduct a, hipStream_t st)
     return FTK_OK;
 }
 
-// Tiles that a problem is cut into, at most (rows of experts that are no multiple of a tile leave a broken one each).
-static int64_t count_tiles(const MxProduct &a, bool outer, int64_t tm, int64_t tn)
+// What the tiles of a kernel take, in about a microsecond: so many of them run at once, one starts and ends in `ends` and
+// takes `stage` for 256 elements.  (Measured: 16384 x 2 rows, 16 matrices of 4096 x 4096 in tiles of 256 / 128 rows and columns 355 / 445 us;
+// 4096 x 2 rows, 8 matrices 121 / 121, of 64 166; 1024 x 2 rows 48 / 49 / 54; 256 x 2 rows 42 / 28 / 25; of 512 x 512, 64 matrices,
+// 16384 x 2 rows 35 / 30 / 33.)
+static double tile_cost(const MxProduct &a, bool outer, int side, int at_once, double ends, double stage)
 {
-    const int64_t rows = outer ? ceil_div(a.M, tm) * a.E : a.M / tm + (a.M < a.E ? a.M : a.E);
-    return rows * ceil_div(a.F, tn);
+    // half of the experts with rows leave a broken tile more
+    const int64_t rows = outer ? ceil_div(a.M, side) * a.E : a.M / side + (a.M < a.E ? a.M : (a.E + 1) / 2);
+    const double stages = (double)a.K / (outer ? a.E : 1) / 256;
+    return (double)ceil_div(rows * ceil_div(a.F, side), at_once) * (ends + stages * stage);
 }
 
 template <typename Out, bool OUTER>
@@ -570,9 +576,10 @@ static ftk_status launch_packed(const MxProduct &a, hipStream_t st)
 {
     // offsets within a column tile are 32 bits wide
     if (a.N == 0 || a.pitch >= 1 << 20) return launch_direct<uint8_t, Out, 4, 4, OUTER>(a, st);
-    if (count_tiles(a, OUTER, 256, 256) >= 1536) return launch_tile<8, 8, Out, OUTER>(a, st);
-    if (count_tiles(a, OUTER, 64, 64) > 1536) return launch_tile<4, 4, Out, OUTER>(a, st);
-    return launch_tile<2, 2, Out, OUTER>(a, st);
+    const double large = tile_cost(a, OUTER, 256, 256, 11, 1.75), middle = tile_cost(a, OUTER, 128, 512, 6, 1.27),
+                 small = tile_cost(a, OUTER, 64, 1024, 5, 0.75);
+    if (large <= middle && large <= small) return launch_tile<8, 8, Out, OUTER>(a, st);
+    return middle <= small ? launch_tile<4, 4, Out, OUTER>(a, st) : launch_tile<2, 2, Out, OUTER>(a, st);
 }
 
 // Whether dense rows are packed by every workgroup that needs them rather than once beforehand.
@@ -676,7 +683,7 @@ ftk_status ftk_mx4_linear(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N
     }
     return with_mx_type(dtype, [&](auto tag) {
         using T = typename decltype(tag)::type;
-        return few ? launch_direct<T, T, 1, 8, false>(a, st) : launch_packed<T, false>(a, st);
+        return few ? launch_direct<T, T, 2, 8, false>(a, st) : launch_packed<T, false>(a, st);
     });
 }
 

@@ -48,27 +48,30 @@ __global__ __launch_bounds__(ROUTE_THREADS) void route_count_kernel(const int32_
 }
 
 // table[b][e] becomes the slots of e before workgroup b; totals[e] all of them.  A workgroup has 64 experts, a wave a
-// quarter of the rows.
-__global__ __launch_bounds__(ROUTE_THREADS) void route_prefix_kernel(int32_t *__restrict__ table, int chunks, int E,
-                                                                     int32_t *__restrict__ totals)
+// sixteenth of the rows, all requested at once.
+constexpr int PREFIX_WAVES = 16, PREFIX_ROWS = ROUTE_MAX_CHUNKS / PREFIX_WAVES;
+__global__ __launch_bounds__(64 * PREFIX_WAVES) void route_prefix_kernel(int32_t *__restrict__ table, int chunks, int E,
+                                                                         int32_t *__restrict__ totals)
 {
-    __shared__ int part[ROUTE_WAVES][64];
-    const int e = blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
-    const int each = (chunks + ROUTE_WAVES - 1) / ROUTE_WAVES, b0 = w * each, b1 = min(chunks, b0 + each);
-    int sum = 0;
-    if (e < E)
-        for (int b = b0; b < b1; ++b) sum += table[(int64_t)b * E + e];
-    part[w][threadIdx.x & 63] = sum;
+    __shared__ int part[PREFIX_WAVES][64];
+    const int lane = threadIdx.x & 63, e = blockIdx.x * 64 + lane, w = threadIdx.x >> 6;
+    const int each = (chunks + PREFIX_WAVES - 1) / PREFIX_WAVES, b0 = w * each;  // each <= PREFIX_ROWS
+    int v[PREFIX_ROWS], sum = 0;
+#pragma unroll
+    for (int i = 0; i < PREFIX_ROWS; ++i) v[i] = i < each && b0 + i < chunks && e < E ? table[(int64_t)(b0 + i) * E + e] : 0;
+#pragma unroll
+    for (int i = 0; i < PREFIX_ROWS; ++i) sum += v[i];
+    part[w][lane] = sum;
     __syncthreads();
     if (e >= E) return;
     int run = 0;
-    for (int i = 0; i < w; ++i) run += part[i][threadIdx.x & 63];
-    for (int b = b0; b < b1; ++b) {
-        const int t = table[(int64_t)b * E + e];
-        table[(int64_t)b * E + e] = run;
-        run += t;
+    for (int i = 0; i < w; ++i) run += part[i][lane];
+#pragma unroll
+    for (int i = 0; i < PREFIX_ROWS; ++i) {
+        if (i < each && b0 + i < chunks) table[(int64_t)(b0 + i) * E + e] = run;
+        run += v[i];
     }
-    if (w == ROUTE_WAVES - 1) totals[e] = run;
+    if (w == PREFIX_WAVES - 1) totals[e] = run;
 }
 
 __device__ __forceinline__ int round_up(int v, int a) { return (v + a - 1) / a * a; }
@@ -416,7 +419,9 @@ __global__ __launch_bounds__(256) void route_combine_grad_kernel(const T *__rest
     }
 }
 
-// Lanes of a row: as many as it has pieces, a power of two of 4 to 64.
+// Lanes of a row: as many as it has pieces, a power of two of 4 to 64.  (Fewer, where that leaves fewer of them idle in the last
+// round, gain nothing: 333 floats, 84 pieces, weighted sum and its gradients 43 + 69 us with 64 lanes, 45 + 68
+// with 32, 51 + 76 with 16, 83 + 118 with 4.)
 static int row_lanes(int np)
 {
     int l = 4;
@@ -432,6 +437,17 @@ static ftk_status with_lanes(int np, F &&f)
     case 16: return f(std::integral_constant<int, 16>{});
     case 32: return f(std::integral_constant<int, 32>{});
     default: return f(std::integral_constant<int, 64>{});
+    }
+}
+// slots of a token that are worked on together: all of them up to three, else four at a time
+template <typename F>
+static ftk_status with_slots(int k, F &&f)
+{
+    switch (k) {
+    case 1: return f(std::integral_constant<int, 1>{});
+    case 2: return f(std::integral_constant<int, 2>{});
+    case 3: return f(std::integral_constant<int, 3>{});
+    default: return f(std::integral_constant<int, 4>{});
     }
 }
 static int row_grid(int64_t N, int lanes)
@@ -536,7 +552,7 @@ static ftk_status launch_plan(const RoutePlan &p, PlaceArgs a, void *ws, hipStre
     if (p.chunks > 1) {
         int32_t *totals = (int32_t *)ws, *table = totals + a.E;
         route_count_kernel<<<p.chunks, ROUTE_THREADS, (size_t)a.E * 4, st>>>(a.labels, p.S, p.chunk, a.E, table);
-        route_prefix_kernel<<<(a.E + 63) / 64, ROUTE_THREADS, 0, st>>>(table, p.chunks, a.E, totals);
+        route_prefix_kernel<<<(a.E + 63) / 64, 64 * PREFIX_WAVES, 0, st>>>(table, p.chunks, a.E, totals);
         a.table = table;
         a.totals = totals;
     }
@@ -664,16 +680,13 @@ ftk_status ftk_route_combine(ftk_dtype dtype, const void *Y, int64_t ldy, int64_
         const RowShape h{N, rows, k, D, row_pieces<T>(D)};
         return with_lanes(h.np, [&](auto lanes) {
             constexpr int L = decltype(lanes)::value;
-            auto launch = [&](auto slots) {
+            return with_slots(k, [&](auto slots) {
                 constexpr int J = decltype(slots)::value;
                 route_combine_kernel<T, WeightOf<T>, L, J><<<row_grid(N, L), 256, 0, st>>>(
                     (const T *)Y, ldy, h, pos, (const WeightOf<T> *)weights, (T *)out, ldo);
                 FTK_TRY_HIP(hipGetLastError());
                 return FTK_OK;
-            };
-            if (k == 1) return launch(std::integral_constant<int, 1>{});
-            if (k == 2) return launch(std::integral_constant<int, 2>{});
-            return launch(std::integral_constant<int, 4>{});
+            });
         });
     });
 }
@@ -706,7 +719,7 @@ ftk_status ftk_route_combine_grad(ftk_dtype dtype, const void *dOut, int64_t ldg
         const RowShape h{N, rows, k, D, row_pieces<T>(D)};
         return with_lanes(h.np, [&](auto lanes) {
             constexpr int L = decltype(lanes)::value;
-            auto launch = [&](auto slots) {
+            return with_slots(k, [&](auto slots) {
                 constexpr int J = decltype(slots)::value;
                 const int fill = fill_grid(rows);
                 route_combine_grad_kernel<T, WeightOf<T>, L, J><<<row_grid(N, L) + fill, 256, 0, st>>>(
@@ -714,9 +727,7 @@ ftk_status ftk_route_combine_grad(ftk_dtype dtype, const void *dOut, int64_t ldg
                     (WeightOf<T> *)dweights, fill);
                 FTK_TRY_HIP(hipGetLastError());
                 return FTK_OK;
-            };
-            if (k == 1) return launch(std::integral_constant<int, 1>{});
-            return launch(std::integral_constant<int, 2>{});
+            });
         });
     });
 }

@@ -185,6 +185,51 @@ def test_products(N, D, F, E, k, dtype, align, kind):
     assert (out[:, :3] == 9).all() and (out[:, -3:] == 9).all()
 
 
+@pytest.mark.parametrize("N,D,F,E,k,dtype,align,kind", [
+    (40001, 256, 2050, 5, 1, "bf16", 1, "skew"), (20000, 384, 2100, 3, 2, "f32", 1, "skew"), (30000, 640, 2048, 4, 1, "f16", 16, "even"),
+    (12000, 1024, 4096, 2, 1, "bf16", 128, "skew"), (20000, 100, 4000, 16, 2, "bf16", 1, "wild"), (9000, 1408, 4200, 3, 1, "bf16", 1, "one")])
+def test_products_in_large_tiles(N, D, F, E, k, dtype, align, kind):
+    """Enough rows and columns for tiles of 256 by 256: whole and broken ones, an odd and an even number of steps, rows of fewer and of
+    more than 16 scales, the last 16 scales moved back into the row."""
+    print("large product", N, D, F, E, k, dtype, align, kind, flush=True)
+    g = torch.Generator(device=DEV).manual_seed(N)
+    X = (torch.randn(N, D, generator=g, device=DEV) * torch.exp2(torch.randint(-3, 4, (N, 1), generator=g, device=DEV))).to(DTYPES[dtype])
+    W = ftk.mx4_quantize(torch.randn(E * F, D, generator=g, device=DEV))
+    r = ftk.route_plan(dev(labels_of(np.random.default_rng(N), N, k, E, kind)), E, align)
+    x, w = ftk.mx4_dequantize(ftk.mx4_quantize(X)).double(), ftk.mx4_dequantize(W).double().view(E, F, D)
+    A = ftk.route_gather(X, r)
+    got = [ftk.mx4_linear(X, W, r, gather=True), ftk.mx4_linear(A, W, r),
+           ftk.mx4_matmul(ftk.mx4_quantize(X), W, r, gather=True, out_dtype=DTYPES[dtype])]
+    off, steps = r.offsets.tolist(), -(-D // 128)
+    for e in range(E + 1):
+        p = slice(off[e], off[e + 1] if e < E else r.rows)
+        slot = r.order[p].long()
+        rows = torch.where((slot >= 0).unsqueeze(1), x[slot.clamp(min=0) // k], 0) if e < E else x.new_zeros(slot.numel(), D)
+        m = w[e].t().contiguous() if e < E else x.new_zeros(D, F)
+        want, size = rows @ m, rows.abs() @ m.abs()
+        bound = UNIT[dtype] * want.abs() + (steps + 8) * 2.0 ** -23 * size + STEP[dtype]
+        for out in got:
+            assert ((out[p].double() - want).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("N,F,D,E,dtype", [(2400, 2048, 2048, 8, "bf16"), (3000, 2100, 1990, 6, "f32"), (700, 4096, 4096, 2, "f16")])
+def test_sums_in_large_tiles(N, F, D, E, dtype):
+    print("large outer", N, F, D, E, dtype, flush=True)
+    g = torch.Generator(device=DEV).manual_seed(N)
+    r = ftk.route_plan(dev(labels_of(np.random.default_rng(N), N, 1, E, "skew")), E, 128)
+    A = ftk.route_gather(torch.randn(N, F, generator=g, device=DEV).to(DTYPES[dtype]), r)
+    B = ftk.route_gather(torch.randn(N, D, generator=g, device=DEV).to(DTYPES[dtype]), r)
+    qa, qb = ftk.mx4_quantize(A, transpose=True), ftk.mx4_quantize(B, transpose=True)
+    a, b = ftk.mx4_dequantize(qa).double(), ftk.mx4_dequantize(qb).double()
+    got, off = ftk.mx4_outer(qa, qb, r, out_dtype=DTYPES[dtype]), r.offsets.tolist()
+    for e in range(E):
+        p = slice(off[e], off[e + 1])
+        m = b[:, p].t().contiguous()
+        want, size = a[:, p] @ m, a[:, p].abs() @ m.abs()
+        bound = UNIT[dtype] * want.abs() + ((off[e + 1] - off[e]) // 128 + 8) * 2.0 ** -23 * size + STEP[dtype]
+        assert ((got[e].double() - want).abs() <= bound).all()
+
+
 @pytest.mark.parametrize("N,F,D,E,k,dtype,kind", [
     (1, 1, 1, 1, 1, "f32", "even"), (50, 20, 33, 3, 2, "f32", "skew"), (700, 130, 257, 5, 2, "bf16", "skew"),
     (3, 64, 64, 4, 1, "f16", "none"), (1000, 300, 129, 2, 1, "f32", "one"), (2000, 256, 512, 6, 2, "bf16", "even"),
