@@ -116,7 +116,8 @@ __global__ __launch_bounds__(256) void mx_quantize_across_kernel(const T *__rest
 
 template <typename T, int UNITS>
 __global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint32_t *__restrict__ codes, const uint8_t *__restrict__ scales,
-                                                            int64_t N, int D, int pieces, T *__restrict__ out, int64_t ldo)
+                                                            int64_t N, int D, int pieces, T *__restrict__ out, int64_t ldo,
+                                                            bool stream)
 {
     typedef float pair __attribute__((ext_vector_type(2)));
     for_units<UNITS>(N, pieces, [&](MxUnit t, int64_t u) {
@@ -136,7 +137,7 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint32_t *__re
                 PieceOf<T> w;
 #pragma unroll
                 for (int e = 0; e < PIECE<T>; ++e) w[e] = v[k * PIECE<T> + e];
-                put_piece(o + k * PIECE<T>, w);
+                put_piece(o + k * PIECE<T>, w, stream);
             }
         } else {
 #pragma unroll
@@ -231,7 +232,8 @@ ftk_status ftk_mx4_dequantize(ftk_dtype dtype, const void *codes, const void *sc
         using T = typename decltype(tag)::type;
         return with_units(N, D, [&](auto units, unsigned grid) {
             mx_dequantize_kernel<T, decltype(units)::value><<<grid, 256, 0, (hipStream_t)hip_stream>>>(
-                (const uint32_t *)codes, (const uint8_t *)scales, N, D, (int)(mx_padded(D) / 8), (T *)out, ldo);
+                (const uint32_t *)codes, (const uint8_t *)scales, N, D, (int)(mx_padded(D) / 8), (T *)out, ldo,
+                streams_out((double)N * D * sizeof(T)));
             FTK_TRY_HIP(hipGetLastError());
             return FTK_OK;
         });

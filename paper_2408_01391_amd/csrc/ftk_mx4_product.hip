@@ -30,6 +30,7 @@ struct MxProduct {
     void *out;
     int64_t ldo;
     int ntiles;      // column tiles
+    bool stream;     // the result is written past the caches
     int by_row;      // row tiles are numbered by their first row (few rows), else by tiles before them
 };
 
@@ -529,7 +530,7 @@ __global__ __launch_bounds__(256, MT* NT >= 64 ? 1 : 2) void mx_tile_kernel(MxPr
 #pragma unroll
             for (int c = 0; c < 8; ++c) v[c] = held ? (Out)acc[i][j + (c >> 2)][c & 3] : (Out)0.f;
             if (n + 8 <= a.F) {
-                *reinterpret_cast<Eight *>(o + n) = v;
+                STREAM_STORE(reinterpret_cast<Eight *>(o + n), v, a.stream);
             } else {
 #pragma unroll
                 for (int c = 0; c < 8; ++c)
@@ -544,6 +545,7 @@ static ftk_status launch_tile(MxProduct a, hipStream_t st)
 {
     using S = TileShape<MT, NT>;
     a.ntiles = (int)ceil_div(a.F, S::TN);
+    a.stream = streams_out((double)a.M * a.F * (OUTER ? a.E : 1) * sizeof(Out));
     int64_t mtiles = OUTER ? ceil_div(a.M, S::TM) * a.E : a.M / S::TM + a.E + 1;
     if (!OUTER) {
         a.by_row = a.M < mtiles;
@@ -650,7 +652,7 @@ ftk_status ftk_mx4_matmul(ftk_dtype out_dtype, const void *a_codes, const void *
     }
     FTK_TRY(check_device());
     const MxProduct a{(const uint8_t *)a_codes, (const uint8_t *)a_scales, nullptr, 0, N, D, mx_padded(D) / MX_BLOCK,
-                      (const uint8_t *)b_codes, (const uint8_t *)b_scales, M, F, E, offsets, order, k, out, ldo, 0, 0};
+                      (const uint8_t *)b_codes, (const uint8_t *)b_scales, M, F, E, offsets, order, k, out, ldo, 0, false, 0};
     return with_mx_type(out_dtype, [&](auto tag) {
         return launch_packed<typename decltype(tag)::type, false>(a, (hipStream_t)hip_stream);
     });
@@ -672,7 +674,7 @@ ftk_status ftk_mx4_linear(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N
     FTK_TRY(check_device());
     hipStream_t st = (hipStream_t)hip_stream;
     MxProduct a{nullptr, nullptr, X, ldx, N, D, mx_padded(D) / MX_BLOCK, (const uint8_t *)b_codes,
-                (const uint8_t *)b_scales, M, F, E, offsets, order, k, out, ldo, 0, 0};
+                (const uint8_t *)b_scales, M, F, E, offsets, order, k, out, ldo, 0, false, 0};
     if (!few) {
         size_t codes = 0;
         packed_bytes(N, D, &codes);
@@ -711,7 +713,7 @@ ftk_status ftk_mx4_outer(ftk_dtype out_dtype, const void *a_codes, const void *a
     }
     FTK_TRY(check_device());
     MxProduct a{(const uint8_t *)a_codes, (const uint8_t *)a_scales, nullptr, 0, F, (int)rows, mx_padded(rows) / MX_BLOCK,
-                (const uint8_t *)b_codes, (const uint8_t *)b_scales, F, D, E, rows ? offsets : nullptr, nullptr, 1, out, D, 0, 0};
+                (const uint8_t *)b_codes, (const uint8_t *)b_scales, F, D, E, rows ? offsets : nullptr, nullptr, 1, out, D, 0, false, 0};
     return with_mx_type(out_dtype, [&](auto tag) {
         return launch_packed<typename decltype(tag)::type, true>(a, (hipStream_t)hip_stream);
     });

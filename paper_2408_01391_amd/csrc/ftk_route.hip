@@ -77,7 +77,8 @@ __global__ __launch_bounds__(64 * PREFIX_WAVES) void route_prefix_kernel(int32_t
 __device__ __forceinline__ int round_up(int v, int a) { return (v + a - 1) / a * a; }
 
 // Exclusive prefix over the threads of a workgroup.
-__device__ __forceinline__ int block_prefix(int v, int *sums /* [ROUTE_WAVES], LDS */)
+template <int WAVES>
+__device__ __forceinline__ int block_prefix(int v, int *sums /* [WAVES], LDS */)
 {
     const int lane = threadIdx.x & 63;
     int run = v;
@@ -90,16 +91,33 @@ __device__ __forceinline__ int block_prefix(int v, int *sums /* [ROUTE_WAVES], L
     __syncthreads();
     int before = 0;
 #pragma unroll
-    for (int w = 0; w < ROUTE_WAVES; ++w)
+    for (int w = 0; w < WAVES; ++w)
         if (w < (int)(threadIdx.x >> 6)) before += sums[w];
     __syncthreads();
     return before + run - v;
 }
 
+// Place of a lane's slot, -1 without an expert.  The lanes of one label find each other by ballots over the label's bits, so
+// a slot's rank is the count of lower lanes in its set, and the order of the slots is kept whatever the
+// schedule; the first lane of a set moves its counter for all of them.  All lanes of a wave come here.
+__device__ __forceinline__ int place_of(uint32_t l, int E, int ebits, int *counters)
+{
+    const int lane = threadIdx.x & 63;
+    const bool routed = l < (uint32_t)E;
+    unsigned long long same = __ballot(routed);
+    for (int k = 0; k < ebits; ++k) {
+        const unsigned long long m = __ballot((l >> k) & 1);
+        same &= ((l >> k) & 1) ? m : ~m;
+    }
+    if (!routed) return -1;
+    const int rank = __popcll(same & ((1ull << lane) - 1));
+    int base = 0;
+    if (rank == 0) base = atomicAdd(&counters[l], (int)__popcll(same));
+    return __shfl(base, __ffsll(same) - 1, 64) + rank;
+}
+
 // Place of every slot.  cnt holds a row of counters for every wave, which has a contiguous quarter of the workgroup's
-// slots: first how many of each expert it has, then where its next one goes.  64 slots at a time: the
-// lanes of one label find each other by ballots over the label's bits, so a slot's rank is the count of
-// lower lanes in its set, and the order of the slots is kept whatever the schedule.
+// slots: first how many of each expert it has, then where its next one goes, 64 slots at a time.
 struct PlaceArgs {
     const int32_t *labels;
     int S, chunk, E, align, ebits;
@@ -133,7 +151,7 @@ __device__ __forceinline__ void place_slots(const PlaceArgs &a, int b, int block
             for (int i = 0; i < ROUTE_WAVES; ++i) t += cnt[i * E + e];
         need += round_up(t, a.align);
     }
-    int off = block_prefix(need, sums);
+    int off = block_prefix<ROUTE_WAVES>(need, sums);
     for (int e = e0; e < e1; ++e) {
         int run = off + (a.table ? a.table[(int64_t)b * E + e] : 0), t = 0;
         for (int i = 0; i < ROUTE_WAVES; ++i) {
@@ -161,21 +179,7 @@ __device__ __forceinline__ void place_slots(const PlaceArgs &a, int b, int block
     for (int i = i0; i < i1; i += 64) {
         const bool in = i + lane < i1;
         const uint32_t l = in ? (uint32_t)a.labels[s0 + i + lane] : 0xffffffffu;
-        const bool routed = l < (uint32_t)E;
-        unsigned long long same = __ballot(routed);
-        for (int k = 0; k < a.ebits; ++k) {
-            const unsigned long long m = __ballot((l >> k) & 1);
-            same &= ((l >> k) & 1) ? m : ~m;
-        }
-        int p = -1;
-        if (routed) {
-            const int rank = __popcll(same & ((1ull << lane) - 1));
-            // the first lane of a set moves its counter for all of them
-            int base = 0;
-            if (rank == 0) base = atomicAdd(&mine[l], __popcll(same));
-            base = __shfl(base, __ffsll(same) - 1, 64);
-            p = base + rank;
-        }
+        const int p = place_of(l, E, a.ebits, mine);
         if (in) {
             if (write) {
                 a.pos[s0 + i + lane] = p;
@@ -200,6 +204,7 @@ struct RowShape {
     int64_t N;
     int64_t rows;
     int k, D, np;  // np: pieces of a row
+    bool stream;   // the result's rows are written past the caches
 };
 
 template <typename T, typename W>
@@ -233,7 +238,7 @@ __device__ __forceinline__ void fill_rows(const int32_t *order, const RowShape &
             } else {
                 for (int i = lane; i < h.np; i += 64) {
                     PieceOf<T> z = {};
-                    put_piece(o + min(i * PIECE<T>, h.D - PIECE<T>), z);
+                    put_piece(o + min(i * PIECE<T>, h.D - PIECE<T>), z, h.stream);
                 }
             }
         }
@@ -256,7 +261,7 @@ __device__ __forceinline__ void copy_piece(const T *x, const int32_t *p, const W
         const PieceOf<T> v = row_piece(x + c);
         for (int j = 0; j < h.k; ++j) {
             const int32_t r = p[j];
-            if ((uint32_t)r < (uint64_t)h.rows) put_piece(out + r * ldo + c, w ? scale_piece<T>(v, w[j]) : v);
+            if ((uint32_t)r < (uint64_t)h.rows) put_piece(out + r * ldo + c, w ? scale_piece<T>(v, w[j]) : v, h.stream);
         }
     }
 }
@@ -347,7 +352,7 @@ __global__ __launch_bounds__(256) void route_combine_kernel(const T *__restrict_
                 PieceOf<T> o;
 #pragma unroll
                 for (int e = 0; e < PIECE<T>; ++e) o[e] = (T)acc[e];
-                put_piece(out + t * ldo + c, o);
+                put_piece(out + t * ldo + c, o, h.stream);
             } else {
                 out[t * ldo + c] = (T)acc[0];
             }
@@ -398,7 +403,7 @@ __global__ __launch_bounds__(256) void route_combine_grad_kernel(const T *__rest
                         if (!in[j]) continue;
 #pragma unroll
                         for (int e = 0; e < PIECE<T>; ++e) dot[j] += e < twice ? (Acc)0 : (Acc)g[e] * (Acc)y[j][e];
-                        put_piece(dY + r[j] * ldd + c, scale_piece<T>(g, w[j]));
+                        put_piece(dY + r[j] * ldd + c, scale_piece<T>(g, w[j]), h.stream);
                     }
                 } else {
                     const Acc g = (Acc)G[t * ldg + c];
@@ -571,6 +576,7 @@ static ftk_status launch_gather(ftk_dtype dtype, const void *X, int64_t ldx, con
         using T = typename decltype(tag)::type;
         RowShape h = shape;
         h.np = row_pieces<T>(h.D);
+        h.stream = streams_out((double)h.rows * h.D * sizeof(T));
         return with_lanes(h.np, [&](auto lanes) {
             constexpr int L = decltype(lanes)::value;
             const int fill = fill_grid(h.rows);
@@ -625,7 +631,7 @@ ftk_status ftk_route_gather(ftk_dtype dtype, const void *X, int64_t ldx, int64_t
         if (weights) FTK_TRY(check_ptr(weights, esz == 8 ? 8 : 4, "weights"));
     }
     FTK_TRY(check_device());
-    return launch_gather(dtype, X, ldx, RowShape{N, rows, k, D, 0}, order, pos, weights, out, ldo, (hipStream_t)hip_stream);
+    return launch_gather(dtype, X, ldx, RowShape{N, rows, k, D, 0, false}, order, pos, weights, out, ldo, (hipStream_t)hip_stream);
 }
 
 ftk_status ftk_route_dispatch(ftk_dtype dtype, const void *X, int64_t ldx, int32_t D, const int32_t *labels, int64_t N,
@@ -645,7 +651,7 @@ ftk_status ftk_route_dispatch(ftk_dtype dtype, const void *X, int64_t ldx, int32
     if (rows > 0 && N * k <= FTK_ROUTE_FEW && align == 1 && lds <= 32768)
         return with_type(dtype, [&](auto tag) {
             using T = typename decltype(tag)::type;
-            const RowShape h{N, rows, k, D, row_pieces<T>(D)};
+            const RowShape h{N, rows, k, D, row_pieces<T>(D), false};
             return with_lanes(h.np, [&](auto lanes) {
                 constexpr int L = decltype(lanes)::value;
                 route_few_kernel<T, L><<<row_grid(N, L), ROUTE_THREADS, lds, st>>>(a, (const T *)X, ldx, h, (T *)out, ldo);
@@ -655,7 +661,7 @@ ftk_status ftk_route_dispatch(ftk_dtype dtype, const void *X, int64_t ldx, int32
         });
     FTK_TRY(launch_plan(p, a, workspace, st));
     if (rows == 0) return FTK_OK;
-    return launch_gather(dtype, X, ldx, RowShape{N, rows, k, D, 0}, order, pos, nullptr, out, ldo, st);
+    return launch_gather(dtype, X, ldx, RowShape{N, rows, k, D, 0, false}, order, pos, nullptr, out, ldo, st);
 }
 
 ftk_status ftk_route_combine(ftk_dtype dtype, const void *Y, int64_t ldy, int64_t rows, const int32_t *pos,
@@ -677,7 +683,7 @@ ftk_status ftk_route_combine(ftk_dtype dtype, const void *Y, int64_t ldy, int64_
     hipStream_t st = (hipStream_t)hip_stream;
     return with_type(dtype, [&](auto tag) {
         using T = typename decltype(tag)::type;
-        const RowShape h{N, rows, k, D, row_pieces<T>(D)};
+        const RowShape h{N, rows, k, D, row_pieces<T>(D), streams_out((double)N * D * sizeof(T))};
         return with_lanes(h.np, [&](auto lanes) {
             constexpr int L = decltype(lanes)::value;
             return with_slots(k, [&](auto slots) {
@@ -716,7 +722,7 @@ ftk_status ftk_route_combine_grad(ftk_dtype dtype, const void *dOut, int64_t ldg
     hipStream_t st = (hipStream_t)hip_stream;
     return with_type(dtype, [&](auto tag) {
         using T = typename decltype(tag)::type;
-        const RowShape h{N, rows, k, D, row_pieces<T>(D)};
+        const RowShape h{N, rows, k, D, row_pieces<T>(D), streams_out((double)rows * D * sizeof(T))};
         return with_lanes(h.np, [&](auto lanes) {
             constexpr int L = decltype(lanes)::value;
             return with_slots(k, [&](auto slots) {

@@ -28,11 +28,29 @@ __device__ __forceinline__ PieceOf<T> row_piece(const T *p)
 {
     return *reinterpret_cast<const PieceOf<T> *>(p);
 }
+// STREAM_STORE(to, value, stream): *to = value; where `stream`, past the caches (see streams_out).  A macro, because a function would
+// lose the alignment of what `to` points to; the empty statements keep the branch, of whose two stores the
+// compiler would make an ordinary one.
+#define STREAM_STORE(to, value, stream)                    \
+    do {                                                   \
+        if (stream) {                                      \
+            asm volatile("");                              \
+            __builtin_nontemporal_store((value), (to));    \
+            asm volatile("");                              \
+        } else {                                           \
+            *(to) = (value);                               \
+        }                                                  \
+    } while (0)
 template <typename T>
-__device__ __forceinline__ void put_piece(T *p, PieceOf<T> v)
+__device__ __forceinline__ void put_piece(T *p, PieceOf<T> v, bool stream = false)
 {
-    *reinterpret_cast<PieceOf<T> *>(p) = v;
+    STREAM_STORE(reinterpret_cast<PieceOf<T> *>(p), v, stream);
 }
+
+// Results of more than a quarter of the memory-side cache's 256 MB go past the caches: whoever reads them next finds little of
+// them there, and the operands stay.  (With and without: rows to their places, 60000 x 1024 fp32 99 / 119 us; weighted sum back,
+// 65536 x 2 slots x 1024 bf16 61 / 76; 65536 x 2048 bf16 from 4 bits and back 110 / 139; but 40 MB from 4 bits 15 / 11.)
+static inline bool streams_out(double bytes) { return bytes > 64e6; }
 
 // Rows are read by whole pieces; the last one is moved back into the row where the row is no multiple of a
 // piece, so that two pieces may share elements.  Rows shorter than a piece go by elements (one "piece" each).
