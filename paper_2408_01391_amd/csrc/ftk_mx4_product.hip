@@ -80,6 +80,22 @@ __device__ __forceinline__ bool find_tile(const MxProduct &a, int64_t t, RowTile
     return r.m0 >= first && r.m0 < r.end;
 }
 
+// The expert with the i-th most rows, among up to 64 (else expert i).  Sums over rows take as long as an expert has rows, and
+// workgroups start in order: the long ones first, so that none is left over (8 experts of 1400 to 8000 rows, 4096 x 2048
+// sums each, 235 us in the experts' own order).
+__device__ __forceinline__ int by_size(const MxProduct &a, int i)
+{
+    if (!a.offsets || a.E > 64) return i;
+    const int lane = threadIdx.x & 63;
+    const int rows = lane < a.E ? (int)((uint32_t)a.offsets[lane + 1] - (uint32_t)a.offsets[lane]) : INT32_MIN;
+    int larger = 0;
+    for (int e = 0; e < a.E; ++e) {
+        const int other = __builtin_amdgcn_readlane(rows, e);
+        larger += other > rows || (other == rows && e < lane);
+    }
+    return __builtin_amdgcn_readfirstlane((int)__ffsll(__ballot(lane < a.E && larger == i)) - 1);
+}
+
 __device__ __forceinline__ int64_t source_of(const MxProduct &a, int64_t m, int32_t slot)
 {
     const int64_t s = !a.order ? m : slot < 0 ? -1 : slot / a.k;
@@ -327,6 +343,7 @@ __global__ __launch_bounds__(256, MT* NT >= 64 ? 1 : 2) void mx_tile_kernel(MxPr
         const int64_t mt = (a.M + S::TM - 1) / S::TM;
         e = (int)(t / mt);
         m0 = (t - (int64_t)e * mt) * S::TM;
+        e = by_size(a, e);
         end = a.M;
         if (a.offsets) {
             k0 = min(k1, max(0, a.offsets[e]) / 128);

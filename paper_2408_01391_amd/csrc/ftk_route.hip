@@ -654,7 +654,7 @@ ftk_status ftk_route_dispatch(ftk_dtype dtype, const void *X, int64_t ldx, int32
             const RowShape h{N, rows, k, D, row_pieces<T>(D), false};
             return with_lanes(h.np, [&](auto lanes) {
                 constexpr int L = decltype(lanes)::value;
-                route_few_kernel<T, L><<<row_grid(N, L), ROUTE_THREADS, lds, st>>>(a, (const T *)X, ldx, h, (T *)out, ldo);
+                route_few_kernel<T, L><<<N > 0 ? row_grid(N, L) : 1, ROUTE_THREADS, lds, st>>>(a, (const T *)X, ldx, h, (T *)out, ldo);
                 FTK_TRY_HIP(hipGetLastError());
                 return FTK_OK;
             });

@@ -226,6 +226,16 @@ def test_nothing_to_do():
     assert ftk.route_combine(out, r).shape == (0, 8)
     dY, dw = ftk.route_combine_grad(X, out, r, torch.empty(0, 3, device=DEV))
     assert dY.shape == (0, 8) and dw.shape == (0, 3)
+    # arrays for more slots than there are: all of them hold nothing
+    i32 = lambda *s: torch.full(s, 12345, dtype=torch.int32, device=DEV)  # noqa: E731
+    for align in (1, 16):
+        big = ftk.Route(i32(6), i32(5), i32(48), torch.empty(0, 3, dtype=torch.int32, device=DEV), align)
+        out = torch.full((48, 8), 3.0, device=DEV)
+        ftk.route_dispatch(X, labels, 5, align, out=out, route=big)
+        assert (out == 0).all() and (big.order == -1).all() and big.offsets.tolist() == [0] * 6
+        dY = torch.full((48, 8), 3.0, device=DEV)
+        ftk.route_combine_grad(X, out, big, torch.empty(0, 3, device=DEV), dY=dY)
+        assert (dY == 0).all()
 
 
 def test_index_arrays_that_lie():
