@@ -416,12 +416,12 @@ ftk_status ftk_mx4_matmul(ftk_dtype out_dtype, const void *a_codes, const void *
                           void *out, int64_t ldo, void *hip_stream);
 
 /* The same from dense rows X [N x D] of `dtype`, packed on the way exactly as ftk_mx4_quantize does; out has
- * their type.  workspace: ftk_mx4_workspace_bytes(N, D, M) bytes; where that is 0, as for few rows, NULL will do. */
+ * their type.  workspace: ftk_mx4_workspace_bytes(N, D, M, E) bytes; where that is 0, as for few rows, NULL will do. */
 ftk_status ftk_mx4_linear(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N, const void *b_codes,
                           const void *b_scales, int64_t M, int32_t F, int32_t D, int32_t E,
                           const int32_t *offsets /* nullable */, const int32_t *order /* nullable */, int32_t k,
                           void *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *hip_stream);
-int64_t ftk_mx4_workspace_bytes(int64_t N, int32_t D, int64_t M); /* -1: bad arguments */
+int64_t ftk_mx4_workspace_bytes(int64_t N, int32_t D, int64_t M, int32_t E); /* -1: bad arguments */
 
 /* Sums over the rows of every expert, the gradient of the experts' matrices:
  *   out[e][f, d] = sum over p in [offsets[e], offsets[e + 1]) of A[f, p] * B[d, p]

@@ -106,7 +106,7 @@ def load():
     L.ftk_mx4_matmul.restype = i32
     L.ftk_mx4_linear.argtypes = [i32, vp, i64, i64, vp, vp, i64, i32, i32, i32, vp, vp, i32, vp, i64, vp, sz, vp]
     L.ftk_mx4_linear.restype = i32
-    L.ftk_mx4_workspace_bytes.argtypes = [i64, i32, i64]
+    L.ftk_mx4_workspace_bytes.argtypes = [i64, i32, i64, i32]
     L.ftk_mx4_workspace_bytes.restype = i64
     L.ftk_mx4_outer.argtypes = [i32, vp, vp, vp, vp, i64, i32, i32, i32, vp, vp, vp]
     L.ftk_mx4_outer.restype = i32
@@ -669,8 +669,8 @@ def mx4_matmul(A, B, route=None, gather=False, out=None, out_dtype=torch.bfloat1
     return out
 
 
-def mx4_workspace_bytes(N: int, D: int, M: int) -> int:
-    n = load().ftk_mx4_workspace_bytes(N, D, M)
+def mx4_workspace_bytes(N: int, D: int, M: int, E: int = 1) -> int:
+    n = load().ftk_mx4_workspace_bytes(N, D, M, E)
     if n < 0:
         raise FtkError(1, load().ftk_last_error().decode())
     return n
@@ -684,7 +684,7 @@ def mx4_linear(X, B, route=None, gather=False, out=None, workspace=None):
         raise ValueError("X and B must share D (got %d and %d)" % (D, B.D))
     E, F, M, offsets, order, k = _groups(B, route, gather, N)
     out, ldo = _new_rows(out, M, F, X, "out")
-    workspace, wp, wn = _workspace(workspace, mx4_workspace_bytes(N, D, M), X.device)
+    workspace, wp, wn = _workspace(workspace, mx4_workspace_bytes(N, D, M, E), X.device)
     _check(load().ftk_mx4_linear(_row_code(X, "X", _MX_DTYPES), X.data_ptr(), ld, N, B.codes.data_ptr(),
                                  B.scales.data_ptr(), M, F, D, E, _ptr(offsets), _ptr(order), k, out.data_ptr(),
                                  ldo, wp, wn, _stream()))

@@ -82,7 +82,7 @@ __device__ __forceinline__ bool find_tile(const MxProduct &a, int64_t t, RowTile
 
 // The expert with the i-th most rows, among up to 64 (else expert i).  Sums over rows take as long as an expert has rows, and
 // workgroups start in order: the long ones first, so that none is left over (8 experts of 1400 to 8000 rows, 4096 x 2048
-// sums each, 235 us in the experts' own order).
+// sums each, with the packing and the rows' gradients 582 us, in the experts' own order 615).
 __device__ __forceinline__ int by_size(const MxProduct &a, int i)
 {
     if (!a.offsets || a.E > 64) return i;
@@ -157,7 +157,9 @@ __device__ __forceinline__ void mx_sums_done(float4v (&c)[MT][NT])
 // Few rows: 16 output rows by 16 * CT columns a workgroup, whose WAVES waves share the steps of 128 elements out between
 // them, a run each, and add their sums up in LDS.  Operands go from memory straight to registers, UNROLL steps
 // at a time, all requested before the first is used: with one row the weights' way from memory is all the time there
-// is.  A dense row is packed on the way, the whole block of 32 within a lane.
+// is.  A dense row is packed on the way, the whole block of 32 within a lane.  (One token, two matrices of 4096 x 4096: 17.8 MB in 9.6 us
+// with 32 columns and 8 waves a workgroup, 1.9 TB/s behind three dependent requests - offsets, rows or weights, and the launch;
+// 16 columns 11.2, 64 columns 13.0, 16 waves 9.5.)
 template <typename Src, typename Out, int CT, int WAVES, bool OUTER>
 __global__ __launch_bounds__(64 * WAVES) void mx_direct_kernel(MxProduct a)
 {
@@ -288,19 +290,6 @@ static ftk_status launch_direct(MxProduct a, hipStream_t st)
     return FTK_OK;
 }
 
-// Many rows: TM = 32 * MT rows by TN = 32 * NT columns a workgroup, a quarter of them a wave.  k goes in stages of 256
-// elements, one 128-byte line of codes a row, copied straight to LDS a stage ahead of their use; scales go two
-// stages (16 bytes a row) at a time.  A stage is two steps of the instruction.  Which 128 of its elements a step takes is
-// free as long as both operands agree: lane quarter q takes blocks 2q and 2q + 1, so that the scales of both steps
-// are one 16-bit word, out of which the instruction picks the byte.
-//
-// LDS rows are lines of eight 16-byte pieces, piece p at place p ^ key: the key is half the lane row that reads the line, so
-// that the sixteen lanes that LDS serves at once read sixteen different places of its 256 bytes.  The copy keeps the order of its lanes, so it is the lanes' addresses
-// that are permuted, within a line.
-// Column tile j of a wave has, for lane row r, column 32 * (j / 2) + 8 * (r / 4) + 4 * (j % 2) + r % 4: two
-// tiles together give a lane eight consecutive columns to store.
-//
-// While one step's fragments are multiplied the next one's are read.
 // Copies as to_lds16 (ftk_mma.h), to an LDS address; the second from a common base and 32-bit offsets of the lanes.
 __device__ __forceinline__ void to_lds16_at(const uint8_t *g, uint32_t at)
 {
@@ -318,6 +307,26 @@ __device__ __forceinline__ const uint8_t *uniform(const uint8_t *p)
     return (const uint8_t *)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)b) |
                              (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) << 32);
 }
+
+// Many rows: TM = 32 * MT rows by TN = 32 * NT columns a workgroup, a quarter of them a wave.  k goes in stages of 256
+// elements, one 128-byte line of codes a row, copied straight to LDS a stage ahead of their use; scales go two
+// stages (16 bytes a row) at a time.  A stage is two steps of the instruction.  Which 128 of its elements a step takes is
+// free as long as both operands agree: lane quarter q takes blocks 2q and 2q + 1, so that the scales of both steps
+// are one 16-bit word, out of which the instruction picks the byte.  While one step's fragments are multiplied the next
+// one's are read.
+//
+// LDS rows are lines of eight 16-byte pieces, piece p at place p ^ key: the key is half the lane row that reads the line, so
+// that the sixteen lanes that LDS serves at once read sixteen different places of its 256 bytes.  The copy keeps the
+// order of its lanes, so it is the lanes' addresses that are permuted, within a line.
+// Column tile j of a wave has, for lane row r, column 32 * (j / 2) + 8 * (r / 4) + 4 * (j % 2) + r % 4: two
+// tiles together give a lane eight consecutive columns to store.
+//
+// 256 x 256 sums a workgroup (MT = NT = 8), one workgroup a compute unit: 16384 x 2 rows through 16 matrices of 4096 x 4096 in
+// 340 to 355 us, 3.1 to 3.2 PFLOP/s; the matrix instructions alone would take 160 at the rate that power leaves them on
+// such data (6.9 PFLOP/s; 9 on zeros).  The rest: copies 90, of which scales 32, writing the results 55, LDS reads 35; they
+// do not hide behind the products, for a wave has its SIMD to itself and issues in order.  Two waves a SIMD (wave tiles of
+// 128 x 64) took 9 % longer, two workgroups of 256 x 128 12 %, copies four steps of 64-byte lines ahead 5 %, workgroups
+// that go on to their next tile while the last one's results leave 5 %.
 
 template <int MT, int NT>
 struct TileShape {
@@ -601,8 +610,10 @@ static ftk_status launch_packed(const MxProduct &a, hipStream_t st)
     return middle <= small ? launch_tile<4, 4, Out, OUTER>(a, st) : launch_tile<2, 2, Out, OUTER>(a, st);
 }
 
-// Whether dense rows are packed by every workgroup that needs them rather than once beforehand.
-static bool few_rows(int64_t M) { return M <= 16; }
+// Whether dense rows are packed by every workgroup that needs them rather than once beforehand, in a launch of its own.  (Whole call,
+// matrices of 4096 x 4096, with / without: 2 rows 12.2 / 16.8 us, 8 rows of 8 experts 16.5 / 16.7, 16 rows 23.3 / 17.1, of one expert
+// 12.3 / 16.8.)
+static bool few_rows(int64_t M, int E) { return M <= 8 || (M <= 16 && E <= 4); }
 
 static size_t packed_bytes(int64_t N, int D, size_t *codes)
 {
@@ -648,13 +659,14 @@ using namespace ftk;
 
 extern "C" {
 
-int64_t ftk_mx4_workspace_bytes(int64_t N, int32_t D, int64_t M)
+int64_t ftk_mx4_workspace_bytes(int64_t N, int32_t D, int64_t M, int32_t E)
 {
-    if (N < 0 || M < 0 || D < 1 || N > 0x7fffffffLL || M > 0x7fffffffLL || D > MX_MAX) {
-        set_error("need 0 <= N, M < 2^31, 1 <= D <= %d (got N=%lld M=%lld D=%d)", MX_MAX, (long long)N, (long long)M, D);
+    if (N < 0 || M < 0 || D < 1 || E < 1 || N > 0x7fffffffLL || M > 0x7fffffffLL || D > MX_MAX) {
+        set_error("need 0 <= N, M < 2^31, 1 <= D <= %d, E >= 1 (got N=%lld M=%lld D=%d E=%d)", MX_MAX, (long long)N, (long long)M, D,
+                  E);
         return -1;
     }
-    return N == 0 || few_rows(M) ? 0 : (int64_t)packed_bytes(N, D, nullptr);
+    return N == 0 || few_rows(M, E) ? 0 : (int64_t)packed_bytes(N, D, nullptr);
 }
 
 ftk_status ftk_mx4_matmul(ftk_dtype out_dtype, const void *a_codes, const void *a_scales, int64_t N, const void *b_codes,
@@ -686,7 +698,7 @@ ftk_status ftk_mx4_linear(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N
         return FTK_EINVAL;
     }
     if (N > 0) FTK_TRY(check_ptr(X, dtype_size(dtype), "X"));
-    const bool few = N == 0 || few_rows(M);
+    const bool few = N == 0 || few_rows(M, E);
     if (!few) FTK_TRY(check_workspace(workspace, workspace_bytes, packed_bytes(N, D, nullptr)));
     FTK_TRY(check_device());
     hipStream_t st = (hipStream_t)hip_stream;

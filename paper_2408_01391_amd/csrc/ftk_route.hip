@@ -152,24 +152,31 @@ __device__ __forceinline__ void place_slots(const PlaceArgs &a, int b, int block
         need += round_up(t, a.align);
     }
     int off = block_prefix<ROUTE_WAVES>(need, sums);
-    for (int e = e0; e < e1; ++e) {
-        int run = off + (a.table ? a.table[(int64_t)b * E + e] : 0), t = 0;
-        for (int i = 0; i < ROUTE_WAVES; ++i) {
-            const int c = cnt[i * E + e];
-            cnt[i * E + e] = run;
-            run += c;
-            t += c;
+    for (int i = 0; i < per; ++i) {
+        const int e = e0 + i;
+        int fill = 0, end = 0;  // rows that hold nothing, a wave's experts' one after the other
+        if (e < e1) {
+            int run = off + (a.table ? a.table[(int64_t)b * E + e] : 0), t = 0;
+            for (int v = 0; v < ROUTE_WAVES; ++v) {
+                const int c = cnt[v * E + e];
+                cnt[v * E + e] = run;
+                run += c;
+                t += c;
+            }
+            if (a.totals) t = a.totals[e];
+            end = off + round_up(t, a.align);
+            if (write && b == 0) {
+                a.offsets[e] = off;
+                if (a.counts) a.counts[e] = t;
+                if (e == E - 1) a.offsets[E] = end;
+            }
+            fill = write && e % blocks == b ? off + t : end;
+            off = end;
         }
-        if (a.totals) t = a.totals[e];
-        const int end = off + round_up(t, a.align);
-        if (write && b == 0) {
-            a.offsets[e] = off;
-            if (a.counts) a.counts[e] = t;
-            if (e == E - 1) a.offsets[E] = end;
+        for (unsigned long long m = __ballot(fill < end); m; m &= m - 1) {
+            const int from = __shfl(fill, __ffsll(m) - 1, 64), to = __shfl(end, __ffsll(m) - 1, 64);
+            for (int64_t p = (int64_t)from + lane; p < to; p += 64) a.order[p] = -1;
         }
-        if (write && e % blocks == b)
-            for (int p = off + t; p < end; ++p) a.order[p] = -1;
-        off = end;
     }
     if (e1 == E && e0 < E) sums[0] = off;  // all sorted rows
     __syncthreads();
@@ -576,7 +583,6 @@ static ftk_status launch_gather(ftk_dtype dtype, const void *X, int64_t ldx, con
         using T = typename decltype(tag)::type;
         RowShape h = shape;
         h.np = row_pieces<T>(h.D);
-        h.stream = streams_out((double)h.rows * h.D * sizeof(T));
         return with_lanes(h.np, [&](auto lanes) {
             constexpr int L = decltype(lanes)::value;
             const int fill = fill_grid(h.rows);

@@ -48,8 +48,9 @@ __device__ __forceinline__ void put_piece(T *p, PieceOf<T> v, bool stream = fals
 }
 
 // Results of more than a quarter of the memory-side cache's 256 MB go past the caches: whoever reads them next finds little of
-// them there, and the operands stay.  (With and without: rows to their places, 60000 x 1024 fp32 99 / 119 us; weighted sum back,
-// 65536 x 2 slots x 1024 bf16 61 / 76; 65536 x 2048 bf16 from 4 bits and back 110 / 139; but 40 MB from 4 bits 15 / 11.)
+// them there, and the operands stay.  (With and without, in turn with other operands: weighted sum back, 65536 x 2 slots x 1024 bf16
+// 70 / 76 us; both gradients 205 / 215; 65536 x 2048 bf16 to 4 bits and back 105 / 142; but 40 MB from 4 bits 15 / 11, and rows to
+// their places, 60000 x 1024 fp32, 125 / 124 among others and 149 / 140 alone: those are written as usual.)
 static inline bool streams_out(double bytes) { return bytes > 64e6; }
 
 // Rows are read by whole pieces; the last one is moved back into the row where the row is no multiple of a

@@ -341,7 +341,7 @@ def test_on_another_stream_and_in_a_graph():
         got = ftk.mx4_linear(X, W, r, gather=True)
     torch.cuda.current_stream().wait_stream(side)
     assert torch.equal(got, want)
-    ws = torch.empty(ftk.mx4_workspace_bytes(N, D, r.rows) + 256, dtype=torch.uint8, device=DEV)
+    ws = torch.empty(ftk.mx4_workspace_bytes(N, D, r.rows, E) + 256, dtype=torch.uint8, device=DEV)
     out = torch.empty_like(want)
     g = torch.cuda.CUDAGraph()
     with torch.cuda.graph(g):

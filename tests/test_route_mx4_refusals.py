@@ -29,7 +29,7 @@ def test_sizes():
         ftk.route_workspace_bytes(1, 1, 0)
     assert ftk.mx4_workspace_bytes(100, 1000, 10000) >= 100 * 1024 * 17 // 32
     assert ftk.mx4_workspace_bytes(0, 1000, 10000) == 0
-    for bad in ((-1, 10, 1), (1, 0, 1), (1, 10, -1), (1, 1 << 25, 1), (1 << 31, 10, 1)):
+    for bad in ((-1, 10, 1), (1, 0, 1), (1, 10, -1), (1, 1 << 25, 1), (1 << 31, 10, 1), (1, 10, 1, 0)):
         with pytest.raises(ftk.FtkError):
             ftk.mx4_workspace_bytes(*bad)
 
