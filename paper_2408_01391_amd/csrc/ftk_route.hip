@@ -129,41 +129,61 @@ __device__ __forceinline__ void place_slots(const PlaceArgs &a, int b, int block
                                             int *lds_pos /* or NULL */)
 {
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, E = a.E;
-    for (int i = tid; i < ROUTE_WAVES * E; i += ROUTE_THREADS) cnt[i] = 0;
-    __syncthreads();
     const int64_t s0 = (int64_t)b * a.chunk;
     const int n = (int)((int64_t)a.S - s0 < a.chunk ? (int64_t)a.S - s0 : a.chunk);
     const int each = round_up((n + ROUTE_WAVES - 1) / ROUTE_WAVES, 64), i0 = w * each, i1 = min(n, i0 + each);
+    // what has to be read is asked for at once: a lane's first labels, and the counts of a thread's first experts (a thread
+    // has a run of consecutive ones)
+    const int per = (E + ROUTE_THREADS - 1) / ROUTE_THREADS, e0 = min(E, tid * per), e1 = min(E, e0 + per);
+    constexpr int KEEP = ROUTE_CHUNK / ROUTE_THREADS;
+    uint32_t label[KEEP];
+    int total[KEEP], before[KEEP];
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k) {
+        const int i = i0 + k * 64 + lane;
+        label[k] = i < i1 ? (uint32_t)a.labels[s0 + i] : 0xffffffffu;
+        total[k] = a.totals && e0 + k < e1 ? a.totals[e0 + k] : 0;
+        before[k] = a.table && e0 + k < e1 ? a.table[(int64_t)b * E + e0 + k] : 0;
+    }
+    for (int i = tid; i < ROUTE_WAVES * E; i += ROUTE_THREADS) cnt[i] = 0;
+    __syncthreads();
     int *mine = cnt + w * E;
-    for (int i = i0 + lane; i < i1; i += 64) {
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k)
+        if (label[k] < (uint32_t)E) atomicAdd(&mine[label[k]], 1);
+    for (int i = i0 + KEEP * 64 + lane; i < i1; i += 64) {
         const uint32_t l = (uint32_t)a.labels[s0 + i];
         if (l < (uint32_t)E) atomicAdd(&mine[l], 1);
     }
     __syncthreads();
-    // a thread has a run of consecutive experts
-    const int per = (E + ROUTE_THREADS - 1) / ROUTE_THREADS, e0 = min(E, tid * per), e1 = min(E, e0 + per);
+    // f(expert of the run, its slots, those before this workgroup's)
+    auto for_experts = [&](auto f) {
+#pragma unroll
+        for (int k = 0; k < KEEP; ++k)
+            if (k < per) f(e0 + k, total[k], before[k]);
+        for (int e = e0 + KEEP; e < e0 + per; ++e)
+            f(e, a.totals && e < e1 ? a.totals[e] : 0, a.table && e < e1 ? a.table[(int64_t)b * E + e] : 0);
+    };
     int need = 0;
-    for (int e = e0; e < e1; ++e) {
-        int t = 0;
-        if (a.totals)
-            t = a.totals[e];
-        else
-            for (int i = 0; i < ROUTE_WAVES; ++i) t += cnt[i * E + e];
+    for_experts([&](int e, int t, int) {
+        if (e >= e1) return;
+        if (!a.totals)
+            for (int v = 0; v < ROUTE_WAVES; ++v) t += cnt[v * E + e];
         need += round_up(t, a.align);
-    }
+    });
     int off = block_prefix<ROUTE_WAVES>(need, sums);
-    for (int i = 0; i < per; ++i) {
-        const int e = e0 + i;
+    for_experts([&](int e, int t, int run) {
         int fill = 0, end = 0;  // rows that hold nothing, a wave's experts' one after the other
         if (e < e1) {
-            int run = off + (a.table ? a.table[(int64_t)b * E + e] : 0), t = 0;
+            int mine_all = 0;
+            run += off;
             for (int v = 0; v < ROUTE_WAVES; ++v) {
                 const int c = cnt[v * E + e];
                 cnt[v * E + e] = run;
                 run += c;
-                t += c;
+                mine_all += c;
             }
-            if (a.totals) t = a.totals[e];
+            if (!a.totals) t = mine_all;
             end = off + round_up(t, a.align);
             if (write && b == 0) {
                 a.offsets[e] = off;
@@ -177,24 +197,26 @@ __device__ __forceinline__ void place_slots(const PlaceArgs &a, int b, int block
             const int from = __shfl(fill, __ffsll(m) - 1, 64), to = __shfl(end, __ffsll(m) - 1, 64);
             for (int64_t p = (int64_t)from + lane; p < to; p += 64) a.order[p] = -1;
         }
-    }
+    });
     if (e1 == E && e0 < E) sums[0] = off;  // all sorted rows
     __syncthreads();
     if (write)
         for (int64_t p = sums[0] + (int64_t)b * ROUTE_THREADS + tid; p < a.rows; p += (int64_t)blocks * ROUTE_THREADS)
             a.order[p] = -1;
-    for (int i = i0; i < i1; i += 64) {
-        const bool in = i + lane < i1;
-        const uint32_t l = in ? (uint32_t)a.labels[s0 + i + lane] : 0xffffffffu;
+    auto place = [&](int i, uint32_t l) {  // 64 slots from i on
         const int p = place_of(l, E, a.ebits, mine);
-        if (in) {
+        if (i + lane < i1) {
             if (write) {
                 a.pos[s0 + i + lane] = p;
                 if (p >= 0) a.order[p] = (int)(s0 + i + lane);
             }
             if (lds_pos) lds_pos[i + lane] = p;
         }
-    }
+    };
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k)
+        if (i0 + k * 64 < i1) place(i0 + k * 64, label[k]);
+    for (int i = i0 + KEEP * 64; i < i1; i += 64) place(i, i + lane < i1 ? (uint32_t)a.labels[s0 + i + lane] : 0xffffffffu);
 }
 
 __global__ __launch_bounds__(ROUTE_THREADS) void route_place_kernel(PlaceArgs a)
@@ -268,7 +290,7 @@ __device__ __forceinline__ void copy_piece(const T *x, const int32_t *p, const W
         const PieceOf<T> v = row_piece(x + c);
         for (int j = 0; j < h.k; ++j) {
             const int32_t r = p[j];
-            if ((uint32_t)r < (uint64_t)h.rows) put_piece(out + r * ldo + c, w ? scale_piece<T>(v, w[j]) : v, h.stream);
+            if ((uint32_t)r < (uint64_t)h.rows) put_piece(out + r * ldo + c, w ? scale_piece<T>(v, w[j]) : v);
         }
     }
 }
