@@ -265,6 +265,7 @@ __global__ __launch_bounds__(64 * WAVES) void mx_direct_kernel(MxProduct a)
         float4v sum = part[0][i][lane];
 #pragma unroll
         for (int v = 1; v < WAVES; ++v) sum += part[v][i][lane];
+        if (src < 0) sum = float4v{0, 0, 0, 0};  // (zeros times a matrix that holds NaN are not)
         store4(o, n0 + 16 * i + 4 * q, a.F, sum);
     }
 }

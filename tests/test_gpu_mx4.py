@@ -353,3 +353,28 @@ def test_on_another_stream_and_in_a_graph():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("M", [1, 8, 16, 40, 700])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_rows_without_a_slot_are_zero_beside_nan_weights(M, dtype):
+    """An output row whose order is -1 becomes zero whatever its expert's matrix holds, for few rows and many."""
+    rng = np.random.default_rng(21)
+    N, D, F, E = max(1, M // 2), 160, 70, 2
+    X = dev(rng.standard_normal((N, D)).astype(np.float32)).to(DTYPES[dtype])
+    B = rng.standard_normal((E * F, D)).astype(np.float32)
+    B[3, 7] = np.nan  # of the first expert
+    B[F + 5, 150] = np.inf  # of the second
+    W = ftk.mx4_quantize(dev(B))
+    order = torch.arange(M, dtype=torch.int32, device=DEV) % (2 * N)
+    order[::2] = -1
+    first = (M + 1) // 2
+    off = torch.tensor([0, first, M], dtype=torch.int32, device=DEV)
+    r = ftk.Route(off, off[:E], order, torch.arange(2 * N, dtype=torch.int32, device=DEV).view(N, 2), 1)
+    for out in (ftk.mx4_linear(X, W, r, gather=True), ftk.mx4_matmul(ftk.mx4_quantize(X), W, r, gather=True, out_dtype=X.dtype)):
+        assert (out[::2] == 0).all()
+        nan = torch.isnan(out)
+        want = torch.zeros_like(nan)
+        want[1:first:2, 3] = True
+        want[first + (first + 1) % 2::2, 5] = True
+        assert torch.equal(nan, want)
