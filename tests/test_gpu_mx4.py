@@ -378,3 +378,21 @@ def test_rows_without_a_slot_are_zero_beside_nan_weights(M, dtype):
         want[1:first:2, 3] = True
         want[first + (first + 1) % 2::2, 5] = True
         assert torch.equal(nan, want)
+
+
+def test_sums_over_very_many_rows():
+    """More than 2^25 rows, beyond which lines of codes are too long for the tiles' 32-bit offsets.  All sums are exact."""
+    big, rows = 2 ** 25, 2 ** 25 + 384
+    A = torch.zeros(rows, 3, dtype=torch.float16, device=DEV)
+    B = torch.zeros(rows, 2, dtype=torch.float16, device=DEV)
+    A[:, 0] = 1
+    A[big - 1, 1], A[-1, 1] = 3, 2
+    A[::1024, 2] = 1
+    B[:, 0] = 1
+    B[big - 1, 1], B[-1, 1] = 2, -4
+    off = torch.tensor([0, big, rows], dtype=torch.int32, device=DEV)
+    order = torch.arange(rows, dtype=torch.int32, device=DEV)
+    r = ftk.Route(off, off[:2], order, order.view(rows, 1), 128)
+    got = ftk.mx4_outer(ftk.mx4_quantize(A, transpose=True), ftk.mx4_quantize(B, transpose=True), r)
+    assert got[0].tolist() == [[2.0 ** 25, 2.0], [3.0, 6.0], [2.0 ** 15, 0.0]]
+    assert got[1].tolist() == [[384.0, -4.0], [2.0, -8.0], [1.0, 0.0]]
