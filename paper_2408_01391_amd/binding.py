@@ -705,6 +705,8 @@ def mx4_outer(A, B, route=None, out=None, out_dtype=torch.float32):
             raise ValueError("mx4_outer takes all sorted rows, and a route whose align is a multiple of 128")
     if out is None:
         out = torch.empty(E, A.N, B.N, dtype=out_dtype, device=A.codes.device)
+    elif not out.is_cuda:
+        raise ValueError("out must live on the GPU")
     elif tuple(out.shape) != (E, A.N, B.N) or not out.is_contiguous():
         raise ValueError("out must be a contiguous tensor [%d, %d, %d]" % (E, A.N, B.N))
     _check(load().ftk_mx4_outer(_row_code(out, "out", _MX_DTYPES), A.codes.data_ptr(), A.scales.data_ptr(),

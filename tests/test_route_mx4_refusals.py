@@ -95,3 +95,11 @@ def test_binding():
     # the calls that do not know the 16-bit types refuse them
     assert ftk.load().ftk_workspace_bytes(ftk.BF16, 100, 8, 4, 0) == 0
     refused(1, "ftk_absmax", ftk.F16, P, 10, P, None)
+
+
+def test_sums_into_host_memory(monkeypatch):
+    """A result on the host is refused before its address goes anywhere."""
+    monkeypatch.setattr(ftk.Mx4, "check", lambda self, name: self)  # (there may be no device to hold the operands)
+    q = ftk.Mx4(torch.zeros(3, 64, dtype=torch.uint8), torch.zeros(3, 4, dtype=torch.uint8), 128)
+    with pytest.raises(ValueError, match="out must live on the GPU"):
+        ftk.mx4_outer(q, q, out=torch.zeros(1, 3, 3))
