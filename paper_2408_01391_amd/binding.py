@@ -188,9 +188,14 @@ def new_workspace(X: torch.Tensor, K: int, ft_mode: int = FT_CORRECT) -> torch.T
 
 
 def _ws_args(ws: torch.Tensor):
+    """(first aligned address, bytes from there on) of a workspace, a contiguous device tensor of any type."""
+    if not ws.is_cuda:
+        raise ValueError("workspace must live on the GPU")
+    if not ws.is_contiguous():
+        raise ValueError("workspace must be contiguous")
     base = ws.data_ptr()
     aligned = (base + 255) // 256 * 256
-    return aligned, ws.numel() - (aligned - base)
+    return aligned, max(0, ws.numel() * ws.element_size() - (aligned - base))
 
 
 def assign_geometry(dtype_code: int, N: int, D: int, K: int, ft_mode: int = FT_OFF) -> Geometry:

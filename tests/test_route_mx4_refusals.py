@@ -103,3 +103,31 @@ def test_sums_into_host_memory(monkeypatch):
     q = ftk.Mx4(torch.zeros(3, 64, dtype=torch.uint8), torch.zeros(3, 4, dtype=torch.uint8), 128)
     with pytest.raises(ValueError, match="out must live on the GPU"):
         ftk.mx4_outer(q, q, out=torch.zeros(1, 3, 3))
+
+
+class OnDevice:
+    """What the binding looks at of a workspace, without a device."""
+
+    def __init__(self, t, base):
+        self.t, self.base, self.is_cuda = t, base, True
+
+    def data_ptr(self):
+        return self.base
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+
+def test_workspaces():
+    host = torch.zeros(4096, dtype=torch.uint8)
+    for take in (ftk._ws_args, lambda ws: ftk._workspace(ws, 1024, "cuda:0")):
+        with pytest.raises(ValueError, match="GPU"):
+            take(host)
+        with pytest.raises(ValueError, match="contiguous"):
+            take(OnDevice(host[:1].expand(4096), P))
+        assert take(OnDevice(host, P))[-2:] == (P, 4096)
+        assert take(OnDevice(host[:1000].view(torch.float32), P))[-2:] == (P, 1000)  # bytes, whatever the type
+        assert take(OnDevice(host[:1000], P + 1))[-2:] == (P + 256, 745)
+        assert take(OnDevice(host[:255], P + 1))[-1] == 0
+        # what alignment takes away is not more than there is: a size below zero would be an enormous one to the library
+        assert take(OnDevice(host[:10], P + 1))[-1] == 0
