@@ -405,7 +405,8 @@ ftk_status ftk_mx4_dequantize(ftk_dtype dtype, const void *codes, const void *sc
 /* The experts' products on packed rows: out[m, f] = sum_d A[src(m), d] * B[g(m) * F + f, d].
  *   A : N packed rows of D elements; B : E * F packed rows of D elements, E matrices of F rows.
  *   offsets [E + 1]  : expert e has the output rows [offsets[e], offsets[e + 1]) (device data, ascending, within
- *                      [0, M]); rows outside all of them become zero.  NULL: E must be 1 and has all rows.
+ *                      [0, M]); rows in front of the first one's and behind the last one's become zero.  NULL: E
+ *                      must be 1 and has all rows.
  *   order [M], k     : src(m) = order[m] / k, and an output row whose order[m] is -1 becomes zero; NULL: src(m) = m.
  *   out [M x F]      : FTK_F32, FTK_BF16 or FTK_F16, row stride ldo.  N must be at least M where order is NULL.
  * Products of 4-bit elements are exact, sums are held in 32 bits and rounded once to out's type.

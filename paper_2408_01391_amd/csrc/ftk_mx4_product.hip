@@ -38,8 +38,7 @@ struct MxProduct {
 // whatever they hold, the rows stay within [0, M].
 __device__ __forceinline__ int64_t first_row(const MxProduct &a, int e)
 {
-    if (e <= 0) return 0;
-    if (e > a.E || !a.offsets) return a.M;
+    if (e > a.E || !a.offsets) return e <= 0 ? 0 : a.M;
     const int64_t o = a.offsets[e];
     return o < 0 ? 0 : o < a.M ? o : a.M;
 }
@@ -47,10 +46,11 @@ __device__ __forceinline__ int64_t first_row(const MxProduct &a, int e)
 // The work of a workgroup's row tile of TM rows: its rows, its expert, or nothing.
 // Numbered by tiles, expert e starts at number first_row(e) / TM + e, which leaves room for its last, broken tile;
 // with few rows a tile belongs to the row that it starts at.  Either way the expert is the last one whose number is
-// not above the tile's: 64 lanes look at 64 of them at a time.
+// not above the tile's: 64 lanes look at 64 of them at a time.  Tiles of the first expert start at row 0; those of its rows
+// that lie before `begin` are nobody's.
 struct RowTile {
     int e;
-    int64_t m0, end;
+    int64_t m0, begin, end;
 };
 template <int TM>
 __device__ __forceinline__ bool find_tile(const MxProduct &a, int64_t t, RowTile &r)
@@ -68,8 +68,9 @@ __device__ __forceinline__ bool find_tile(const MxProduct &a, int64_t t, RowTile
     const int f = (int)first_row(a, lo + lane);
     const int below = __builtin_amdgcn_readfirstlane(
         (int)__popcll(__ballot(lane > 0 && lo + lane <= hi && number((int64_t)f, lo + lane) <= t)));
-    const int64_t first = __builtin_amdgcn_readlane(f, below);
     r.e = lo + below;
+    r.begin = __builtin_amdgcn_readlane(f, below);
+    const int64_t first = r.e ? r.begin : 0;
     r.end = __builtin_amdgcn_readlane(f, below + 1);
     if (a.by_row) {
         if (t < first || (t - first) % TM) return false;
@@ -192,7 +193,7 @@ __global__ __launch_bounds__(64 * WAVES) void mx_direct_kernel(MxProduct a)
         m = r.m0 + row;
         end = r.end;
         if (e >= a.E) k1 = 0;
-        src = m >= end ? -1 : early ? source_of(a, m, slot) : source_row(a, m);
+        src = m < r.begin || m >= end ? -1 : early ? source_of(a, m, slot) : source_row(a, m);
     }
     float4v acc[CT];
 #pragma unroll
@@ -353,7 +354,7 @@ __global__ __launch_bounds__(256, MT* NT >= 64 ? 1 : 2) void mx_tile_kernel(MxPr
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, q = lane >> 4;
     const int64_t t = blockIdx.x / a.ntiles;
     const int n0 = (int)(blockIdx.x - t * a.ntiles) * S::TN;
-    int64_t m0, end;
+    int64_t m0, begin = 0, end;
     int e, k0 = 0, k1 = (int)(a.pitch / 4);
     if constexpr (OUTER) {
         const int64_t mt = (a.M + S::TM - 1) / S::TM;
@@ -370,6 +371,7 @@ __global__ __launch_bounds__(256, MT* NT >= 64 ? 1 : 2) void mx_tile_kernel(MxPr
         if (!find_tile<S::TM>(a, t, tile)) return;
         e = tile.e;
         m0 = tile.m0;
+        begin = tile.begin;
         end = tile.end;
         if (e >= a.E) k1 = 0;
     }
@@ -384,7 +386,7 @@ __global__ __launch_bounds__(256, MT* NT >= 64 ? 1 : 2) void mx_tile_kernel(MxPr
     // rows of A, -1 where an output row has none
     for (int row = tid; row < S::TM; row += 256) {
         const int64_t m = m0 + row;
-        source[row] = (int)(m >= end ? -1 : OUTER ? m : source_row(a, m));
+        source[row] = (int)(m < begin || m >= end ? -1 : OUTER ? m : source_row(a, m));
     }
     __syncthreads();
     if (steps > 0) {

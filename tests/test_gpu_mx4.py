@@ -396,3 +396,39 @@ def test_sums_over_very_many_rows():
     got = ftk.mx4_outer(ftk.mx4_quantize(A, transpose=True), ftk.mx4_quantize(B, transpose=True), r)
     assert got[0].tolist() == [[2.0 ** 25, 2.0], [3.0, 6.0], [2.0 ** 15, 0.0]]
     assert got[1].tolist() == [[384.0, -4.0], [2.0, -8.0], [1.0, 0.0]]
+
+
+@pytest.mark.parametrize("M,D,F,offsets,dtype", [
+    (1, 40, 20, [1, 1], "f32"), (5, 100, 33, [3, 4, 5], "bf16"), (16, 640, 129, [1, 9, 9, 12], "f16"), (16, 64, 40, [16, 16], "f32"),
+    (40, 64, 40, list(range(5, 105)), "bf16"), (200, 1000, 333, [70, 130, 131, 190], "f32"), (3000, 512, 768, [129, 2000, 2000, 2900], "bf16"),
+    (300, 130, 64, [300, 300, 300], "f32"), (20000, 384, 2100, [1000, 9000, 19999], "bf16"), (12000, 1100, 4096, [255, 12000], "f16")])
+def test_rows_before_the_first_expert_are_zero(M, D, F, offsets, dtype):
+    """Offsets that begin above 0: the rows in front belong to no expert, as those behind the last, whatever the first one's matrix holds."""
+    print("first offset", M, D, F, dtype, flush=True)
+    g = torch.Generator(device=DEV).manual_seed(M)
+    E = len(offsets) - 1
+    X = torch.randn(M, D, generator=g, device=DEV).to(DTYPES[dtype])
+    B = torch.randn(E * F, D, generator=g, device=DEV)
+    B[3, 7] = float("nan")  # of the first expert
+    W = ftk.mx4_quantize(B)
+    off = torch.tensor(offsets, dtype=torch.int32, device=DEV)
+    order = torch.randint(-1, 2 * M, (M,), generator=g, device=DEV).int()
+    r = ftk.Route(off, off[:E], order, torch.zeros(M, 2, dtype=torch.int32, device=DEV), 1)
+    x, w = ftk.mx4_dequantize(ftk.mx4_quantize(X)).double(), ftk.mx4_dequantize(W).double().view(E, F, D)
+    for gather in (False, True):
+        source = torch.where(order < 0, -1, order // 2).long() if gather else torch.arange(M, device=DEV)
+        rows = torch.where((source >= 0).unsqueeze(1), x[source.clamp(min=0)], 0)
+        want, size = torch.zeros(M, F, dtype=torch.float64, device=DEV), torch.zeros(M, F, dtype=torch.float64, device=DEV)
+        for e in range(E):
+            p, m = slice(min(offsets[e], M), min(offsets[e + 1], M)), w[e].t().contiguous()
+            want[p], size[p] = rows[p] @ m, rows[p].abs() @ m.abs()
+        empty = source < 0
+        empty[:offsets[0]] = True
+        empty[min(offsets[E], M):] = True
+        want[empty], size[empty] = 0, 0  # (also where zeros met NaN)
+        nan = torch.isnan(want)
+        bound = UNIT[dtype] * want.abs() + (-(-D // 128) + 8) * 2.0 ** -23 * size + STEP[dtype]
+        for out in (ftk.mx4_linear(X, W, r, gather=gather), ftk.mx4_matmul(ftk.mx4_quantize(X), W, r, gather=gather, out_dtype=DTYPES[dtype])):
+            assert (out[empty] == 0).all()
+            assert torch.equal(torch.isnan(out), nan)
+            assert ((out.double() - want).abs() <= bound)[~nan].all()
