@@ -19,7 +19,9 @@ from . import binding as ftk
 class RoutedExperts:
     """out[t] = sum over the slots (t, j) of g[t, j] * W[label[t, j]] x[t] with W packed to 4 bits.
 
-    weights: [K + 1, F, D]: one matrix a cluster, the last one shared.  Packed once for either direction."""
+    weights: [K + 1, F, D]: one matrix a cluster, the last one shared.  Packed once for either direction.
+    width: squared distance at which a cluster's weight has fallen to 1 / e; without one the mean squared distance of the centroids
+    from their own mean.  It belongs to the layer: what a token gets does not depend on its batch."""
 
     def __init__(self, weights, centroids, width=None):
         E, F, D = weights.shape
@@ -27,20 +29,30 @@ class RoutedExperts:
             raise ValueError("need a matrix for each of the %d centroids and a shared one, got %d" % (centroids.shape[0], E))
         self.E, self.F, self.D = E, F, D
         self.centroids = centroids.float().contiguous()
-        self.width = width  # squared distance at which a cluster's weight has fallen to a third; None: that of the batch
+        if width is None:
+            width = self._width((self.centroids - self.centroids.mean(0)).square().sum(1), self.centroids)
+        if not width > 0:
+            raise ValueError("width must be above 0, got %s" % width)
+        self.width = float(width)
         self.W = ftk.mx4_quantize(weights.reshape(E * F, D))
         self.WT = ftk.mx4_quantize(weights.transpose(1, 2).reshape(E * D, F))
 
     @classmethod
     def fitted(cls, weights, samples, iters=10, seed=0):
-        """The centroids from a Lloyd fit over sample rows."""
-        fit = ftk.kmeans_fit(samples.float().contiguous(), weights.shape[0] - 1, iters, seed=seed, want_inertia=False)
-        return cls(weights, fit["C"])
+        """The centroids from a Lloyd fit over sample rows, the width their mean squared distance from them."""
+        samples = samples.float().contiguous()
+        C = ftk.kmeans_fit(samples, weights.shape[0] - 1, iters, seed=seed, want_inertia=False)["C"]
+        return cls(weights, C, cls._width(ftk.kmeans_assign(samples, C)[1], C))
+
+    @staticmethod
+    def _width(dist, centroids):
+        """Mean of squared distances, at least about what 32 bits resolve beside rows as long as the centroids."""
+        return max(float(dist.mean()), float(centroids.square().sum(1).mean()) * 2.0 ** -20, torch.finfo(torch.float32).tiny)
 
     def gate(self, x):
         """labels int32 [N, 2] and weights float [N, 2]."""
         nearest, dist = ftk.kmeans_assign(x.float().contiguous(), self.centroids)
-        near = torch.exp(-dist / (dist.mean() if self.width is None else self.width))
+        near = torch.exp(-dist / self.width)
         labels = torch.stack([nearest, torch.full_like(nearest, self.E - 1)], 1)
         return labels, torch.stack([near, 1 - near], 1)
 

@@ -68,3 +68,40 @@ def test_fitted_router_and_refusals():
         RoutedExperts(weights, x[:7])
     assert ftk.mx4_dequantize(layer.W).shape == (80, 32)
     assert DEV.type == "cuda"
+
+
+def test_gate_on_the_centroids():
+    """Tokens that all lie on their centroids: their weight is 1, not 0 / 0."""
+    centres = dev(np.arange(24).reshape(3, 8) % 7 * 3.0).float()
+    weights = dev(np.random.default_rng(3).standard_normal((4, 16, 8))).float()
+    x = centres[torch.tensor([0, 2, 2, 1], device=DEV)]
+    for layer in (RoutedExperts(weights, centres), RoutedExperts(weights, centres, width=4.0), RoutedExperts.fitted(weights, centres, iters=2),
+                  RoutedExperts(weights[:2], torch.zeros(1, 8, device=DEV))):
+        y = x if layer.E == 4 else torch.zeros(4, 8, device=DEV)
+        labels, gates = layer.gate(y)
+        assert torch.equal(gates, torch.tensor([[1.0, 0.0]] * 4, device=DEV))
+        assert torch.isfinite(layer.forward(y)[0]).all()
+
+
+def test_gate_of_a_token_does_not_depend_on_its_batch():
+    """Small whole numbers, whose distances are exact in 32 bits: exp(-distance / width), in a batch and alone."""
+    rng = np.random.default_rng(8)
+    K, N, D = 5, 60, 64
+    centres = rng.integers(-4, 5, (K, D)).astype(np.float32)
+    x = centres[rng.integers(0, K, N)] + rng.integers(-1, 2, (N, D)).astype(np.float32) * (np.arange(N)[:, None] % 3)
+    weights = dev(rng.standard_normal((K + 1, 24, D))).float()
+    nearest = ((x[:, None].astype(np.float64) - centres) ** 2).sum(2).min(1)
+    for layer in (RoutedExperts(weights, dev(centres)), RoutedExperts(weights, dev(centres), width=50.0)):
+        labels, gates = layer.gate(dev(x))
+        want = np.exp(-nearest / layer.width)
+        # one rounding of the quotient (2^-24 of at most 104, beyond which the weight is 0) and of the exponential
+        assert np.abs(f64(gates) - np.stack([want, 1 - want], 1)).max() <= 104 * 2.0 ** -23
+        for t in range(0, N, 7):
+            one = layer.gate(dev(x[t:t + 1]))
+            assert torch.equal(one[0], labels[t:t + 1]) and torch.equal(one[1], gates[t:t + 1])
+    fitted = RoutedExperts.fitted(weights, dev(x), iters=4)
+    spread = ((x[:, None].astype(np.float64) - f64(fitted.centroids)) ** 2).sum(2).min(1).mean()
+    assert abs(fitted.width - spread) <= 1e-4 * spread
+    for width in (0.0, -1.0, float("nan")):
+        with pytest.raises(ValueError):
+            RoutedExperts(weights, dev(centres), width=width)
