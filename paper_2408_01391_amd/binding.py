@@ -2,7 +2,8 @@
 
 PyTorch provides device memory and the current stream; every step of the hot path runs
 inside the HIP library.  There is no CPU fallback: if the library is missing or a call
-fails, an exception is raised.
+fails, an exception is raised.  The calls compute values: torch records nothing of them, and results come without
+``requires_grad`` whatever the operands' is (gradients are calls of their own).
 """
 from __future__ import annotations
 

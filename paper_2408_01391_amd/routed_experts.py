@@ -66,8 +66,9 @@ class RoutedExperts:
         return ftk.route_combine(y, route, gates), (x, y, route, gates) if training else None
 
     def backward(self, dout, saved):
-        """Gradients (dx [N, D], dgates [N, 2], dweights [E, F, D] in 32 bits) of sum(dout * out); rounding to 4 bits counts as
-        the identity."""
+        """Gradients (dx [N, D], dgates [N, 2], dweights [E, F, D] in 32 bits) of sum(dout * out) with labels and gates held fixed;
+        rounding to 4 bits counts as the identity.  Where the gates depend on x, as those of gate() do, what reaches x through
+        them is not in dx: it is dgates through whatever made them."""
         x, y, route, gates = saved
         dy, dgates = ftk.route_combine_grad(dout, y, route, gates)
         dx = ftk.route_combine(ftk.mx4_linear(dy, self.WT, route=route), route)

@@ -105,3 +105,24 @@ def test_gate_of_a_token_does_not_depend_on_its_batch():
     for width in (0.0, -1.0, float("nan")):
         with pytest.raises(ValueError):
             RoutedExperts(weights, dev(centres), width=width)
+
+
+def test_backward_holds_the_gates_fixed():
+    """The layer's own gates give the same gradients as the same gates given, and dgates is what the gates' own gradient starts from:
+    moving them moves sum(dout * out) by that much, the sum being linear in them."""
+    rng = np.random.default_rng(12)
+    N, D, F, K = 90, 64, 48, 4
+    centres = dev(rng.standard_normal((K, D)) * 2).float()
+    layer = RoutedExperts(dev(rng.standard_normal((K + 1, F, D)) * 0.1).float(), centres)
+    x = centres[dev(rng.integers(0, K, N))] + dev(rng.standard_normal((N, D)) * 0.3).float()
+    dout = dev(rng.standard_normal((N, F))).float()
+    labels, gates = layer.gate(x)
+    out, saved = layer.forward(x, training=True)
+    own, given = layer.backward(dout, saved), layer.backward(dout, layer.forward(x, labels, gates, training=True)[1])
+    for a, b in zip(own, given):
+        assert torch.equal(a, b) and not a.requires_grad
+    step = dev(rng.standard_normal((N, 2)) * 0.5).float()
+    moved = layer.forward(x, labels, gates + step)[0]
+    by = (f64(dout) * (f64(moved) - f64(out))).sum()
+    want, size = (f64(own[1]) * f64(step)).sum(), (np.abs(f64(dout)) @ np.abs(f64(moved)).T).max() * N
+    assert abs(by - want) <= 1e-5 * size
