@@ -295,11 +295,11 @@ static ftk_status launch_direct(MxProduct a, hipStream_t st)
 // Copies as to_lds16 (ftk_mma.h), to an LDS address; the second from a common base and 32-bit offsets of the lanes.
 __device__ __forceinline__ void to_lds16_at(const uint8_t *g, uint32_t at)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(g) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(g) : "memory", "m0");
 }
 __device__ __forceinline__ void to_lds16_from(const uint8_t *base, uint32_t offset, uint32_t at)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(base) : "memory", "m0");
 }
 
 // Pieces of a line by their places before the key, and the reverse: those of a stage's first step (even ones) come first.
