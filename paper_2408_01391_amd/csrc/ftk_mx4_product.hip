@@ -533,15 +533,16 @@ __global__ __launch_bounds__(256, MT* NT >= 64 ? 1 : 2) void mx_tile_kernel(MxPr
         for (; st < whole; ++st) stage(Zero{}, st);
         if (steps & 1) {  // half a stage: blocks 0 to 3 of the line
             const int at = (whole & 1) * S::STAGE + (place_of_piece(q) ^ key) * 16, sat = scale_at(whole) + q;
+            // (one scale a lane: a byte, at any address)
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
                 read_b(at, j, 0);
-                read_xb(sat, j, 0);
+                xb[0][j] = sb[sat + (j >> 1) * 32 * 16 + (j & 1) * 4 * 16];
             }
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
                 read_a(at, i);
-                read_xa(sat, i);
+                xa[i] = sa[sat + i * 16 * 16];
             }
 #pragma unroll
             for (int i = 0; i < MT; ++i)
