@@ -352,10 +352,9 @@ ftk_status check_device()
     return FTK_OK;
 }
 
-ftk_status allow_lds(const void *kernel, size_t bytes)
+ftk_status set_lds_limit(const void *kernel, int bytes)
 {
-    if (bytes > 65536)
-        FTK_TRY_HIP(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    FTK_TRY_HIP(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
     return FTK_OK;
 }
 

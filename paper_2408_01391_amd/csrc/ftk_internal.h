@@ -28,8 +28,14 @@ ftk_status hip_failed(hipError_t e, const char *what);
 ftk_status check_ptr(const void *p, size_t align, const char *name);
 ftk_status check_workspace(void *ws, size_t bytes, size_t need);
 ftk_status check_device();
-// lets a kernel have more than 64 KB of dynamic LDS on the current device
-ftk_status allow_lds(const void *kernel, size_t bytes);
+// Lets a kernel have up to BYTES of dynamic LDS on the current device.  The limit is the process's, not the call's: were it set to
+// what a call needs, another thread could lower it before the launch, so it is the most that any call of the kernel takes.
+ftk_status set_lds_limit(const void *kernel, int bytes);
+template <size_t BYTES>
+ftk_status allow_lds(const void *kernel)
+{
+    return BYTES > 65536 ? set_lds_limit(kernel, (int)BYTES) : FTK_OK;
+}
 
 static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }

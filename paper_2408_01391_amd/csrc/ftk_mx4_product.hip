@@ -591,7 +591,7 @@ static ftk_status launch_tile(MxProduct a, hipStream_t st)
         set_error("too many tiles: M=%lld F=%d E=%d", (long long)a.M, a.F, a.E);
         return FTK_EINVAL;
     }
-    FTK_TRY(allow_lds((const void *)mx_tile_kernel<MT, NT, Out, OUTER>, S::LDS));
+    FTK_TRY(allow_lds<S::LDS>((const void *)mx_tile_kernel<MT, NT, Out, OUTER>));
     mx_tile_kernel<MT, NT, Out, OUTER><<<(unsigned)(mtiles * a.ntiles), 256, S::LDS, st>>>(a);
     FTK_TRY_HIP(hipGetLastError());
     return FTK_OK;

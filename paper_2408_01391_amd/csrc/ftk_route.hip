@@ -582,7 +582,7 @@ static PlaceArgs place_args(const RoutePlan &p, const int32_t *labels, int E, in
 static ftk_status launch_plan(const RoutePlan &p, PlaceArgs a, void *ws, hipStream_t st)
 {
     const size_t lds = (size_t)ROUTE_WAVES * a.E * 4;
-    FTK_TRY(allow_lds((const void *)route_place_kernel, lds));
+    if (lds > 65536) FTK_TRY(allow_lds<ROUTE_WAVES * ROUTE_MAX_EXPERTS * 4>((const void *)route_place_kernel));
     if (p.chunks > 1) {
         int32_t *totals = (int32_t *)ws, *table = totals + a.E;
         route_count_kernel<<<p.chunks, ROUTE_THREADS, (size_t)a.E * 4, st>>>(a.labels, p.S, p.chunk, a.E, table);

@@ -432,3 +432,40 @@ def test_rows_before_the_first_expert_are_zero(M, D, F, offsets, dtype):
             assert (out[empty] == 0).all()
             assert torch.equal(torch.isnan(out), nan)
             assert ((out.double() - want).abs() <= bound)[~nan].all()
+
+
+@pytest.mark.parametrize("N,F,D", [(20000, 2100, 384), (6000, 768, 512), (1500, 2048, 2048)])
+def test_large_tiles_in_a_graph(N, F, D):
+    """Products and sums over rows in tiles that take more than 64 KB of LDS, and the packing before them."""
+    g = torch.Generator(device=DEV).manual_seed(N)
+    E = 3
+    X = torch.randn(N, D, generator=g, device=DEV).bfloat16()
+    W = ftk.mx4_quantize(torch.randn(E * F, D, generator=g, device=DEV))
+    r = ftk.route_plan(dev(labels_of(np.random.default_rng(N), N, 1, E, "skew")), E, 128)
+    ws = torch.empty(ftk.mx4_workspace_bytes(N, D, r.rows, E) + 256, dtype=torch.uint8, device=DEV)
+    A = ftk.route_gather(X, r)
+    qy, qa = ftk.mx4_quantize(ftk.mx4_linear(X, W, r, gather=True), transpose=True), ftk.mx4_quantize(A, transpose=True)
+    out = torch.empty(r.rows, F, dtype=X.dtype, device=DEV)
+    sums = torch.empty(E, F, D, device=DEV)
+
+    def step():
+        ftk.mx4_linear(X, W, r, gather=True, out=out, workspace=ws)
+        ftk.route_gather(X, r, out=A)
+        ftk.mx4_quantize(out, transpose=True, out=qy)
+        ftk.mx4_quantize(A, transpose=True, out=qa)
+        ftk.mx4_outer(qy, qa, r, out=sums)
+
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(3):
+        X.mul_(-0.6)
+        step()
+        want = out.clone(), sums.clone()
+        out.fill_(7), sums.fill_(7)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(sums, want[1])
+        assert torch.isfinite(sums).all() and sums.abs().max() > 0

@@ -300,3 +300,49 @@ def test_on_another_stream_and_in_a_graph():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(r2.pos, r.pos)
+
+
+def test_plans_of_many_experts_from_two_threads():
+    """Calls that need different amounts of more than 64 KB of LDS, under way in two threads at once."""
+    import threading
+    rng = np.random.default_rng(31)
+    N, wrong = 3000, []
+
+    def work(E):
+        labels = labels_of(rng, N, 1, E, "even")
+        want = plan_of(labels, E, 1, N)
+        labels = dev(labels)
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(40):
+                try:
+                    check_plan(ftk.route_plan(labels, E), want)
+                except Exception as e:  # (an assertion in a thread would be lost)
+                    wrong.append((E, repr(e)))
+
+    dev(np.zeros(1))
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=work, args=(E,)) for E in (8192, 4200)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong, wrong[:3]
+
+
+def test_plan_of_many_experts_in_a_graph():
+    rng = np.random.default_rng(32)
+    N, E = 5000, 8000
+    labels = dev(labels_of(rng, N, 2, E, "skew"))
+    r = ftk.route_plan(labels, E)
+    ws = torch.empty(ftk.route_workspace_bytes(N, 2, E) + 256, dtype=torch.uint8, device=DEV)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        ftk.route_plan(labels, E, route=r, workspace=ws)
+    for seed in range(3):
+        labels.copy_(dev(labels_of(np.random.default_rng(seed), N, 2, E, "skew")))
+        want = ftk.route_plan(labels, E)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for name in ("offsets", "counts", "order", "pos"):
+            assert torch.equal(getattr(r, name), getattr(want, name)), name
