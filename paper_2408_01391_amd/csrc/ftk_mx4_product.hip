@@ -83,7 +83,7 @@ __device__ __forceinline__ bool find_tile(const MxProduct &a, int64_t t, RowTile
 
 // The expert with the i-th most rows, among up to 64 (else expert i).  Sums over rows take as long as an expert has rows, and
 // workgroups start in order: the long ones first, so that none is left over (8 experts of 1400 to 8000 rows, 4096 x 2048
-// sums each, with the packing and the rows' gradients 582 us, in the experts' own order 615).
+// sums each, with the packing and the rows' gradients 582 us, in the experts' own order 611).
 __device__ __forceinline__ int by_size(const MxProduct &a, int i)
 {
     if (!a.offsets || a.E > 64) return i;
@@ -158,9 +158,10 @@ __device__ __forceinline__ void mx_sums_done(float4v (&c)[MT][NT])
 // Few rows: 16 output rows by 16 * CT columns a workgroup, whose WAVES waves share the steps of 128 elements out between
 // them, a run each, and add their sums up in LDS.  Operands go from memory straight to registers, UNROLL steps
 // at a time, all requested before the first is used: with one row the weights' way from memory is all the time there
-// is.  A dense row is packed on the way, the whole block of 32 within a lane.  (One token, two matrices of 4096 x 4096: 17.8 MB in 9.6 us
-// with 32 columns and 8 waves a workgroup, 1.9 TB/s behind three dependent requests - offsets, rows or weights, and the launch;
-// 16 columns 11.2, 64 columns 13.0, 16 waves 9.5.)
+// is.  A dense row is packed on the way, the whole block of 32 within a lane.  (One token, two matrices of 4096 x 4096: 17.8 MB in 9.6
+// to 9.9 us with 32 columns and 8 waves a workgroup, 1.8 TB/s, of which the bytes alone would take 3.5; how much of the rest is
+// the launch, the requests that wait for offsets and order, and the packing has not been told apart.  16 columns 11.2, 64
+// columns 13.0, 16 waves 9.5.)
 template <typename Src, typename Out, int CT, int WAVES, bool OUTER>
 __global__ __launch_bounds__(64 * WAVES) void mx_direct_kernel(MxProduct a)
 {
@@ -324,13 +325,13 @@ __device__ __forceinline__ const uint8_t *uniform(const uint8_t *p)
 // LDS rows are lines of eight 16-byte pieces.  Those that a stage's first step reads come first, and a row's key, half the
 // lane row that reads the line, is xored into the place.  Measured at the large case below, summed over the chip: 9.4e6
 // LDS cycles are lost to bank conflicts beside 2.3e7 of access; with the pieces in their own order it was 2.8e7, and the
-// call took 392 us in place of 386.  The copy keeps the order of its lanes, so it is the lanes' addresses that are
+// call took 392 us in place of 386 (one run).  The copy keeps the order of its lanes, so it is the lanes' addresses that are
 // permuted, within a line.
 // Column tile j of a wave has, for lane row r, column 32 * (j / 2) + 8 * (r / 4) + 4 * (j % 2) + r % 4: two
 // tiles together give a lane eight consecutive columns to store.
 //
 // 256 x 256 sums a workgroup (MT = NT = 8), one workgroup a compute unit: 16384 x 2 rows through 16 matrices of 4096 x 4096 in
-// 340 to 355 us, 3.1 to 3.2 PFLOP/s; the matrix instructions alone would take 160 at the rate that power leaves them on
+// 340 to 365 us by the box, 3.0 to 3.2 PFLOP/s; the matrix instructions alone would take 160 at the rate that power leaves them on
 // such data (6.9 PFLOP/s; 9 on zeros).  The rest: copies 90, of which scales 32, writing the results 55, LDS reads 35; they
 // do not hide behind the products, for a wave has its SIMD to itself and issues in order.  Two waves a SIMD (wave tiles of
 // 128 x 64) took 9 % longer, two workgroups of 256 x 128 12 %, copies four steps of 64-byte lines ahead 5 %, workgroups
@@ -598,9 +599,9 @@ static ftk_status launch_tile(MxProduct a, hipStream_t st)
 }
 
 // What the tiles of a kernel take, in about a microsecond: so many of them run at once, one starts and ends in `ends` and
-// takes `stage` for 256 elements.  (Measured: 16384 x 2 rows, 16 matrices of 4096 x 4096 in tiles of 256 / 128 rows and columns 355 / 445 us;
-// 4096 x 2 rows, 8 matrices 121 / 121, of 64 166; 1024 x 2 rows 48 / 49 / 54; 256 x 2 rows 42 / 28 / 25; of 512 x 512, 64 matrices,
-// 16384 x 2 rows 35 / 30 / 33.)
+// takes `stage` for 256 elements.  (Whole calls with the packing, in tiles of 256 / 128 / 64 rows and columns: 16384 x 2 rows, 16 matrices
+// of 4096 x 4096 393 / 439 / 608 us; 4096 x 2 rows, 8 matrices 125 / 124 / 166; 1024 x 2 rows 45 / 46 / 51; 256 x 2 rows 39 / 25 / 22; 64
+// matrices of 512 x 512, 16384 x 2 rows 34 / 29 / 31.)
 static double tile_cost(const MxProduct &a, bool outer, int side, int at_once, double ends, double stage)
 {
     // half of the experts with rows leave a broken tile more
@@ -621,8 +622,8 @@ static ftk_status launch_packed(const MxProduct &a, hipStream_t st)
 }
 
 // Whether dense rows are packed by every workgroup that needs them rather than once beforehand, in a launch of its own.  (Whole call,
-// matrices of 4096 x 4096, with / without: 2 rows 12.2 / 16.8 us, 8 rows of 8 experts 16.5 / 16.7, 16 rows 23.3 / 17.1, of one expert
-// 12.3 / 16.8.)
+// matrices of 4096 x 4096, with / without: 2 rows 12.8 / 17.5 us, 8 rows of 8 experts 18.1 / 17.8, 16 rows 25.1 / 17.6, of 4 experts 16.1 /
+// 17.5, of 2 12.9 / 17.5; 32 rows of 8 29.8 / 17.5.)
 static bool few_rows(int64_t M, int E) { return M <= 8 || (M <= 16 && E <= 4); }
 
 static size_t packed_bytes(int64_t N, int D, size_t *codes)
