@@ -47,7 +47,7 @@ typedef enum {
     FTK_EUNCORRECTABLE = 5 /* reserved: never returned; see ftk_ft_stats.uncorrectable   */
 } ftk_status;
 
-/* FTK_BF16 and FTK_F16 are taken by the ftk_route_* and ftk_mx4_* calls alone. */
+/* FTK_BF16 and FTK_F16 are taken by the ftk_route_*, ftk_mx4_*, ftk_xent* and ftk_adamw_* calls alone. */
 typedef enum { FTK_F32 = 0, FTK_F64 = 1, FTK_BF16 = 2, FTK_F16 = 3 } ftk_dtype;
 
 /* Fault-tolerance mode of the contraction (Section 4).
@@ -433,6 +433,102 @@ int64_t ftk_mx4_workspace_bytes(int64_t N, int32_t D, int64_t M, int32_t E); /* 
 ftk_status ftk_mx4_outer(ftk_dtype out_dtype, const void *a_codes, const void *a_scales, const void *b_codes,
                          const void *b_scales, int64_t rows, int32_t F, int32_t D, int32_t E,
                          const int32_t *offsets /* nullable */, void *out, void *hip_stream);
+
+/* ---- a gate that learns ------------------------------------------------------------------------
+ * Which k of E experts each of N rows goes to, from logits [N x E] (FTK_F32, FTK_BF16 or FTK_F16, row stride ldz):
+ *   p = softmax of a row; labels [N x k]: its k largest logits in descending order, equal ones in ascending index;
+ *   weights [N x k]: p of them, or with normalise != 0 the softmax over them alone; lse [N]: log of the sum of exponentials.
+ * and how evenly the rows use the experts:
+ *   counts [E + 1] : slots of every expert, and behind them T, the rows that took part
+ *   probs [E]      : mean of p over those rows
+ *   loss [1]       : E * sum_e counts[e] / (k T) * probs[e], 1 where all are used alike; 0 where T is.
+ * An expert whose logit is -infinity is closed to the row: it is never chosen, and slots that find no expert get the label -1
+ * (a dropped slot of ftk_route_plan) and the weight 0.  A row closed to all takes no part: lse -infinity.  A row with
+ * a NaN or +infinity gets labels -1 and NaN weights, and makes probs and loss NaN.
+ * Sums are held in 32 bits or more, in an order that N, E, k and dtype set: results are bitwise reproducible.
+ * workspace: ftk_route_gate_workspace_bytes(N, E); up to FTK_ROUTE_GATE_FEW rows none is needed: NULL will do.
+ * Limits: 1 <= E <= 8192, 1 <= k <= 64, k <= E, N * k < 2^31.  N = 0 is a valid call (T = 0). */
+#define FTK_ROUTE_GATE_FEW 64
+size_t ftk_route_gate_workspace_bytes(int64_t N, int32_t E); /* 0: bad arguments */
+ftk_status ftk_route_gate(ftk_dtype dtype, const void *logits, int64_t ldz, int64_t N, int32_t E, int32_t k, int32_t normalise,
+                          int32_t *labels, float *weights, float *lse, int32_t *counts, float *probs, float *loss,
+                          void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* dlogits [N x E] (type of the logits; may be the logits themselves) = gradient of sum(dweights * weights) + dloss * loss, labels and
+ * counts held fixed.  dweights [N x k] or dloss [1] (device) may be NULL.  labels, weights, lse and counts as ftk_route_gate left
+ * them (counts may have been summed over several calls, or processes, with equal E and k: the loss is then that of all their
+ * rows). */
+ftk_status ftk_route_gate_grad(ftk_dtype dtype, const void *logits, int64_t ldz, int64_t N, int32_t E, int32_t k,
+                               int32_t normalise, const int32_t *labels, const float *weights, const float *lse,
+                               const int32_t *counts, const float *dweights /* nullable */, const float *dloss /* nullable */,
+                               void *dlogits, int64_t ldd, void *hip_stream);
+
+/* ---- softmax cross entropy over many classes ------------------------------------------------------
+ * Rows against the classes' vectors, the soft counterpart of the assignment: with bias_v = -||w_v||^2 / 2 a logit is the
+ * assignment's score (Section 3.1.2) of a centroid.  The logits [N x V] are not kept.
+ *   z_nv = scale * <x_n, w_v> + bias_v;   lse_n = log sum_v exp z_nv;   loss_n = lse_n - z_n,label_n
+ *   X [N x D], W [V x D] of `dtype` (FTK_F32, FTK_BF16 or FTK_F16), row strides ldx and ldw; bias [V] or NULL: 0
+ *   labels [N]: a row whose label lies outside [0, V) is ignored: nothing of it is looked at, loss and lse are 0
+ *   loss, lse [N]
+ * Logits and sums are held in 32 bits; FTK_F32 operands are taken to 24 bits.  A bias of -infinity closes a class of finite
+ * w.  A row all of whose logits are -infinity has lse -infinity, a NaN loss and no gradient; a NaN or +infinity among its
+ * logits makes a row's loss, lse and gradients NaN.  Results are bitwise reproducible.
+ * workspace: ftk_xent_workspace_bytes(dtype, N, V, D, grad); it grows with N * D, never with N * V beyond 128 MB, or 128 MB of
+ * W laid out anew (rows whose address, stride or length is no multiple of 16 bytes, and FTK_F32).
+ * Limits: N, V < 2^31, D <= 2^20. */
+int64_t ftk_xent_workspace_bytes(ftk_dtype dtype, int64_t N, int64_t V, int32_t D, int32_t grad); /* -1: bad arguments */
+ftk_status ftk_xent(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N, const void *W, int64_t ldw, int64_t V, int32_t D,
+                    const float *bias /* nullable */, double scale, const int32_t *labels, float *loss, float *lse,
+                    void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Gradients of sum(dloss * loss), d_nv = dloss_n (exp(z_nv - lse_n) - [v = label_n]), zero for ignored rows:
+ *   dX = scale * d W [N x D], dW = scale * d^T X [V x D] (type of the rows), dbias_v = sum_n d_nv [V]; each may be NULL.
+ * lse as ftk_xent left it.  d is rounded to the rows' type (FTK_F32: not at all) before the products; every gradient is written
+ * once, in whole, and must not overlap an input. */
+ftk_status ftk_xent_grad(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N, const void *W, int64_t ldw, int64_t V, int32_t D,
+                         const float *bias /* nullable */, double scale, const int32_t *labels, const float *lse,
+                         const float *dloss, void *dX /* nullable */, int64_t lddx, void *dW /* nullable */, int64_t lddw,
+                         float *dbias /* nullable */, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* ---- many weights updated at once ----------------------------------------------------------------
+ * One AdamW step over a list of tensors, in place, one pass over each:
+ *   g = grad_scale * grad;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2      (32 bits, every operation rounded)
+ *   w = w - lr lr_scale (weight_decay w + m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps))
+ * param: FTK_F32, FTK_BF16 or FTK_F16 (`dtype`); grad: FTK_F32 or the weights' type, for weights in 32 bits any of the three.
+ * master: 32-bit weights beside 16-bit ones, which become the masters rounded; all tensors of a call have them or none has.
+ *   Without them updates smaller than half a step of a 16-bit weight are lost.
+ * state_bits 32: m and v are floats.
+ * state_bits 8: m, v [count] codes and m_scales, v_scales [ceil(count / 32)].  32 consecutive elements share a power of
+ *   two 2^b, held as the byte b + 127.  A code is exponent e (4 bits) over mantissa f (M bits: 3 for m, under a sign; 4 for v) and
+ *   stands for f * 2^b where e = 0, else (2^M + f) * 2^(e - 1) * 2^b.  b is the least (>= -127) for which none of the block
+ *   can be rounded out of range.  Numbers are rounded to one of their neighbours at random, the nearer one more often, so
+ *   that the expected value is the number (rounded to the nearest, a state that changes by less than half a step would
+ *   stay for ever); a positive v is never rounded to 0.  The random bits are a function of (seed, step, place in the
+ *   list, element): a step is bitwise reproducible.  A block with an infinity or NaN gets the byte 255 and stands for 32 NaN.
+ *   All zeros is the start of both kinds of state.
+ * Tensors: any alignment of their element type, contiguous, apart from each other.  A tensor without grad (NULL), or of no
+ * elements, is left as it is.  count <= 2^37.  Nothing is kept of the list: it may change from call to call. */
+typedef struct {
+    void *param;
+    const void *grad;
+    void *m, *v;
+    uint8_t *m_scales, *v_scales; /* state_bits 8 */
+    float *master;                /* nullable */
+    int64_t count;
+} ftk_adamw_tensor;
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;
+    const float *lr_scale, *grad_scale; /* device scalars, may be NULL: 1 */
+    const int64_t *step;                /* device scalar: number of this step, 1 for the first (counted by the caller) */
+    uint64_t seed;
+} ftk_adamw_options;
+ftk_status ftk_adamw_step(ftk_dtype dtype, ftk_dtype grad_dtype, int32_t state_bits, const ftk_adamw_tensor *tensors /* (host) */,
+                          int32_t n, const ftk_adamw_options *options /* (host) */, void *hip_stream);
+
+/* What 8-bit states stand for: m_out[i], v_out[i] [count] of `dtype`, rounded once (exact in FTK_F32 and FTK_BF16 but for the
+ * type's range).  Takes m, v, m_scales, v_scales and count of the list's tensors.  m_out, v_out: lists (host) of n pointers. */
+ftk_status ftk_adamw_moments(ftk_dtype dtype, const ftk_adamw_tensor *tensors /* (host) */, int32_t n, void *const *m_out /* (host) */,
+                             void *const *v_out /* (host) */, void *hip_stream);
 
 /* Profiling aid for benchmarks.  While enabled, every ftk_kmeans_assign call brackets its main
  * contraction kernel (not the small norm / refine kernels around it; on the scan path: the scan with

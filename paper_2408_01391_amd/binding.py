@@ -111,6 +111,22 @@ def load():
     L.ftk_mx4_workspace_bytes.restype = i64
     L.ftk_mx4_outer.argtypes = [i32, vp, vp, vp, vp, i64, i32, i32, i32, vp, vp, vp]
     L.ftk_mx4_outer.restype = i32
+    L.ftk_route_gate_workspace_bytes.argtypes = [i64, i32]
+    L.ftk_route_gate_workspace_bytes.restype = sz
+    L.ftk_route_gate.argtypes = [i32, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.ftk_route_gate.restype = i32
+    L.ftk_route_gate_grad.argtypes = [i32, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+    L.ftk_route_gate_grad.restype = i32
+    L.ftk_xent_workspace_bytes.argtypes = [i32, i64, i64, i32, i32]
+    L.ftk_xent_workspace_bytes.restype = i64
+    L.ftk_xent.argtypes = [i32, vp, i64, i64, vp, i64, i64, i32, vp, ctypes.c_double, vp, vp, vp, vp, sz, vp]
+    L.ftk_xent.restype = i32
+    L.ftk_xent_grad.argtypes = [i32, vp, i64, i64, vp, i64, i64, i32, vp, ctypes.c_double, vp, vp, vp, vp, i64, vp, i64, vp, vp, sz, vp]
+    L.ftk_xent_grad.restype = i32
+    L.ftk_adamw_step.argtypes = [i32, i32, i32, vp, i32, vp, vp]
+    L.ftk_adamw_step.restype = i32
+    L.ftk_adamw_moments.argtypes = [i32, vp, i32, vp, vp, vp]
+    L.ftk_adamw_moments.restype = i32
     L.ftk_last_error.restype = ctypes.c_char_p
     L.ftk_version.restype = ctypes.c_char_p
     _lib = L
@@ -122,6 +138,8 @@ EXPORTS = ("ftk_workspace_bytes", "ftk_assign_geometry", "ftk_plan_padded_rows",
            "ftk_route_rows", "ftk_route_workspace_bytes", "ftk_route_plan", "ftk_route_gather", "ftk_route_dispatch",
            "ftk_route_combine", "ftk_route_combine_grad", "ftk_mx4_quantize", "ftk_mx4_dequantize", "ftk_mx4_matmul",
            "ftk_mx4_linear", "ftk_mx4_workspace_bytes", "ftk_mx4_outer",
+           "ftk_route_gate_workspace_bytes", "ftk_route_gate", "ftk_route_gate_grad", "ftk_xent_workspace_bytes", "ftk_xent",
+           "ftk_xent_grad", "ftk_adamw_step", "ftk_adamw_moments",
            "ftk_profile_read", "ftk_tuning_override", "ftk_last_error", "ftk_version")
 
 
@@ -718,4 +736,262 @@ def mx4_outer(A, B, route=None, out=None, out_dtype=torch.float32):
     _check(load().ftk_mx4_outer(_row_code(out, "out", _MX_DTYPES), A.codes.data_ptr(), A.scales.data_ptr(),
                                 B.codes.data_ptr(), B.scales.data_ptr(), A.D, A.N, B.N, E,
                                 None if route is None else route.offsets.data_ptr(), out.data_ptr(), _stream()))
+    return out
+
+
+# ---- a gate that learns ----------------------------------------------------------------------
+
+GATE_FEW = 64  # rows that need no workspace
+
+
+class Gate:
+    """What a gate decided (device tensors): labels int32 and weights float [N, k], lse float [N]; counts int32 [E + 1] (slots of every
+    expert, then the rows that took part), probs float [E], loss float [1]."""
+
+    __slots__ = ("labels", "weights", "lse", "counts", "probs", "loss", "normalise")
+
+    def __init__(self, labels, weights, lse, counts, probs, loss, normalise):
+        self.labels, self.weights, self.lse = labels, weights, lse
+        self.counts, self.probs, self.loss, self.normalise = counts, probs, loss, normalise
+
+
+def _here(*tensors):
+    """All on the current device: calls are enqueued on its current stream."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError("a tensor lives on device %d, the current one is %d" % (t.get_device(), device))
+
+
+def _floats(t, name, *shape):
+    if not t.is_cuda or t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous float32 device tensor of shape %s" % (name, list(shape)))
+    return t
+
+
+def route_gate_workspace_bytes(N: int, E: int) -> int:
+    n = load().ftk_route_gate_workspace_bytes(N, E)
+    if n == 0:
+        raise FtkError(1, load().ftk_last_error().decode())
+    return n
+
+
+def route_gate(logits, k, normalise=True, gate=None, workspace=None):
+    """The k experts of every row of logits [N, E], their weights (probabilities; normalise: over the k alone), and how evenly the
+    rows use the experts.  Returns a Gate, whose labels route_plan and route_dispatch take."""
+    ld = _row_stride(logits, "logits")
+    N, E = logits.shape
+    code, dev = _row_code(logits, "logits", _MX_DTYPES), logits.device
+    if gate is None:
+        if not 1 <= k <= E:
+            raise ValueError("need 1 <= k <= %d experts, got %d" % (E, k))
+        ints = torch.empty(N * k + E + 1, dtype=torch.int32, device=dev)
+        labels, counts = ints.split_with_sizes((N * k, E + 1))
+        floats = torch.empty(N * k + N + E + 1, dtype=torch.float32, device=dev)
+        weights, lse, probs, loss = floats.split_with_sizes((N * k, N, E, 1))
+        gate = Gate(labels.view(N, k), weights.view(N, k), lse, counts, probs, loss, normalise)
+    else:
+        _index(gate.labels, "labels", N, k), _floats(gate.weights, "weights", N, k), _floats(gate.lse, "lse", N)
+        _index(gate.counts, "counts", E + 1), _floats(gate.probs, "probs", E), _floats(gate.loss, "loss", 1)
+        gate.normalise = normalise
+    _here(logits, gate.labels, workspace)
+    workspace, wp, wn = _workspace(workspace, route_gate_workspace_bytes(N, E) if N > GATE_FEW else 0, dev)
+    _check(load().ftk_route_gate(code, logits.data_ptr(), ld, N, E, k, 1 if normalise else 0, gate.labels.data_ptr(),
+                                 gate.weights.data_ptr(), gate.lse.data_ptr(), gate.counts.data_ptr(), gate.probs.data_ptr(),
+                                 gate.loss.data_ptr(), wp, wn, _stream()))
+    return gate
+
+
+def route_gate_grad(logits, gate, dweights=None, dloss=None, out=None):
+    """Gradient [N, E] of sum(dweights * gate.weights) + dloss * gate.loss; dweights float [N, k], dloss float [1], either may be None.
+    Labels and counts are held fixed.  out may be logits."""
+    ld = _row_stride(logits, "logits")
+    N, E = logits.shape
+    k = gate.labels.shape[1]
+    _index(gate.labels, "labels", N, k), _floats(gate.weights, "weights", N, k), _floats(gate.lse, "lse", N)
+    _index(gate.counts, "counts", E + 1)
+    if dweights is not None:
+        _floats(dweights, "dweights", N, k)
+    if dloss is not None:
+        _floats(dloss, "dloss", 1)
+    out, ldo = _new_rows(out, N, E, logits, "out")
+    _here(logits, gate.labels, dweights, dloss, out)
+    _check(load().ftk_route_gate_grad(_row_code(logits, "logits", _MX_DTYPES), logits.data_ptr(), ld, N, E, k,
+                                      1 if gate.normalise else 0, gate.labels.data_ptr(), gate.weights.data_ptr(),
+                                      gate.lse.data_ptr(), gate.counts.data_ptr(), _ptr(dweights), _ptr(dloss), out.data_ptr(), ldo,
+                                      _stream()))
+    return out
+
+
+# ---- softmax cross entropy over many classes -------------------------------------------------
+
+
+def xent_workspace_bytes(dtype_code: int, N: int, V: int, D: int, grad: bool) -> int:
+    n = load().ftk_xent_workspace_bytes(dtype_code, N, V, D, 1 if grad else 0)
+    if n < 0:
+        raise FtkError(1, load().ftk_last_error().decode())
+    return n
+
+
+def _xent_args(X, W, labels, bias):
+    ldx, ldw = _row_stride(X, "X"), _row_stride(W, "W")
+    N, D = X.shape
+    V = W.shape[0]
+    if W.shape[1] != D or W.dtype != X.dtype:
+        raise ValueError("X [N, D] and W [V, D] must share type and D")
+    _index(labels, "labels", N)
+    if bias is not None:
+        _floats(bias, "bias", V)
+    _here(X, W, labels, bias)
+    return _row_code(X, "X", _MX_DTYPES), ldx, ldw, N, V, D
+
+
+def xent(X, W, labels, bias=None, scale=1.0, loss=None, lse=None, workspace=None):
+    """Softmax cross entropy of rows X [N, D] against the classes' rows W [V, D]: logits scale * X W^T + bias, which are not kept.
+    labels int32 [N]; a row whose label lies outside [0, V) is ignored.  Returns (loss, lse), float [N]."""
+    code, ldx, ldw, N, V, D = _xent_args(X, W, labels, bias)
+    if loss is None or lse is None:
+        both = torch.empty(2, N, dtype=torch.float32, device=X.device)
+        loss, lse = both[0] if loss is None else loss, both[1] if lse is None else lse
+    _floats(loss, "loss", N), _floats(lse, "lse", N)
+    _here(loss, lse, workspace)
+    if N == 0:
+        return loss, lse
+    workspace, wp, wn = _workspace(workspace, xent_workspace_bytes(code, N, V, D, False), X.device)
+    _check(load().ftk_xent(code, X.data_ptr(), ldx, N, W.data_ptr(), ldw, V, D, _ptr(bias), scale, labels.data_ptr(),
+                           loss.data_ptr(), lse.data_ptr(), wp, wn, _stream()))
+    return loss, lse
+
+
+def xent_grad(X, W, labels, lse, dloss, bias=None, scale=1.0, dX=None, dW=None, dbias=None, need=(True, True, None), workspace=None):
+    """Gradients of sum(dloss * loss), dloss float [N]; lse as xent returned it.  Returns (dX [N, D], dW [V, D], dbias float [V]); those
+    that `need` leaves out are None (dbias by default unless there is a bias)."""
+    code, ldx, ldw, N, V, D = _xent_args(X, W, labels, bias)
+    _floats(lse, "lse", N), _floats(dloss, "dloss", N)
+    lddx = lddw = D
+    if need[0] or dX is not None:
+        dX, lddx = _new_rows(dX, N, D, X, "dX")
+    if need[1] or dW is not None:
+        dW, lddw = _new_rows(dW, V, D, W, "dW")
+    if dbias is not None:
+        _floats(dbias, "dbias", V)
+    elif need[2] or (need[2] is None and bias is not None):
+        dbias = torch.empty(V, dtype=torch.float32, device=X.device)
+    _here(lse, dloss, dX, dW, dbias, workspace)
+    workspace, wp, wn = _workspace(workspace, xent_workspace_bytes(code, N, V, D, True), X.device)
+    # (an empty tensor has no address, and no rows that would need one)
+    _check(load().ftk_xent_grad(code, X.data_ptr(), ldx, N, W.data_ptr(), ldw, V, D, _ptr(bias), scale, labels.data_ptr(),
+                                lse.data_ptr(), dloss.data_ptr(), _ptr(dX) if N else None, lddx, _ptr(dW), lddw, _ptr(dbias), wp, wn,
+                                _stream()))
+    return dX, dW, dbias
+
+
+# ---- many weights updated at once ------------------------------------------------------------
+
+
+class _AdamwTensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "m", "v", "m_scales", "v_scales", "master")] + [("count", ctypes.c_int64)]
+
+
+class _AdamwOptions(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")]
+                + [(n, ctypes.c_void_p) for n in ("lr_scale", "grad_scale", "step")] + [("seed", ctypes.c_uint64)])
+
+
+class AdamW:
+    """Weights and their states for adamw_step: contiguous device tensors of one type (float32, bfloat16 or float16), not overlapping.
+
+    bits: 32 (m, v float32) or 8 (m, v uint8 codes and a scale byte for every 32 elements).  States that are not given start at
+    zero.  master: float32 copies of 16-bit weights; True makes them from the weights."""
+
+    def __init__(self, params, bits=32, m=None, v=None, m_scales=None, v_scales=None, master=None):
+        if bits not in (8, 32):
+            raise ValueError("states have 8 or 32 bits, got %r" % (bits,))
+        self.params, self.bits = list(params), bits
+        if not self.params:
+            raise ValueError("no weights given")
+        self.dtype = self.params[0].dtype
+        self.code = _row_code(self.params[0], "params", _MX_DTYPES)
+        if master and self.dtype == torch.float32:
+            raise ValueError("weights in 32 bits are their own masters")
+        state, zeros = torch.uint8 if bits == 8 else torch.float32, torch.zeros_like
+        self.m = [zeros(p, dtype=state) for p in self.params] if m is None else list(m)
+        self.v = [zeros(p, dtype=state) for p in self.params] if v is None else list(v)
+        scales = lambda given: [torch.zeros(-(-p.numel() // 32), dtype=torch.uint8, device=p.device)  # noqa: E731
+                                for p in self.params] if given is None else list(given)
+        self.m_scales, self.v_scales = (scales(m_scales), scales(v_scales)) if bits == 8 else (None, None)
+        self.master = [p.float() for p in self.params] if master is True else list(master) if master else None
+        self._table = (_AdamwTensor * len(self.params))()
+        lists = [("params", self.params, self.dtype), ("m", self.m, state), ("v", self.v, state), ("m_scales", self.m_scales, torch.uint8),
+                 ("v_scales", self.v_scales, torch.uint8), ("master", self.master, torch.float32)]
+        spans = []
+        for name, tensors, dtype in lists:
+            if tensors is None:
+                continue
+            if len(tensors) != len(self.params):
+                raise ValueError("%s: %d tensors for %d weights" % (name, len(tensors), len(self.params)))
+            for t, p, row in zip(tensors, self.params, self._table):
+                need = -(-p.numel() // 32) if name.endswith("scales") else p.numel()
+                if not t.is_cuda or t.device != self.params[0].device or t.dtype != dtype or t.numel() != need or not t.is_contiguous():
+                    raise ValueError("%s must be contiguous tensors of %s with the weights' elements, on their device" % (name, dtype))
+                if need:
+                    setattr(row, "param" if name == "params" else name, t.data_ptr())
+                    spans.append((t.data_ptr(), t.data_ptr() + need * t.element_size()))
+        for p, row in zip(self.params, self._table):
+            row.count = p.numel()
+        spans.sort()
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            raise ValueError("weights or states overlap")
+
+
+def adamw_step(state, grads, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, seed=0, lr_scale=None, grad_scale=None):
+    """One AdamW step over all of state's weights, in place.  grads: a contiguous tensor for each weight, of one type (float32 or the
+    weights'; float32 weights: any), or None: that weight stays.  step: int64 device tensor of one element, 1 at the first
+    step.  lr_scale, grad_scale: float32 device tensors of one element that multiply the rate and the gradients.  seed: of the
+    rounding of 8-bit states."""
+    params = state.params
+    if len(grads) != len(params):
+        raise ValueError("%d gradients for %d weights" % (len(grads), len(params)))
+    dtype, device = None, params[0].get_device()
+    for g, p, row in zip(grads, params, state._table):
+        if g is None:
+            row.grad = None
+            continue
+        if dtype is None:
+            dtype = g.dtype
+        if g.dtype != dtype or g.numel() != p.numel() or g.get_device() != device or not g.is_contiguous():
+            raise ValueError("gradients must be contiguous tensors of one type with the weights' elements, on their device")
+        row.grad = g.data_ptr()
+    if dtype is None:
+        return
+    code = _MX_DTYPES.get(dtype)
+    if code is None:
+        raise TypeError("gradients: %s is not one of float32, bfloat16, float16" % dtype)
+    if not step.is_cuda or step.dtype != torch.int64 or step.numel() != 1:
+        raise ValueError("step must be an int64 device tensor of one element")
+    for t, name in ((lr_scale, "lr_scale"), (grad_scale, "grad_scale")):
+        if t is not None and (not t.is_cuda or t.dtype != torch.float32 or t.numel() != 1):
+            raise ValueError("%s must be a float32 device tensor of one element" % name)
+    _here(params[0], step, lr_scale, grad_scale)
+    options = _AdamwOptions(lr, beta1, beta2, eps, weight_decay, _ptr(lr_scale), _ptr(grad_scale), step.data_ptr(), seed & (2**64 - 1))
+    _check(load().ftk_adamw_step(state.code, code, state.bits, state._table, len(params), ctypes.byref(options), _stream()))
+
+
+def adamw_moments(state, out=None, dtype=torch.float32):
+    """What 8-bit states stand for: lists (m, v) of tensors of the weights' sizes; out: such a pair of lists to write to."""
+    if state.bits != 8:
+        raise ValueError("states in 32 bits are their own values")
+    if out is None:
+        out = [[torch.empty_like(p, dtype=dtype) for p in state.params] for _ in range(2)]
+    dtype = out[0][0].dtype
+    lists = []
+    for ts in out:
+        if len(ts) != len(state.params):
+            raise ValueError("out must be two lists of %d tensors" % len(state.params))
+        for t, p in zip(ts, state.params):
+            if t.dtype != dtype or t.numel() != p.numel() or t.get_device() != p.get_device() or not t.is_contiguous():
+                raise ValueError("out must be contiguous tensors of one type with the weights' elements, on their device")
+        lists.append((ctypes.c_void_p * len(ts))(*[t.data_ptr() for t in ts]))
+    _here(state.params[0])
+    _check(load().ftk_adamw_moments(_row_code(out[0][0], "out", _MX_DTYPES), state._table, len(state.params), lists[0], lists[1], _stream()))
     return out

@@ -246,6 +246,16 @@ __device__ __forceinline__ void to_lds4(const void *g, void *l)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(at), "v"(g) : "memory", "m0");
 }
 
+// The same to an LDS address; the second from a common base and 32-bit offsets of the lanes.
+__device__ __forceinline__ void to_lds16_at(const uint8_t *g, uint32_t at)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(g) : "memory", "m0");
+}
+__device__ __forceinline__ void to_lds16_from(const uint8_t *base, uint32_t offset, uint32_t at)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(base) : "memory", "m0");
+}
+
 // wait until all but the youngest N memory loads, and all LDS accesses, are done
 template <int N>
 __device__ __forceinline__ void wait_loads()

@@ -1,0 +1,861 @@
+// Softmax cross entropy of rows against many classes, without keeping the logits: loss and gradients.
+//
+//   z = scale * X W^T + bias;  lse_n = log sum_v exp z_nv;  loss_n = lse_n - z_n,label
+//   d = dloss_n (softmax(z) - [v = label]);  dbias = sum_n d;  dX = scale d W;  dW = scale d^T X
+//
+// All of it is products of three forms on tiles that go through LDS, and what happens to a tile's sums at its end:
+//   logits     X W^T  : both operands lie along k; the end takes the largest and the sum of exponentials of the tile's
+//                       part of a row, or forms d in 16 bits, for a piece of the classes at a time
+//   rows' gradient    d W : the second operand lies across k
+//   classes' gradient d^T X : both do
+// What lies across k is read from LDS by ds_read_b64_tr_b16, which gives a lane four elements from four of LDS's rows, so that
+// nothing is transposed in memory.
+// 16-bit rows use the 16-bit matrix instructions, sums in 32 bits; d is rounded to the rows' type like any operand of theirs (for
+// fp16 times a power of two that brings the largest dloss to 2^14, where no probability that counts is lost).
+// 32-bit rows are split into three bf16 pieces each (24 bits), of whose products the six largest are
+// added: what is left out is below 2^-24 of the magnitudes.
+#include <math.h>
+
+#include "ftk_mma.h"
+#include "ftk_mx4.h"
+#include "ftk_quads.h"
+
+namespace ftk {
+
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef uint16_t half8 __attribute__((ext_vector_type(8)));
+
+constexpr int XENT_STAGE = 64;  // elements of k in LDS at a time: a line of 128 bytes
+constexpr int64_t XENT_MAX_LD = 1 << 23;  // elements of a row: offsets within a tile are 32 bits wide
+constexpr int XENT_MAX_D = 1 << 20;
+
+// One operand: `outer` rows or columns of the result by `inner` elements of k.
+// Along k: rows of ld elements.  Across k: rows are k.  Multiples of eight elements, 16-byte aligned.
+struct Operand {
+    const uint16_t *p;
+    int64_t ld, plane;  // elements from one bf16 piece of the rows to the next
+    int64_t outer, inner;
+};
+struct Product {
+    Operand a, b;  // the result's rows and columns
+    int64_t mt, nt;
+    int stages;  // of a segment
+    int segments;  // 1, or 6: products of pieces
+};
+
+template <int MT_, int NT_, int WM_, int WN_>
+struct Shape {
+    static constexpr int MT = MT_, NT = NT_, WM = WM_, WN = WN_, WAVES = WM * WN, THREADS = 64 * WAVES;
+    static constexpr int TM = 16 * MT * WM, TN = 16 * NT * WN;
+    static constexpr int A = TM * 128, STAGE = (TM + TN) * 128, LDS = 2 * STAGE;
+};
+
+// What a workgroup's end knows of its place.
+struct Place {
+    int64_t m0, n0;  // of the tile
+    int wm, wn;      // of the wave within it
+    int64_t mtile, ntile;
+};
+
+// Row of row tile i, and column of column tile j, that lane row r (of 16) has.  Two column tiles give a lane eight consecutive
+// columns of a result row; what lies across k is read the same way.
+template <bool ACROSS>
+__device__ __forceinline__ int line_of(int i, int r)
+{
+    return ACROSS ? 32 * (i >> 1) + 8 * (r >> 2) + 4 * (i & 1) + (r & 3) : 16 * i + r;
+}
+
+// Pieces of 16 bytes are stored at their place xor a key, so that lanes that read together meet all banks.
+// Along k (lines of 8 pieces): the rows that 16 lanes read differ in the key or in parity.
+template <bool PERMUTED>
+__device__ __forceinline__ int line_key(int row)
+{
+    return PERMUTED ? ((row >> 1) & 1) | ((row >> 3) & 3) << 1 : (row >> 1) & 7;
+}
+// Across k (T columns, T / 8 pieces a row): four rows of k, four pieces each.
+template <int T>
+__device__ __forceinline__ int across_key(int k)
+{
+    return T >= 128 ? (k & 3) * 4 : (k >> 1 & 1) * 4;
+}
+
+// Copies of one operand's tile of T rows (columns) to LDS, a share of them a wave.
+template <int T, int WAVES, bool ACROSS, bool PERMUTED>
+struct Copies {
+    static constexpr int N = T / 8 / WAVES;  // of a wave
+    uint32_t off[N];
+    const uint8_t *base;
+    int64_t step;  // bytes of a stage
+    static __device__ __forceinline__ int k_of(int c, int lane) { return c * (512 / T) + lane / (T / 8); }
+    static __device__ __forceinline__ int piece_of(int c, int lane)
+    {
+        if (ACROSS) return (lane & (T / 8 - 1)) ^ across_key<T>(k_of(c, lane));
+        return (lane & 7) ^ line_key<PERMUTED>(c * 8 + (lane >> 3));
+    }
+    __device__ __forceinline__ void begin(const Operand &o, int64_t first, int w, int lane)
+    {
+        base = (const uint8_t *)(o.p + (ACROSS ? first : first * o.ld));
+        step = ACROSS ? XENT_STAGE * o.ld * 2 : XENT_STAGE * 2;
+        const int64_t left = o.outer - first;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int c = w * N + i;
+            int piece = piece_of(c, lane);
+            if (ACROSS) {
+                if (piece * 8 >= left) piece = 0;
+                off[i] = (uint32_t)k_of(c, lane) * (uint32_t)o.ld * 2 + piece * 16;
+            } else {
+                const int64_t row = c * 8 + (lane >> 3);
+                off[i] = (uint32_t)(row < left ? row : left - 1) * (uint32_t)o.ld * 2 + piece * 16;
+            }
+        }
+    }
+    // stage st of a segment's `stages`, from piece `plane` of the rows
+    __device__ __forceinline__ void copy(const Operand &o, int plane, int st, int stages, uint32_t lds, int w, int lane) const
+    {
+        const uint8_t *from = base + plane * o.plane * 2 + st * step;
+        const int64_t left = o.inner - (int64_t)st * XENT_STAGE;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            uint32_t at = off[i];
+            if (left < XENT_STAGE) {
+                const int c = w * N + i;
+                if (ACROSS) {
+                    const int k = k_of(c, lane);
+                    if (k >= left) at -= (uint32_t)(k - (int)left + 1) * (uint32_t)o.ld * 2;
+                } else if (piece_of(c, lane) * 8 >= left) {
+                    at -= piece_of(c, lane) * 16;
+                }
+            }
+            to_lds16_from(from, at, lds + (w * N + i) * 1024);
+        }
+    }
+};
+
+// Fragments of one operand: 16 rows (columns), lane quarter q has elements 8 q ... of a step of 32.
+template <int T, bool ACROSS, bool PERMUTED>
+struct Fragments {
+    // first: of the wave's rows within the tile
+    static __device__ __forceinline__ half8 read(const uint8_t *lds, int first, int i, int s, int lane)
+    {
+        const int r = lane & 15, q = lane >> 4;
+        if constexpr (ACROSS) {
+            typedef __attribute__((address_space(3))) short4v lds4;
+            const int k = s * 32 + q * 8 + (r >> 2), piece = (first >> 3) + 4 * (i >> 1) + (r & 3);
+            const uint8_t *p = lds + k * (T * 2) + (piece ^ across_key<T>(k)) * 16 + (i & 1) * 8;
+            // (k + 4 has the same key)
+            const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)p);
+            const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(p + 4 * T * 2));
+            return __builtin_bit_cast(half8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            const int row = first + line_of<PERMUTED>(i, r);
+            return *reinterpret_cast<const half8 *>(lds + row * 128 + ((s * 4 + q) ^ line_key<PERMUTED>(row)) * 16);
+        }
+    }
+};
+
+template <typename H>
+__device__ __forceinline__ float4v mma(half8 b, half8 a, float4v c)
+{
+    typedef H vec __attribute__((ext_vector_type(8)));
+    if constexpr (std::is_same<H, __bf16>::value)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(vec, b), __builtin_bit_cast(vec, a), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(vec, b), __builtin_bit_cast(vec, a), c, 0, 0, 0);
+}
+
+// The pieces of segment g, the small products first.
+__device__ __forceinline__ int plane_a(int segments, int g) { return segments == 1 ? 0 : g == 0 ? 2 : g == 1 || g == 3 ? 1 : 0; }
+__device__ __forceinline__ int plane_b(int segments, int g) { return segments == 1 ? 0 : g == 2 ? 2 : g == 1 || g == 4 ? 1 : 0; }
+
+// Workgroups are dealt to the eight XCDs in turn; each XCD gets a run of tiles, eight rows of tiles high, so that the 32 tiles
+// under way there share their operands in its L2.
+__device__ __forceinline__ void tile_of(const Product &g, int64_t &mtile, int64_t &ntile)
+{
+    const int64_t all = g.mt * g.nt, each = (all + 7) / 8;
+    int64_t t = blockIdx.x;
+    const int64_t x = t & 7, full = all & 7;  // the first `full` XCDs have one more where all is no multiple
+    t = full ? x * (each - 1) + min(x, full) + (t >> 3) : x * each + (t >> 3);
+    const int64_t panel = t / (8 * g.nt), in = t - panel * 8 * g.nt, high = min((int64_t)8, g.mt - panel * 8);
+    ntile = in / high;
+    mtile = panel * 8 + (in - ntile * high);
+}
+
+template <typename S, typename H, bool AT, bool BT, typename End>
+__global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product g, End end)
+{
+    extern __shared__ __align__(16) uint8_t lds[];
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Place at;
+    tile_of(g, at.mtile, at.ntile);
+    at.m0 = at.mtile * S::TM;
+    at.n0 = at.ntile * S::TN;
+    at.wm = w / S::WN * 16 * S::MT;
+    at.wn = w % S::WN * 16 * S::NT;
+    float4v acc[S::MT][S::NT];
+#pragma unroll
+    for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+        for (int j = 0; j < S::NT; ++j) acc[i][j] = float4v{0, 0, 0, 0};
+    Copies<S::TM, S::WAVES, AT, false> ca;
+    Copies<S::TN, S::WAVES, BT, true> cb;
+    ca.begin(g.a, at.m0, w, lane);
+    cb.begin(g.b, at.n0, w, lane);
+    const int total = g.stages * g.segments;
+    int seg = 0, st = 0;  // of the next copy
+    auto copy = [&](int buffer) __attribute__((always_inline)) {
+        const uint32_t to = lds0 + buffer * S::STAGE;
+        ca.copy(g.a, plane_a(g.segments, seg), st, g.stages, to, w, lane);
+        cb.copy(g.b, plane_b(g.segments, seg), st, g.stages, to + S::A, w, lane);
+        if (++st == g.stages) {
+            st = 0;
+            ++seg;
+        }
+    };
+    copy(0);
+    for (int n = 0; n < total; ++n) {
+        // stage n has arrived, and the one before it is read, in all waves
+        wait_loads<0>();
+        __syncthreads();
+        if (n + 1 < total) copy((n + 1) & 1);
+        const uint8_t *const la = lds + (n & 1) * S::STAGE, *const lb = la + S::A;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            half8 a[S::MT], b[S::NT];
+#pragma unroll
+            for (int j = 0; j < S::NT; ++j) b[j] = Fragments<S::TN, BT, true>::read(lb, at.wn, j, s, lane);
+#pragma unroll
+            for (int i = 0; i < S::MT; ++i) a[i] = Fragments<S::TM, AT, false>::read(la, at.wm, i, s, lane);
+#pragma unroll
+            for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+                for (int j = 0; j < S::NT; ++j) acc[i][j] = mma<H>(b[j], a[i], acc[i][j]);
+        }
+    }
+    __syncthreads();
+    end.template run<S, AT>(acc, at, lds);
+}
+
+// ---- ends -----------------------------------------------------------------------------------
+
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+
+struct Logits {
+    const float *bias;      // NULL: none
+    const int32_t *labels;
+    int64_t N;
+    int64_t first, last;    // classes of this call: `first` is the products' first one
+    int64_t V;
+    float scale;
+    __device__ __forceinline__ float bias_of(int64_t v) const { return bias && v < V ? bias[v] : 0.f; }
+};
+
+// The tile's part of a row: its largest logit, the sum of exponentials below it, and the label's logit.
+struct SumEnd {
+    Logits z;
+    float2 *parts;  // [N][tiles]
+    int64_t tiles, first_tile;
+    float *label_logit;  // [N]
+    template <typename S, bool AT>
+    __device__ __forceinline__ void run(float4v (&acc)[S::MT][S::NT], const Place &at, uint8_t *lds) const
+    {
+        const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+        float2 *const part = reinterpret_cast<float2 *>(lds);  // [WN][TM]
+        const int64_t v0 = z.first + at.n0 + at.wn + 8 * q;
+        float bias[S::NT][4];
+#pragma unroll
+        for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) bias[j][c] = z.bias_of(v0 + 32 * (j >> 1) + 4 * (j & 1) + c);
+#pragma unroll
+        for (int i = 0; i < S::MT; ++i) {
+            const int row = at.wm + line_of<AT>(i, r);
+            const int64_t n = at.m0 + row;
+            const int64_t label = n < z.N ? z.labels[n] : -1;
+            float top = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const int64_t v = v0 + 32 * (j >> 1) + 4 * (j & 1) + c;
+                    const float x = v < z.last ? fmaf(z.scale, acc[i][j][c], bias[j][c]) : -__builtin_inff();
+                    if (v == label && v < z.last) z_store(n, x);
+                    acc[i][j][c] = x;
+                    top = fmaxf(top, x);
+                }
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float shift = top > -__builtin_inff() ? top : 0.f;
+#pragma unroll
+            for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) sum += exp2_of(acc[i][j][c] - shift);
+            sum += __shfl_xor(sum, 16, 64);
+            sum += __shfl_xor(sum, 32, 64);
+            if (q == 0) part[at.wn / (16 * S::NT) * S::TM + row] = float2{top, sum};
+        }
+        __syncthreads();
+        for (int row = threadIdx.x; row < S::TM; row += S::THREADS) {
+            const int64_t n = at.m0 + row;
+            if (n >= z.N) break;
+            float2 p = part[row];
+#pragma unroll
+            for (int k = 1; k < S::WN; ++k) p = joined(p, part[k * S::TM + row]);
+            parts[n * tiles + first_tile + at.ntile] = p;
+        }
+    }
+    __device__ __forceinline__ void z_store(int64_t n, float x) const { label_logit[n] = x; }
+    static __device__ __forceinline__ float2 joined(float2 a, float2 b)
+    {
+        const float top = fmaxf(a.x, b.x), shift = top > -__builtin_inff() ? top : 0.f;
+        return float2{top, a.y * exp2_of(a.x - shift) + b.y * exp2_of(b.x - shift)};
+    }
+};
+
+// A wave a row: its parts together.
+__global__ __launch_bounds__(256) void xent_loss_kernel(const float2 *parts, int64_t tiles, const float *label_logit,
+                                                        const int32_t *labels, int64_t N, int64_t V, float *loss, float *lse)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (n >= N) return;
+    float top = -__builtin_inff();
+    for (int64_t t = lane; t < tiles; t += 64) top = fmaxf(top, parts[n * tiles + t].x);
+    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+    const float shift = top > -__builtin_inff() ? top : 0.f;
+    float sum = 0.f;
+    for (int64_t t = lane; t < tiles; t += 64) {
+        const float2 p = parts[n * tiles + t];
+        sum += p.y * exp2_of(p.x - shift);
+    }
+    sum = group_sum<64>(sum);
+    if (lane == 0) {
+        const int64_t label = labels[n];
+        const bool live = label >= 0 && label < V;
+        const float l = sum == 0.f ? -__builtin_inff() : shift + logf(sum);
+        lse[n] = live ? l : 0.f;
+        loss[n] = live ? l - label_logit[n] : 0.f;
+    }
+}
+
+// Power of two that brings the largest |dloss| to [2^14, 2^15) (fp16 rows), else 1.
+__device__ __forceinline__ float factor_of(const uint32_t *top)
+{
+    if (!top) return 1.f;
+    const int e = (int)(*top >> 23);
+    return *top == 0 || e == 255 ? 1.f : __uint_as_float((uint32_t)min(254, max(1, 268 - e)) << 23);
+}
+
+// d of a tile, in 16 bits (or three bf16 pieces), zero in rows and columns that only fill up; sums over the tile's rows.
+template <typename H, int PLANES>
+struct GradEnd {
+    Logits z;
+    const float *lse, *dloss;
+    const uint32_t *top;
+    uint16_t *d;        // [rows][ld]
+    int64_t ld, plane, rows;
+    float *dbias;       // [row tiles][ld], or NULL
+    template <typename S, bool AT>
+    __device__ __forceinline__ void run(float4v (&acc)[S::MT][S::NT], const Place &at, uint8_t *lds) const
+    {
+        const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+        const int64_t v0 = z.first + at.n0 + at.wn + 8 * q;
+        const float factor = factor_of(top);
+        float bias[S::NT][4], sum[S::NT][4];
+#pragma unroll
+        for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                bias[j][c] = z.bias_of(v0 + 32 * (j >> 1) + 4 * (j & 1) + c);
+                sum[j][c] = 0.f;
+            }
+#pragma unroll
+        for (int i = 0; i < S::MT; ++i) {
+            const int64_t n = at.m0 + at.wm + line_of<AT>(i, r);
+            const bool in = n < z.N;
+            const int64_t label = in ? z.labels[n] : -1;
+            const bool live = label >= 0 && label < z.V;
+            const float l = in ? lse[n] : 0.f, g = in ? dloss[n] : 0.f;
+#pragma unroll
+            for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const int64_t v = v0 + 32 * (j >> 1) + 4 * (j & 1) + c;
+                    const float x = fmaf(z.scale, acc[i][j][c], bias[j][c]);
+                    float p = l == -__builtin_inff() ? 0.f : exp2_of(x - l);
+                    p = live && v < z.last ? (p - (v == label ? 1.f : 0.f)) * g : 0.f;
+                    sum[j][c] += p;
+                    acc[i][j][c] = p * factor;
+                }
+            if (n >= rows) continue;
+            uint16_t *const to = d + n * ld + at.n0 + at.wn + 8 * q;
+#pragma unroll
+            for (int j = 0; j < S::NT; j += 2) {
+                half8 o[PLANES];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    float x = acc[i][j + (c >> 2)][c & 3];
+#pragma unroll
+                    for (int k = 0; k < PLANES; ++k) {
+                        const H h = (H)x;
+                        o[k][c] = __builtin_bit_cast(uint16_t, h);
+                        x -= (float)h;
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < PLANES; ++k) *reinterpret_cast<half8 *>(to + k * plane + 16 * j) = o[k];
+            }
+        }
+        if (!dbias) return;
+        float *const part = reinterpret_cast<float *>(lds);  // [WM][TN]
+#pragma unroll
+        for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const float s = group_sum<16>(sum[j][c]);
+                if (r == 0) part[at.wm / (16 * S::MT) * S::TN + at.wn + 32 * (j >> 1) + 8 * q + 4 * (j & 1) + c] = s;
+            }
+        __syncthreads();
+        for (int c = threadIdx.x; c < S::TN; c += S::THREADS) {
+            float s = part[c];
+#pragma unroll
+            for (int k = 1; k < S::WM; ++k) s += part[k * S::TN + c];
+            dbias[at.mtile * ld + at.n0 + c] = s;
+        }
+    }
+};
+
+__global__ __launch_bounds__(256) void dbias_kernel(const float *parts, int64_t ld, int64_t tiles, int64_t n, float *out)
+{
+    const int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (v >= n) return;
+    double s = 0;
+    for (int64_t t = 0; t < tiles; ++t) s += parts[t * ld + v];
+    out[v] = (float)s;
+}
+
+// A gradient: the sums times `scale` (and what d was multiplied by taken out), added to those of earlier pieces of the classes.
+template <typename T>
+struct StoreEnd {
+    T *out;
+    int64_t ld, rows, cols;
+    float *sums;  // of earlier and later pieces, or NULL
+    int64_t lds;  // a row of theirs
+    bool first, last;
+    float scale;
+    const uint32_t *top;
+    template <typename S, bool AT>
+    __device__ __forceinline__ void run(float4v (&acc)[S::MT][S::NT], const Place &at, uint8_t *) const
+    {
+        const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+        const float f = scale / factor_of(top);
+        typedef T Eight __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+        typedef float Four __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+        for (int i = 0; i < S::MT; ++i) {
+            const int64_t m = at.m0 + at.wm + line_of<AT>(i, r);
+            if (m >= rows) continue;
+#pragma unroll
+            for (int j = 0; j < S::NT; j += 2) {
+                const int64_t n = at.n0 + at.wn + 16 * j + 8 * q;
+                if (n >= cols) continue;
+                float v[8];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) v[c] = acc[i][j + (c >> 2)][c & 3];
+                const bool whole = n + 8 <= cols;
+                if (sums) {
+                    float *const s = sums + m * lds + n;
+                    if (!first) {
+#pragma unroll
+                        for (int c = 0; c < 8; c += 4) {
+                            if (whole) {
+                                const Four x = *reinterpret_cast<const Four *>(s + c);
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) v[c + k] += x[k];
+                            } else {
+#pragma unroll
+                                for (int k = 0; k < 4; ++k)
+                                    if (n + c + k < cols) v[c + k] += s[c + k];
+                            }
+                        }
+                    }
+                    if (!last) {
+#pragma unroll
+                        for (int c = 0; c < 8; c += 4) {
+                            if (whole) {
+                                *reinterpret_cast<Four *>(s + c) = Four{v[c], v[c + 1], v[c + 2], v[c + 3]};
+                            } else {
+#pragma unroll
+                                for (int k = 0; k < 4; ++k)
+                                    if (n + c + k < cols) s[c + k] = v[c + k];
+                            }
+                        }
+                        continue;
+                    }
+                }
+                T *const o = out + m * ld + n;
+                if (whole) {
+                    Eight x;
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) x[c] = (T)(v[c] * f);
+                    *reinterpret_cast<Eight *>(o) = x;
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)
+                        if (n + c < cols) o[c] = (T)(v[c] * f);
+                }
+            }
+        }
+    }
+};
+
+// Rows to whole lines of 64 elements (three bf16 pieces where PLANES is 3), zeros beyond the row and in rows that are not looked at:
+// those whose label lies outside [0, V), and those from N on.
+template <typename T, typename H, int PLANES>
+__global__ __launch_bounds__(256) void pack_kernel(const T *__restrict__ X, int64_t ldx, int64_t N, int D, int64_t rows, int Dp,
+                                                   const int32_t *labels, int64_t V, uint16_t *__restrict__ out, uint32_t *zero)
+{
+    if (zero && blockIdx.x == 0 && threadIdx.x == 0) *zero = 0;
+    const int pieces = Dp / 8;
+    const int64_t all = rows * pieces;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t n = i / pieces;
+        const int d = (int)(i - n * pieces) * 8;
+        bool live = n < N;
+        if (live && labels) live = labels[n] >= 0 && labels[n] < V;
+        T v[8];
+        if (live) {
+            load8(X + n * ldx, d, D, v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (T)0.f;
+        }
+        half8 o[PLANES];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float x = (float)v[e];
+#pragma unroll
+            for (int k = 0; k < PLANES; ++k) {
+                const H h = (H)x;
+                o[k][e] = __builtin_bit_cast(uint16_t, h);
+                x -= (float)h;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < PLANES; ++k) *reinterpret_cast<half8 *>(out + k * rows * Dp + n * Dp + d) = o[k];
+    }
+}
+
+__global__ __launch_bounds__(256) void dloss_top_kernel(const float *dloss, const int32_t *labels, int64_t N, int64_t V, uint32_t *top)
+{
+    uint32_t m = 0;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < N; i += (int64_t)gridDim.x * 256)
+        if (labels[i] >= 0 && labels[i] < V) m = max(m, mag_bits(dloss[i]));
+    for (int d = 32; d; d >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d, 64));
+    if ((threadIdx.x & 63) == 0 && m) atomicMax(top, m);
+}
+
+// ---- calls -----------------------------------------------------------------------------------
+
+struct XentPlan {
+    bool direct;      // W is read where it lies
+    int planes;
+    int64_t rows;     // N rounded up to whole stages
+    int Dp;           // D rounded up to whole stages
+    int64_t width;    // classes of a piece
+    int64_t tiles;    // column tiles of the logits' sums, all classes
+    size_t X, W, parts, label_logit, d, sums, dbias, top, total;
+};
+
+using Large = Shape<8, 4, 2, 4>;   // 256 x 256, eight waves
+using Middle = Shape<4, 4, 2, 2>;  // 128 x 128
+using Small = Shape<2, 2, 2, 2>;   // 64 x 64
+constexpr int XENT_TILE = 64;      // columns that a sum's part stands for at least
+
+static bool rows_direct(ftk_dtype dtype, const void *p, int64_t ld, int D)
+{
+    return dtype != FTK_F32 && (uintptr_t)p % 16 == 0 && ld % 8 == 0 && D % 8 == 0 && ld < XENT_MAX_LD;
+}
+
+// `direct` false: as much as any address and stride of W may need.
+static XentPlan plan_xent(ftk_dtype dtype, int64_t N, int64_t V, int D, bool grad, bool direct)
+{
+    XentPlan p;
+    p.direct = direct;
+    p.planes = dtype == FTK_F32 ? 3 : 1;
+    p.rows = ceil_div(N > 0 ? N : 1, XENT_STAGE) * XENT_STAGE;  // (without rows gradients are zeros)
+    p.Dp = (int)(ceil_div(D, XENT_STAGE) * XENT_STAGE);
+    // d, or the packed rows of W, of a piece: about 128 MB, which the memory-side cache holds
+    const int64_t rows = grad && p.rows > p.Dp ? p.rows : p.Dp;
+    int64_t width = (64ll << 20) / p.planes / rows / 256 * 256;
+    width = width < 256 ? 256 : width;
+    const int64_t whole = ceil_div(V, 256) * 256;
+    if (!grad && direct) width = whole;
+    p.width = width < whole ? width : whole;
+    // (pieces of equal width)
+    p.width = ceil_div(ceil_div(V, ceil_div(V, p.width)), 256) * 256;
+    p.tiles = ceil_div(V, XENT_TILE);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t a = at;
+        at += align_up(bytes, 256);
+        return a;
+    };
+    p.X = take((size_t)p.planes * p.rows * p.Dp * 2);
+    p.W = direct ? at : take((size_t)p.planes * p.width * p.Dp * 2);
+    p.parts = p.label_logit = p.d = p.sums = p.dbias = p.top = at;
+    if (grad) {
+        p.d = take((size_t)p.planes * p.rows * p.width * 2);
+        p.sums = dtype == FTK_F32 ? at : take((size_t)N * D * 4);
+        p.dbias = take((size_t)ceil_div(p.rows, XENT_TILE) * p.width * 4);
+        p.top = take(256);
+    } else {
+        p.parts = take((size_t)N * p.tiles * 8);
+        p.label_logit = take((size_t)N * 4);
+    }
+    p.total = at;
+    return p;
+}
+
+template <typename S, typename H, bool AT, bool BT, typename End>
+static ftk_status launch_shape(Product g, const End &end, hipStream_t st)
+{
+    g.mt = ceil_div(g.a.outer, S::TM);
+    g.nt = ceil_div(g.b.outer, S::TN);
+    if (g.mt * g.nt > 0x7fffffffLL) {
+        set_error("too many tiles: %lld x %lld", (long long)g.mt, (long long)g.nt);
+        return FTK_EINVAL;
+    }
+    FTK_TRY(allow_lds<S::LDS>((const void *)product_kernel<S, H, AT, BT, End>));
+    product_kernel<S, H, AT, BT, End><<<(unsigned)(g.mt * g.nt), S::THREADS, S::LDS, st>>>(g, end);
+    FTK_TRY_HIP(hipGetLastError());
+    return FTK_OK;
+}
+
+// Time of a shape's tiles in some unit: so many run at once, each takes what its stages take and an end.
+static double shape_cost(const Product &g, int tm, int tn, int at_once, double end, double stage)
+{
+    return (double)ceil_div(ceil_div(g.a.outer, tm) * ceil_div(g.b.outer, tn), at_once) * (end + g.stages * g.segments * stage);
+}
+static int shape_of(const Product &g)
+{
+    const double large = shape_cost(g, 256, 256, 256, 6, 1.0), middle = shape_cost(g, 128, 128, 512, 4, 0.6),
+                 small = shape_cost(g, 64, 64, 1024, 3, 0.4);
+    return large <= middle && large <= small ? 256 : middle <= small ? 128 : 64;
+}
+template <typename H, bool AT, bool BT, typename End>
+static ftk_status launch_product(const Product &g, int tile, const End &end, hipStream_t st)
+{
+    if (tile == 256) return launch_shape<Large, H, AT, BT>(g, end, st);
+    if (tile == 128) return launch_shape<Middle, H, AT, BT>(g, end, st);
+    return launch_shape<Small, H, AT, BT>(g, end, st);
+}
+
+template <typename T, typename H, int PLANES>
+static ftk_status launch_pack(const T *X, int64_t ldx, int64_t N, int D, int64_t rows, int Dp, const int32_t *labels, int64_t V,
+                              uint16_t *out, uint32_t *zero, hipStream_t st)
+{
+    const int64_t groups = ceil_div(rows * (Dp / 8), 256);
+    pack_kernel<T, H, PLANES><<<(unsigned)(groups < 4096 ? groups : 4096), 256, 0, st>>>(X, ldx, N, D, rows, Dp, labels, V, out, zero);
+    FTK_TRY_HIP(hipGetLastError());
+    return FTK_OK;
+}
+
+struct XentCall {
+    const void *X, *W;
+    int64_t ldx, N, ldw, V;
+    int D;
+    const float *bias;
+    float scale;
+    const int32_t *labels;
+    uint8_t *ws;
+    XentPlan p;
+    hipStream_t st;
+    // one piece's rows of W: packed, or where they lie
+    template <typename T, typename H, int PLANES>
+    ftk_status classes(int64_t first, int64_t n, Operand &along, Operand &across) const
+    {
+        if (p.direct) {
+            const uint16_t *w = (const uint16_t *)W + first * ldw;
+            along = Operand{w, ldw, 0, n, D};
+            across = Operand{w, ldw, 0, D, n};
+            return FTK_OK;
+        }
+        uint16_t *w = (uint16_t *)(ws + p.W);
+        FTK_TRY((launch_pack<T, H, PLANES>((const T *)W + first * ldw, ldw, n, D, n, p.Dp, nullptr, 0, w, nullptr, st)));
+        along = Operand{w, p.Dp, n * p.Dp, n, p.Dp};
+        across = Operand{w, p.Dp, n * p.Dp, p.Dp, n};
+        return FTK_OK;
+    }
+};
+
+template <typename T, typename H, int PLANES>
+static ftk_status xent_forward(const XentCall &c, float *loss, float *lse)
+{
+    const XentPlan &p = c.p;
+    uint16_t *x = (uint16_t *)(c.ws + p.X);
+    FTK_TRY((launch_pack<T, H, PLANES>((const T *)c.X, c.ldx, c.N, c.D, p.rows, p.Dp, c.labels, c.V, x, nullptr, c.st)));
+    float2 *parts = (float2 *)(c.ws + p.parts);
+    float *label_logit = (float *)(c.ws + p.label_logit);
+    Product g;
+    g.a = Operand{x, p.Dp, p.rows * p.Dp, c.N, p.Dp};
+    g.stages = p.Dp / XENT_STAGE;
+    g.segments = PLANES == 3 ? 6 : 1;
+    // one shape for all pieces: a part stands for as many columns everywhere
+    g.b.outer = p.width < c.V ? p.width : c.V;
+    const int tile = shape_of(g);
+    const int64_t tiles = ceil_div(c.V, tile);
+    for (int64_t first = 0; first < c.V; first += p.width) {
+        const int64_t n = c.V - first < p.width ? c.V - first : p.width;
+        Operand across;
+        FTK_TRY((c.classes<T, H, PLANES>(first, n, g.b, across)));
+        const SumEnd end{Logits{c.bias, c.labels, c.N, first, first + n, c.V, c.scale}, parts, tiles, first / tile, label_logit};
+        FTK_TRY((launch_product<H, false, false>(g, tile, end, c.st)));
+    }
+    xent_loss_kernel<<<(unsigned)ceil_div(c.N, 4), 256, 0, c.st>>>(parts, tiles, label_logit, c.labels, c.N, c.V, loss, lse);
+    FTK_TRY_HIP(hipGetLastError());
+    return FTK_OK;
+}
+
+template <typename T, typename H, int PLANES>
+static ftk_status xent_backward(const XentCall &c, const float *lse, const float *dloss, T *dX, int64_t lddx, T *dW, int64_t lddw,
+                                float *dbias)
+{
+    const XentPlan &p = c.p;
+    uint16_t *x = (uint16_t *)(c.ws + p.X), *d = (uint16_t *)(c.ws + p.d);
+    uint32_t *top = std::is_same<T, _Float16>::value ? (uint32_t *)(c.ws + p.top) : nullptr;
+    float *parts = (float *)(c.ws + p.dbias);
+    FTK_TRY((launch_pack<T, H, PLANES>((const T *)c.X, c.ldx, c.N, c.D, p.rows, p.Dp, c.labels, c.V, x, top, c.st)));
+    if (top) {
+        const int64_t groups = ceil_div(c.N, 1024);
+        dloss_top_kernel<<<(unsigned)(groups < 256 ? groups : 256), 256, 0, c.st>>>(dloss, c.labels, c.N, c.V, top);
+        FTK_TRY_HIP(hipGetLastError());
+    }
+    const int segments = PLANES == 3 ? 6 : 1;
+    for (int64_t first = 0; first < c.V; first += p.width) {
+        const int64_t n = c.V - first < p.width ? c.V - first : p.width, np = ceil_div(n, XENT_STAGE) * XENT_STAGE;
+        const int64_t plane = p.rows * p.width;
+        Operand along, across;
+        FTK_TRY((c.classes<T, H, PLANES>(first, n, along, across)));
+        Product g{Operand{x, p.Dp, p.rows * p.Dp, p.rows, p.Dp}, along, 0, 0, p.Dp / XENT_STAGE, segments};
+        const int tile = shape_of(g);
+        const GradEnd<H, PLANES> grad{Logits{c.bias, c.labels, c.N, first, first + n, c.V, c.scale}, lse, dloss, top, d, p.width, plane,
+                                      p.rows, dbias ? parts : nullptr};
+        FTK_TRY((launch_product<H, false, false>(g, tile, grad, c.st)));
+        if (dbias) {
+            dbias_kernel<<<(unsigned)ceil_div(n, 256), 256, 0, c.st>>>(parts, p.width, ceil_div(p.rows, tile), n, dbias + first);
+            FTK_TRY_HIP(hipGetLastError());
+        }
+        if (dX) {
+            Product r{Operand{d, p.width, plane, p.rows, np}, across, 0, 0, (int)(np / XENT_STAGE), segments};
+            const bool one = p.width >= c.V;
+            // (in 32 bits dX itself holds them)
+            float *sums = one ? nullptr : PLANES == 3 ? (float *)dX : (float *)(c.ws + p.sums);
+            StoreEnd<T> end{dX, lddx, c.N, c.D, sums, PLANES == 3 ? lddx : c.D, first == 0, first + n == c.V, c.scale, top};
+            FTK_TRY((launch_product<H, false, true>(r, shape_of(r), end, c.st)));
+        }
+        if (dW) {
+            Product r{Operand{d, p.width, plane, np, p.rows}, Operand{x, p.Dp, p.rows * p.Dp, p.Dp, p.rows}, 0, 0,
+                      (int)(p.rows / XENT_STAGE), segments};
+            StoreEnd<T> end{dW + first * lddw, lddw, n, c.D, nullptr, 0, true, true, c.scale, top};
+            FTK_TRY((launch_product<H, true, true>(r, shape_of(r), end, c.st)));
+        }
+    }
+    return FTK_OK;
+}
+
+static ftk_status check_xent(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N, const void *W, int64_t ldw, int64_t V, int32_t D,
+                             const float *bias, double scale, const int32_t *labels)
+{
+    FTK_TRY(check_mx_type(dtype));
+    if (N < 0 || N > 0x7fffffffLL || V < 1 || V > 0x7fffffffLL || D < 1 || D > XENT_MAX_D) {
+        set_error("need 0 <= N < 2^31, 1 <= V < 2^31, 1 <= D <= %d (got N=%lld V=%lld D=%d)", XENT_MAX_D, (long long)N, (long long)V, D);
+        return FTK_EINVAL;
+    }
+    if (ldx < D || ldw < D) {
+        set_error("row strides %lld of X and %lld of W must be at least D = %d", (long long)ldx, (long long)ldw, D);
+        return FTK_EINVAL;
+    }
+    if (!isfinite(scale)) {
+        set_error("scale must be finite (got %g)", scale);
+        return FTK_EINVAL;
+    }
+    if (N > 0) {
+        FTK_TRY(check_ptr(X, dtype_size(dtype), "X"));
+        FTK_TRY(check_ptr(labels, 4, "labels"));
+    }
+    FTK_TRY(check_ptr(W, dtype_size(dtype), "W"));
+    if (bias) FTK_TRY(check_ptr(bias, 4, "bias"));
+    return FTK_OK;
+}
+
+}  // namespace ftk
+
+using namespace ftk;
+
+extern "C" {
+
+int64_t ftk_xent_workspace_bytes(ftk_dtype dtype, int64_t N, int64_t V, int32_t D, int32_t grad)
+{
+    if (check_mx_type(dtype) != FTK_OK) return -1;
+    if (N < 0 || N > 0x7fffffffLL || V < 1 || V > 0x7fffffffLL || D < 1 || D > XENT_MAX_D) {
+        set_error("need 0 <= N < 2^31, 1 <= V < 2^31, 1 <= D <= %d (got N=%lld V=%lld D=%d)", XENT_MAX_D, (long long)N, (long long)V, D);
+        return -1;
+    }
+    return (int64_t)plan_xent(dtype, N, V, D, grad != 0, false).total;
+}
+
+ftk_status ftk_xent(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N, const void *W, int64_t ldw, int64_t V, int32_t D,
+                    const float *bias, double scale, const int32_t *labels, float *loss, float *lse, void *workspace,
+                    size_t workspace_bytes, void *hip_stream)
+{
+    FTK_TRY(check_xent(dtype, X, ldx, N, W, ldw, V, D, bias, scale, labels));
+    if (N == 0) return FTK_OK;
+    FTK_TRY(check_ptr(loss, 4, "loss"));
+    FTK_TRY(check_ptr(lse, 4, "lse"));
+    const XentPlan p = plan_xent(dtype, N, V, D, false, rows_direct(dtype, W, ldw, D));
+    FTK_TRY(check_workspace(workspace, workspace_bytes, p.total));
+    FTK_TRY(check_device());
+    const XentCall c{X, W, ldx, N, ldw, V, D, bias, (float)scale, labels, (uint8_t *)workspace, p, (hipStream_t)hip_stream};
+    switch (dtype) {
+    case FTK_F32: return xent_forward<float, __bf16, 3>(c, loss, lse);
+    case FTK_BF16: return xent_forward<__bf16, __bf16, 1>(c, loss, lse);
+    default: return xent_forward<_Float16, _Float16, 1>(c, loss, lse);
+    }
+}
+
+ftk_status ftk_xent_grad(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N, const void *W, int64_t ldw, int64_t V, int32_t D,
+                         const float *bias, double scale, const int32_t *labels, const float *lse, const float *dloss, void *dX,
+                         int64_t lddx, void *dW, int64_t lddw, float *dbias, void *workspace, size_t workspace_bytes,
+                         void *hip_stream)
+{
+    FTK_TRY(check_xent(dtype, X, ldx, N, W, ldw, V, D, bias, scale, labels));
+    if (!dX && !dW && !dbias) {
+        set_error("no gradient is asked for");
+        return FTK_EINVAL;
+    }
+    if ((dX && lddx < D) || (dW && lddw < D)) {
+        set_error("row strides %lld of dX and %lld of dW must be at least D = %d", (long long)lddx, (long long)lddw, D);
+        return FTK_EINVAL;
+    }
+    if (N > 0) {
+        FTK_TRY(check_ptr(lse, 4, "lse"));
+        FTK_TRY(check_ptr(dloss, 4, "dloss"));
+    }
+    if (dX) FTK_TRY(check_ptr(dX, dtype_size(dtype), "dX"));
+    if (dW) FTK_TRY(check_ptr(dW, dtype_size(dtype), "dW"));
+    if (dbias) FTK_TRY(check_ptr(dbias, 4, "dbias"));
+    const XentPlan p = plan_xent(dtype, N, V, D, true, rows_direct(dtype, W, ldw, D));
+    FTK_TRY(check_workspace(workspace, workspace_bytes, p.total));
+    FTK_TRY(check_device());
+    const XentCall c{X, W, ldx, N, ldw, V, D, bias, (float)scale, labels, (uint8_t *)workspace, p, (hipStream_t)hip_stream};
+    switch (dtype) {
+    case FTK_F32: return xent_backward<float, __bf16, 3>(c, lse, dloss, (float *)dX, lddx, (float *)dW, lddw, dbias);
+    case FTK_BF16: return xent_backward<__bf16, __bf16, 1>(c, lse, dloss, (__bf16 *)dX, lddx, (__bf16 *)dW, lddw, dbias);
+    default: return xent_backward<_Float16, _Float16, 1>(c, lse, dloss, (_Float16 *)dX, lddx, (_Float16 *)dW, lddw, dbias);
+    }
+}
+
+}  // extern "C"

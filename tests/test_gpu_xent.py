@@ -1,0 +1,244 @@
+"""Softmax cross entropy over many classes and its gradients against the formulas in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2408_01391_amd import binding as ftk
+from tests.gpu_util import DEV
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+INF = float("inf")
+
+
+def problem(N, V, D, dtype, bias=False, seed=0, spread=2.0):
+    g = torch.Generator(device=DEV).manual_seed(seed + N + V + D)
+    X = torch.randn(N, D, generator=g, device=DEV).to(TYPES[dtype])
+    W = (torch.randn(V, D, generator=g, device=DEV) * spread * D ** -0.5).to(TYPES[dtype])
+    labels = torch.randint(0, V, (N,), generator=g, device=DEV, dtype=torch.int32)
+    if N > 3:
+        labels[::7] = torch.tensor([-1, V, -5, 2 ** 31 - 1], dtype=torch.int32, device=DEV).repeat(N)[:labels[::7].numel()]
+    b = torch.randn(V, generator=g, device=DEV) if bias else None
+    dloss = torch.randn(N, generator=g, device=DEV) * (64.0 if dtype == "f16" else 1.0) / max(N, 1)
+    return X, W, labels, b, dloss
+
+
+def formulas(X, W, labels, b, dloss, scale):
+    """loss, lse, dX, dW, dbias in 64 bits, and of each the sum of its terms' magnitudes (of loss and lse: the largest logit's)."""
+    V = W.shape[0]
+    live = (labels >= 0) & (labels < V)
+    x, w = torch.where(live.unsqueeze(1), X, 0).double(), W.double()
+    bias = torch.zeros(V, dtype=torch.float64, device=DEV) if b is None else b.double()
+    z = scale * (x @ w.t()) + bias
+    size = (abs(scale) * (x.abs() @ w.abs().t()) + torch.where(bias.isfinite(), bias.abs(), 0)).amax(1)
+    lse = torch.logsumexp(z, 1)
+    at = torch.where(live, labels, 0).long().unsqueeze(1)
+    loss = torch.where(live, lse - z.gather(1, at).squeeze(1), 0)
+    p = torch.exp(z - lse.unsqueeze(1))
+    one = torch.zeros_like(p).scatter_(1, at, 1.0)
+    g = torch.where(live, dloss.double(), 0).unsqueeze(1)
+    d, dsize = g * (p - one), g.abs() * (p + one)
+    return ((loss, torch.where(live, lse, 0), scale * (d @ w), scale * (d.t() @ x), d.sum(0)),
+            (size, abs(scale) * (dsize @ w.abs()), abs(scale) * (dsize.t() @ x.abs()), dsize.sum(0)))
+
+
+def check(X, W, labels, b, dloss, scale=1.0, **outs):
+    (loss, lse, dX, dW, db), (size, sX, sW, sb) = formulas(X, W, labels, b, dloss, scale)
+    N, D = X.shape
+    V, t = W.shape[0], X.dtype
+    half, one = HALF[t], 2.0 ** -24
+    # logits: D products added in 32 bits (six times as many where 32-bit rows go by pieces, which leave out 2^-23 of them besides),
+    # a product and a sum; the exponent's two roundings are of their size too
+    terms = D * (6 if t == torch.float32 else 1) + 8
+    off = (terms * one * size + 2.0 ** -20) * 1.0
+    got = ftk.xent(X, W, labels, bias=b, scale=scale)
+    for mine, want in zip(got, (loss, lse)):
+        # and V terms' sum: by lanes and tiles, each term through less than 300 additions
+        assert ((mine.double() - want).abs() <= 2 * off + 300 * one + 4 * one * want.abs()).all()
+    live = (labels >= 0) & (labels < V)
+    assert (got[0][~live] == 0).all() and (got[1][~live] == 0).all()
+    grads = ftk.xent_grad(X, W, labels, got[1], dloss, bias=b, scale=scale, need=(True, True, True), **outs)
+    worst = float(off.max()) * 3 + 300 * one
+    # d is off by the logits' error and by its rounding (to 24 bits by pieces; fp16: a half step of 2^-24 of the largest dloss, 2^14
+    # times as large, at the least), then come sums over V classes or N rows, and the rounding of the result
+    rounding = 2.0 ** -22 if t == torch.float32 else half
+    top = float(torch.where(live, dloss.abs(), 0).max()) if N else 0.0
+    for mine, want, s, n, scaled in ((grads[0], dX, sX, V, W), (grads[1], dW, sW, N, X)):
+        n = n * (6 if t == torch.float32 else 1) + 8
+        tiny = 0.0
+        if t == torch.float16:
+            tiny = 2.0 ** -25 + top * 2.0 ** -38 * n * float(torch.where(scaled.isfinite(), scaled.abs(), 0).max()) * abs(scale)
+        assert ((mine.double() - want).abs() <= (worst + rounding + n * one) * s + 1.01 * half * want.abs() + tiny + 1e-37).all()
+    assert ((grads[2].double() - db).abs() <= (worst + (N + 8) * one) * sb + one * db.abs() + 1e-37).all()
+    return got, grads
+
+
+SIZES = [(1, 1, 1), (1, 2, 8), (1, 1000, 64), (3, 65, 72), (5, 700, 129), (16, 513, 40), (63, 64, 64), (65, 127, 200), (130, 300, 96),
+         (257, 259, 136), (700, 1100, 64), (40, 5000, 256)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,V,D", SIZES)
+def test_loss_and_gradients(N, V, D, dtype):
+    check(*problem(N, V, D, dtype, bias=V % 2 == 1))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,V,D,rows,cols", [(2500, 4000, 256, 256, 256), (1200, 2100, 320, 128, 128)])
+def test_large_tiles(N, V, D, rows, cols, dtype):
+    check(*problem(N, V, D, dtype, bias=True))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_pieces_of_the_classes(dtype):
+    """So many rows that the classes go in several pieces: gradients of the rows are added up over them."""
+    check(*problem(12000, 9000, 72, dtype, bias=True))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D,ldx,ldw,shift", [(64, 80, 72, 8), (64, 64, 67, 0), (33, 40, 50, 1), (40, 41, 40, 3), (1, 3, 5, 1)])
+def test_strides_and_addresses(D, ldx, ldw, shift, dtype):
+    """Rows of wider arrays, NaN between and around them, at addresses of every alignment; results likewise."""
+    N, V, t = 90, 140, TYPES[dtype]
+    X, W, labels, b, dloss = problem(N, V, D, dtype, bias=True)
+
+    def inside(a, ld):
+        wide = torch.full((a.shape[0] * ld + shift + ld,), float("nan"), dtype=t, device=DEV)
+        view = wide[shift:shift + a.shape[0] * ld].view(-1, ld)[:, :D]
+        view.copy_(a)
+        return wide, view
+
+    (_, x), (_, w), (around, dX), (beside, dW) = inside(X, ldx), inside(W, ldw), inside(0 * X, ldx), inside(0 * W, ldw)
+    got, grads = check(x, w, labels, b, dloss, scale=0.7, dX=dX, dW=dW)
+    assert grads[0] is dX and grads[1] is dW
+    assert int(around.isnan().sum()) == around.numel() - N * D and int(beside.isnan().sum()) == beside.numel() - V * D
+    plain = ftk.xent(X, W, labels, bias=b, scale=0.7)
+    assert torch.equal(plain[0], got[0]) and torch.equal(plain[1], got[1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_ignored_rows_are_not_looked_at(dtype):
+    X, W, labels, b, dloss = problem(200, 333, 64, dtype)
+    live = (labels >= 0) & (labels < 333)
+    clean = ftk.xent(X, W, labels), ftk.xent_grad(X, W, labels, ftk.xent(X, W, labels)[1], dloss)
+    X[~live] = float("nan")
+    dloss = torch.where(live, dloss, INF)
+    loss, lse = ftk.xent(X, W, labels)
+    assert torch.equal(loss, clean[0][0]) and torch.equal(lse, clean[0][1])
+    dX, dW, db = ftk.xent_grad(X, W, labels, lse, dloss)
+    assert torch.equal(dX, clean[1][0]) and torch.equal(dW, clean[1][1]) and db is None
+    assert (dX[~live] == 0).all()
+    none = torch.full_like(labels, -1)
+    loss, lse = ftk.xent(X, W, none)
+    assert (loss == 0).all()
+    assert all((t == 0).all() for t in ftk.xent_grad(X, W, none, lse, dloss, need=(True, True, True)))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_closed_classes_and_bad_values(dtype):
+    X, W, labels, b, dloss = problem(60, 200, 64, dtype, bias=True)
+    b[::3] = -INF
+    labels = torch.where(labels % 3 == 0, labels + 1, labels)  # (all in range: 199 % 3 == 1)
+    check(X, W, labels, b, dloss)
+    labels[4] = 3  # a closed class
+    loss, lse = ftk.xent(X, W, labels, bias=b)
+    assert loss[4] == INF and lse[4].isfinite()
+    dX, dW, db = ftk.xent_grad(X, W, labels, lse, dloss, bias=b)
+    assert dX.isfinite().all() and dW.isfinite().all() and db.isfinite().all()
+    loss, lse = ftk.xent(X, W, labels, bias=torch.full_like(b, -INF))
+    live = (labels >= 0) & (labels < 200)
+    assert (lse[live] == -INF).all() and loss[live].isnan().all()
+    X[9] = float("nan")
+    labels[9] = 1
+    loss, lse = ftk.xent(X, W, labels, bias=b)
+    assert loss[9].isnan() and int(loss.isnan().sum()) == 1
+    dX, dW, db = ftk.xent_grad(X, W, labels, lse, dloss, bias=b)
+    assert dX[9].isnan().all() and int(dX.isnan().any(1).sum()) == 1 and db.isnan().any()
+
+
+def test_large_logits():
+    """Logits of some thousands: nothing overflows, the loss is their difference."""
+    X, W, labels, b, dloss = problem(50, 300, 64, "bf16", spread=800.0)
+    check(X, W, labels, b, dloss)
+
+
+def test_assignment_scores():
+    """With minus half the squared norms as bias the likeliest class is the assignment's label."""
+    g = torch.Generator(device=DEV).manual_seed(2)
+    C = torch.randn(50, 24, generator=g, device=DEV)
+    X = C[torch.randint(50, (400,), generator=g, device=DEV)] + 0.2 * torch.randn(400, 24, generator=g, device=DEV)
+    labels, dist = ftk.kmeans_assign(X, C)
+    bias = -0.5 * C.square().sum(1)
+    loss, lse = ftk.xent(X, C, labels, bias=bias)
+    score = (X.double() @ C.double().t() + bias).gather(1, labels.long().unsqueeze(1)).squeeze(1)
+    assert ((lse - loss).double() - score).abs().max() < 1e-4
+    # raising the rows along the gradient lowers the loss: a step of the descent reaches what its slope says
+    dX, _, _ = ftk.xent_grad(X, C, labels, lse, torch.ones(400, device=DEV), bias=bias, need=(True, False, False))
+    again, _ = ftk.xent((X - 1e-3 * dX).contiguous(), C, labels, bias=bias)
+    slope = dX.double().square().sum(1) * 1e-3
+    assert ((loss - again).double() - slope).abs().max() < 0.05 * float(slope.max()) + 1e-5
+
+
+def test_parts_and_no_rows():
+    X, W, labels, b, dloss = problem(70, 90, 40, "bf16", bias=True)
+    loss, lse = ftk.xent(X, W, labels, bias=b)
+    whole = ftk.xent_grad(X, W, labels, lse, dloss, bias=b)
+    for need in ((True, False, False), (False, True, False), (False, False, True)):
+        part = ftk.xent_grad(X, W, labels, lse, dloss, bias=b, need=need)
+        for n, a, c in zip(need, part, whole):
+            assert torch.equal(a, c) if n else a is None
+    empty = ftk.xent(X[:0], W, labels[:0])
+    assert empty[0].shape == (0,)
+    dX, dW, db = ftk.xent_grad(X[:0], W, labels[:0], lse[:0], dloss[:0], bias=b)
+    assert dX.shape == (0, 40) and (dW == 0).all() and (db == 0).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_graph(dtype):
+    """Both directions captured once, replayed on other operands with eager calls between; the workspace holds NaN before."""
+    N, V, D = 300, 700, 72
+    X, W, labels, b, dloss = problem(N, V, D, dtype, bias=True)
+    code = ftk._MX_DTYPES[X.dtype]
+    ws = [torch.full((ftk.xent_workspace_bytes(code, N, V, D, grad) // 4 + 64,), float("nan"), device=DEV) for grad in (False, True)]
+
+    def step():
+        loss, lse = ftk.xent(X, W, labels, bias=b, workspace=ws[0])
+        return (loss, lse, *ftk.xent_grad(X, W, labels, lse, dloss, bias=b, workspace=ws[1]))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for turn in range(3):
+        x, w, l, bb, dl = problem(N, V, D, dtype, bias=True, seed=10 + turn)
+        for to, new in zip((X, W, labels, b, dloss), (x, w, l, bb, dl)):
+            to.copy_(new)
+        graph.replay()
+        torch.cuda.synchronize()
+        kept = [t.clone() for t in held]
+        loss, lse = ftk.xent(x, w, l, bias=bb)
+        for a, c in zip(kept, (loss, lse, *ftk.xent_grad(x, w, l, lse, dl, bias=bb))):
+            assert torch.equal(a, c)
+
+
+def test_refusals():
+    X, W, labels, b, dloss = problem(10, 12, 16, "f32", bias=True)
+    _, lse = ftk.xent(X, W, labels)
+    for call in (lambda: ftk.xent(X, W[:, :8], labels), lambda: ftk.xent(X, W.bfloat16(), labels), lambda: ftk.xent(X, W, labels.long()),
+                 lambda: ftk.xent(X, W, labels[:5]), lambda: ftk.xent(X, W, labels, bias=b[:5]), lambda: ftk.xent(X.t(), W.t(), labels),
+                 lambda: ftk.xent_grad(X, W, labels, lse[:4], dloss), lambda: ftk.xent_grad(X, W, labels, lse, dloss.double()),
+                 lambda: ftk.xent_grad(X, W, labels, lse, dloss, dX=W)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(TypeError):
+        ftk.xent(X.double(), W.double(), labels)
+    with pytest.raises(ftk.FtkError):
+        ftk.xent(X, W, labels, scale=INF)
+    with pytest.raises(ftk.FtkError):
+        ftk.xent(X, W, labels, workspace=torch.empty(300, dtype=torch.uint8, device=DEV))
