@@ -42,6 +42,7 @@ struct Product {
     int64_t mt, nt;
     int stages;  // of a segment
     int segments;  // 1, or 6: products of pieces
+    int splits;  // workgroups that share a tile's stages out between them
 };
 
 template <int MT_, int NT_, int WM_, int WN_>
@@ -56,6 +57,7 @@ struct Place {
     int64_t m0, n0;  // of the tile
     int wm, wn;      // of the wave within it
     int64_t mtile, ntile;
+    int split;
 };
 
 // Row of row tile i, and column of column tile j, that lane row r (of 16) has.  Two column tiles give a lane eight consecutive
@@ -171,10 +173,9 @@ __device__ __forceinline__ int plane_b(int segments, int g) { return segments ==
 
 // Workgroups are dealt to the eight XCDs in turn; each XCD gets a run of tiles, eight rows of tiles high, so that the 32 tiles
 // under way there share their operands in its L2.
-__device__ __forceinline__ void tile_of(const Product &g, int64_t &mtile, int64_t &ntile)
+__device__ __forceinline__ void tile_of(const Product &g, int64_t t, int64_t &mtile, int64_t &ntile)
 {
     const int64_t all = g.mt * g.nt, each = (all + 7) / 8;
-    int64_t t = blockIdx.x;
     const int64_t x = t & 7, full = all & 7;  // the first `full` XCDs have one more where all is no multiple
     t = full ? x * (each - 1) + min(x, full) + (t >> 3) : x * each + (t >> 3);
     const int64_t panel = t / (8 * g.nt), in = t - panel * 8 * g.nt, high = min((int64_t)8, g.mt - panel * 8);
@@ -189,7 +190,8 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product g, End e
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Place at;
-    tile_of(g, at.mtile, at.ntile);
+    at.split = (int)(blockIdx.x / (g.mt * g.nt));
+    tile_of(g, blockIdx.x - at.split * (g.mt * g.nt), at.mtile, at.ntile);
     at.m0 = at.mtile * S::TM;
     at.n0 = at.ntile * S::TN;
     at.wm = w / S::WN * 16 * S::MT;
@@ -203,8 +205,9 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product g, End e
     Copies<S::TN, S::WAVES, BT, true> cb;
     ca.begin(g.a, at.m0, w, lane);
     cb.begin(g.b, at.n0, w, lane);
-    const int total = g.stages * g.segments;
-    int seg = 0, st = 0;  // of the next copy
+    const int64_t all = (int64_t)g.stages * g.segments;
+    const int begin = (int)(all * at.split / g.splits), total = (int)(all * (at.split + 1) / g.splits) - begin;
+    int seg = begin / g.stages, st = begin - seg * g.stages;  // of the next copy
     auto copy = [&](int buffer) __attribute__((always_inline)) {
         const uint32_t to = lds0 + buffer * S::STAGE;
         ca.copy(g.a, plane_a(g.segments, seg), st, g.stages, to, w, lane);
@@ -214,7 +217,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product g, End e
             ++seg;
         }
     };
-    copy(0);
+    if (total > 0) copy(0);
     for (int n = 0; n < total; ++n) {
         // stage n has arrived, and the one before it is read, in all waves
         wait_loads<0>();
@@ -427,12 +430,21 @@ struct GradEnd {
     }
 };
 
-__global__ __launch_bounds__(256) void dbias_kernel(const float *parts, int64_t ld, int64_t tiles, int64_t n, float *out)
+// 64 classes a workgroup, a sixteenth of the row tiles a wave.
+__global__ __launch_bounds__(1024) void dbias_kernel(const float *__restrict__ parts, int64_t ld, int tiles, int64_t n, float *out)
 {
-    const int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (v >= n) return;
+    __shared__ double sums[16][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t v = (int64_t)blockIdx.x * 64 + lane;
     double s = 0;
-    for (int64_t t = 0; t < tiles; ++t) s += parts[t * ld + v];
+    if (v < n) {
+#pragma unroll 8
+        for (int t = w; t < tiles; t += 16) s += parts[t * ld + v];
+    }
+    sums[w][lane] = s;
+    __syncthreads();
+    if (w || v >= n) return;
+    for (int i = 1; i < 16; ++i) s += sums[i][lane];
     out[v] = (float)s;
 }
 
@@ -511,6 +523,39 @@ struct StoreEnd {
     }
 };
 
+// Sums of a share of the stages, [splits][rows][cols].
+struct PartEnd {
+    float *parts;
+    int64_t rows, cols;
+    template <typename S, bool AT>
+    __device__ __forceinline__ void run(float4v (&acc)[S::MT][S::NT], const Place &at, uint8_t *lds) const
+    {
+        StoreEnd<float>{parts + at.split * rows * cols, cols, rows, cols, nullptr, 0, true, true, 1.f, nullptr}.template run<S, AT>(acc, at, lds);
+    }
+};
+// All shares together, and what StoreEnd does.
+template <typename T>
+__global__ __launch_bounds__(256) void join_kernel(const float *__restrict__ parts, int splits, StoreEnd<T> end)
+{
+    const int64_t all = end.rows * end.cols;
+    const float f = end.scale / factor_of(end.top);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        float s = 0.f;
+#pragma unroll 4
+        for (int k = 0; k < splits; ++k) s += parts[k * all + i];
+        const int64_t m = i / end.cols, n = i - m * end.cols;
+        if (end.sums) {
+            float *const sum = end.sums + m * end.lds + n;
+            if (!end.first) s += *sum;
+            if (!end.last) {
+                *sum = s;
+                continue;
+            }
+        }
+        end.out[m * end.ld + n] = (T)(s * f);
+    }
+}
+
 // Rows to whole lines of 64 elements (three bf16 pieces where PLANES is 3), zeros beyond the row and in rows that are not looked at:
 // those whose label lies outside [0, V), and those from N on.
 template <typename T, typename H, int PLANES>
@@ -566,7 +611,11 @@ struct XentPlan {
     int Dp;           // D rounded up to whole stages
     int64_t width;    // classes of a piece
     int64_t tiles;    // column tiles of the logits' sums, all classes
-    size_t X, W, parts, label_logit, d, sums, dbias, top, total;
+    // how products are cut: logits (or d), the rows' gradients, the classes'
+    struct Cut {
+        int tile, splits;
+    } logits, rows_grad, classes_grad;
+    size_t X, W, parts, label_logit, d, sums, shares, dbias, top, total;
 };
 
 using Large = Shape<8, 4, 2, 4>;   // 256 x 256, eight waves
@@ -579,7 +628,34 @@ static bool rows_direct(ftk_dtype dtype, const void *p, int64_t ld, int D)
     return dtype != FTK_F32 && (uintptr_t)p % 16 == 0 && ld % 8 == 0 && D % 8 == 0 && ld < XENT_MAX_LD;
 }
 
-// `direct` false: as much as any address and stride of W may need.
+// How a product of rows x cols over so many stages of k is cut: the shape of the tiles, and shares of the stages where there are few.
+// In microseconds: a stage of a tile of 256, 128 or 64 takes 1.85, 0.65 or 0.5 with a compute unit for itself, 1.1 and 0.85 where
+// two and four share one, and begin and end take some more; joining shares is a launch and moves them once.
+static XentPlan::Cut cut_of(int64_t rows, int64_t cols, int64_t stages, bool shares)
+{
+    static const struct {
+        int tile, at_once;
+        double ends, alone, shared;
+    } shapes[] = {{256, 1, 7, 1.85, 1.85}, {128, 2, 5, 0.65, 0.55}, {64, 4, 4, 0.5, 0.21}};
+    XentPlan::Cut best{64, 1};
+    double least = 1e300;
+    for (const auto &s : shapes) {
+        const int64_t tiles = ceil_div(rows, s.tile) * ceil_div(cols, s.tile);
+        for (int splits = 1; splits <= (shares ? 64 : 1) && splits * 4 - 3 <= stages; splits *= 2) {
+            if (splits > 1 && tiles * splits > 256 * s.at_once) break;
+            const int64_t groups = ceil_div(tiles * splits, 256);  // of a compute unit
+            const double each = groups < s.at_once ? groups : s.at_once, stage = s.shared * each > s.alone ? s.shared * each : s.alone;
+            const double t = (double)ceil_div(groups, s.at_once) * (s.ends + (double)ceil_div(stages, splits) * stage) +
+                             (splits > 1 ? 5 + (double)rows * cols * (splits * 8 + 4) / 4e6 : 0);
+            if (t < least) {
+                least = t;
+                best = {s.tile, splits};
+            }
+        }
+    }
+    return best;
+}
+
 static XentPlan plan_xent(ftk_dtype dtype, int64_t N, int64_t V, int D, bool grad, bool direct)
 {
     XentPlan p;
@@ -588,7 +664,7 @@ static XentPlan plan_xent(ftk_dtype dtype, int64_t N, int64_t V, int D, bool gra
     p.rows = ceil_div(N > 0 ? N : 1, XENT_STAGE) * XENT_STAGE;  // (without rows gradients are zeros)
     p.Dp = (int)(ceil_div(D, XENT_STAGE) * XENT_STAGE);
     // d, or the packed rows of W, of a piece: about 128 MB, which the memory-side cache holds
-    const int64_t rows = grad && p.rows > p.Dp ? p.rows : p.Dp;
+    const int64_t rows = direct ? p.rows : grad && p.rows > p.Dp ? p.rows : p.Dp;
     int64_t width = (64ll << 20) / p.planes / rows / 256 * 256;
     width = width < 256 ? 256 : width;
     const int64_t whole = ceil_div(V, 256) * 256;
@@ -603,12 +679,19 @@ static XentPlan plan_xent(ftk_dtype dtype, int64_t N, int64_t V, int D, bool gra
         at += align_up(bytes, 256);
         return a;
     };
+    const int64_t segments = p.planes == 3 ? 6 : 1, classes = p.width < V ? p.width : V;
+    p.logits = cut_of(grad ? p.rows : N, classes, p.Dp / XENT_STAGE * segments, false);
+    p.rows_grad = cut_of(p.rows, D, ceil_div(classes, XENT_STAGE) * segments, true);
+    p.classes_grad = cut_of(classes, D, p.rows / XENT_STAGE * segments, true);
     p.X = take((size_t)p.planes * p.rows * p.Dp * 2);
     p.W = direct ? at : take((size_t)p.planes * p.width * p.Dp * 2);
-    p.parts = p.label_logit = p.d = p.sums = p.dbias = p.top = at;
+    p.parts = p.label_logit = p.d = p.sums = p.shares = p.dbias = p.top = at;
     if (grad) {
         p.d = take((size_t)p.planes * p.rows * p.width * 2);
         p.sums = dtype == FTK_F32 ? at : take((size_t)N * D * 4);
+        const size_t rs = p.rows_grad.splits > 1 ? (size_t)p.rows_grad.splits * N * D * 4 : 0;
+        const size_t cs = p.classes_grad.splits > 1 ? (size_t)p.classes_grad.splits * classes * D * 4 : 0;
+        p.shares = take(rs > cs ? rs : cs);
         p.dbias = take((size_t)ceil_div(p.rows, XENT_TILE) * p.width * 4);
         p.top = take(256);
     } else {
@@ -624,33 +707,36 @@ static ftk_status launch_shape(Product g, const End &end, hipStream_t st)
 {
     g.mt = ceil_div(g.a.outer, S::TM);
     g.nt = ceil_div(g.b.outer, S::TN);
-    if (g.mt * g.nt > 0x7fffffffLL) {
+    if (g.mt * g.nt * g.splits > 0x7fffffffLL) {
         set_error("too many tiles: %lld x %lld", (long long)g.mt, (long long)g.nt);
         return FTK_EINVAL;
     }
     FTK_TRY(allow_lds<S::LDS>((const void *)product_kernel<S, H, AT, BT, End>));
-    product_kernel<S, H, AT, BT, End><<<(unsigned)(g.mt * g.nt), S::THREADS, S::LDS, st>>>(g, end);
+    product_kernel<S, H, AT, BT, End><<<(unsigned)(g.mt * g.nt * g.splits), S::THREADS, S::LDS, st>>>(g, end);
     FTK_TRY_HIP(hipGetLastError());
     return FTK_OK;
 }
 
-// Time of a shape's tiles in some unit: so many run at once, each takes what its stages take and an end.
-static double shape_cost(const Product &g, int tm, int tn, int at_once, double end, double stage)
-{
-    return (double)ceil_div(ceil_div(g.a.outer, tm) * ceil_div(g.b.outer, tn), at_once) * (end + g.stages * g.segments * stage);
-}
-static int shape_of(const Product &g)
-{
-    const double large = shape_cost(g, 256, 256, 256, 6, 1.0), middle = shape_cost(g, 128, 128, 512, 4, 0.6),
-                 small = shape_cost(g, 64, 64, 1024, 3, 0.4);
-    return large <= middle && large <= small ? 256 : middle <= small ? 128 : 64;
-}
 template <typename H, bool AT, bool BT, typename End>
 static ftk_status launch_product(const Product &g, int tile, const End &end, hipStream_t st)
 {
     if (tile == 256) return launch_shape<Large, H, AT, BT>(g, end, st);
     if (tile == 128) return launch_shape<Middle, H, AT, BT>(g, end, st);
     return launch_shape<Small, H, AT, BT>(g, end, st);
+}
+
+// A gradient's product, in shares where it is cut into them.
+template <typename H, bool AT, typename T>
+static ftk_status launch_gradient(Product g, const XentPlan::Cut &cut, const StoreEnd<T> &end, float *shares, hipStream_t st)
+{
+    g.splits = cut.splits;
+    if (cut.splits == 1) return launch_product<H, AT, true>(g, cut.tile, end, st);
+    FTK_TRY((launch_product<H, AT, true>(g, cut.tile, PartEnd{shares, end.rows, end.cols}, st)));
+    const int64_t groups = ceil_div(end.rows * end.cols, 256);
+    if (groups == 0) return FTK_OK;
+    join_kernel<T><<<(unsigned)(groups < 2048 ? groups : 2048), 256, 0, st>>>(shares, cut.splits, end);
+    FTK_TRY_HIP(hipGetLastError());
+    return FTK_OK;
 }
 
 template <typename T, typename H, int PLANES>
@@ -703,9 +789,8 @@ static ftk_status xent_forward(const XentCall &c, float *loss, float *lse)
     g.a = Operand{x, p.Dp, p.rows * p.Dp, c.N, p.Dp};
     g.stages = p.Dp / XENT_STAGE;
     g.segments = PLANES == 3 ? 6 : 1;
-    // one shape for all pieces: a part stands for as many columns everywhere
-    g.b.outer = p.width < c.V ? p.width : c.V;
-    const int tile = shape_of(g);
+    g.splits = 1;
+    const int tile = p.logits.tile;
     const int64_t tiles = ceil_div(c.V, tile);
     for (int64_t first = 0; first < c.V; first += p.width) {
         const int64_t n = c.V - first < p.width ? c.V - first : p.width;
@@ -726,7 +811,7 @@ static ftk_status xent_backward(const XentCall &c, const float *lse, const float
     const XentPlan &p = c.p;
     uint16_t *x = (uint16_t *)(c.ws + p.X), *d = (uint16_t *)(c.ws + p.d);
     uint32_t *top = std::is_same<T, _Float16>::value ? (uint32_t *)(c.ws + p.top) : nullptr;
-    float *parts = (float *)(c.ws + p.dbias);
+    float *parts = (float *)(c.ws + p.dbias), *shares = (float *)(c.ws + p.shares);
     FTK_TRY((launch_pack<T, H, PLANES>((const T *)c.X, c.ldx, c.N, c.D, p.rows, p.Dp, c.labels, c.V, x, top, c.st)));
     if (top) {
         const int64_t groups = ceil_div(c.N, 1024);
@@ -739,28 +824,28 @@ static ftk_status xent_backward(const XentCall &c, const float *lse, const float
         const int64_t plane = p.rows * p.width;
         Operand along, across;
         FTK_TRY((c.classes<T, H, PLANES>(first, n, along, across)));
-        Product g{Operand{x, p.Dp, p.rows * p.Dp, p.rows, p.Dp}, along, 0, 0, p.Dp / XENT_STAGE, segments};
-        const int tile = shape_of(g);
+        Product g{Operand{x, p.Dp, p.rows * p.Dp, p.rows, p.Dp}, along, 0, 0, p.Dp / XENT_STAGE, segments, 1};
+        const int tile = p.logits.tile;
         const GradEnd<H, PLANES> grad{Logits{c.bias, c.labels, c.N, first, first + n, c.V, c.scale}, lse, dloss, top, d, p.width, plane,
                                       p.rows, dbias ? parts : nullptr};
         FTK_TRY((launch_product<H, false, false>(g, tile, grad, c.st)));
         if (dbias) {
-            dbias_kernel<<<(unsigned)ceil_div(n, 256), 256, 0, c.st>>>(parts, p.width, ceil_div(p.rows, tile), n, dbias + first);
+            dbias_kernel<<<(unsigned)ceil_div(n, 64), 1024, 0, c.st>>>(parts, p.width, (int)ceil_div(p.rows, tile), n, dbias + first);
             FTK_TRY_HIP(hipGetLastError());
         }
         if (dX) {
-            Product r{Operand{d, p.width, plane, p.rows, np}, across, 0, 0, (int)(np / XENT_STAGE), segments};
+            Product r{Operand{d, p.width, plane, p.rows, np}, across, 0, 0, (int)(np / XENT_STAGE), segments, 1};
             const bool one = p.width >= c.V;
             // (in 32 bits dX itself holds them)
             float *sums = one ? nullptr : PLANES == 3 ? (float *)dX : (float *)(c.ws + p.sums);
             StoreEnd<T> end{dX, lddx, c.N, c.D, sums, PLANES == 3 ? lddx : c.D, first == 0, first + n == c.V, c.scale, top};
-            FTK_TRY((launch_product<H, false, true>(r, shape_of(r), end, c.st)));
+            FTK_TRY((launch_gradient<H, false>(r, p.rows_grad, end, shares, c.st)));
         }
         if (dW) {
             Product r{Operand{d, p.width, plane, np, p.rows}, Operand{x, p.Dp, p.rows * p.Dp, p.Dp, p.rows}, 0, 0,
-                      (int)(p.rows / XENT_STAGE), segments};
+                      (int)(p.rows / XENT_STAGE), segments, 1};
             StoreEnd<T> end{dW + first * lddw, lddw, n, c.D, nullptr, 0, true, true, c.scale, top};
-            FTK_TRY((launch_product<H, true, true>(r, shape_of(r), end, c.st)));
+            FTK_TRY((launch_gradient<H, true>(r, p.classes_grad, end, shares, c.st)));
         }
     }
     return FTK_OK;
@@ -804,7 +889,9 @@ int64_t ftk_xent_workspace_bytes(ftk_dtype dtype, int64_t N, int64_t V, int32_t 
         set_error("need 0 <= N < 2^31, 1 <= V < 2^31, 1 <= D <= %d (got N=%lld V=%lld D=%d)", XENT_MAX_D, (long long)N, (long long)V, D);
         return -1;
     }
-    return (int64_t)plan_xent(dtype, N, V, D, grad != 0, false).total;
+    // for any address and stride of W
+    const size_t packed = plan_xent(dtype, N, V, D, grad != 0, false).total, direct = plan_xent(dtype, N, V, D, grad != 0, true).total;
+    return (int64_t)(packed > direct ? packed : direct);
 }
 
 ftk_status ftk_xent(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N, const void *W, int64_t ldw, int64_t V, int32_t D,
