@@ -135,6 +135,29 @@ def test_steps(dtype, grads, master, bits, aligned):
                     assert torch.equal(got.cpu(), want.to(dt)), (dt, i, M)
 
 
+def test_states_of_all_magnitudes():
+    """Gradients from 2^-60 to 2^60, block by block and within blocks: codes and scales exactly, twice in a row."""
+    rng = np.random.default_rng(1)
+    n = 32 * 400
+    size = np.repeat(rng.uniform(-60, 60, 400), 32) + rng.uniform(-20, 0, n) * (rng.random(n) < 0.5)
+    g = (rng.standard_normal(n) * 2.0 ** size).astype(np.float32)
+    p = torch.zeros(n, device=DEV)
+    state = ftk.AdamW([p], 8)
+    for t in (1, 2):
+        before = [decode(numpy(c[0]), numpy(s[0]), M) for c, s, M in ((state.m, state.m_scales, 3), (state.v, state.v_scales, 4))]
+        ftk.adamw_step(state, [torch.from_numpy(g).to(DEV)], torch.full((1,), t, dtype=torch.int64, device=DEV), seed=2)
+        with np.errstate(over="ignore"):
+            m, v, _, _ = one_step(np.zeros(n), g, *before, t)
+        r = random32(2, t, 0, n)
+        for codes, scales, x, M, u in ((state.m, state.m_scales, m, 3, r >> 16), (state.v, state.v_scales, v, 4, r & 0xFFFF)):
+            want = encode(x, M, u / 65536.0)
+            assert np.array_equal(numpy(scales[0]), want[1]) and np.array_equal(numpy(codes[0]), want[0]), (t, M)
+        g = (g * rng.uniform(-2, 2, n)).astype(np.float32)
+        ms, vs = ftk.adamw_moments(state)
+        assert np.array_equal(numpy(ms[0]), decode(numpy(state.m[0]), numpy(state.m_scales[0]), 3))
+        assert np.array_equal(numpy(vs[0]), decode(numpy(state.v[0]), numpy(state.v_scales[0]), 4))
+
+
 def test_more_tensors_than_a_launch_takes():
     """With tensors left out here and there: those stay, the others keep their place in the list."""
     sizes = [1 + (i * 37) % 300 for i in range(170)]
