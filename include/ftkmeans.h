@@ -446,9 +446,9 @@ ftk_status ftk_mx4_outer(ftk_dtype out_dtype, const void *a_codes, const void *a
  * (a dropped slot of ftk_route_plan) and the weight 0.  A row closed to all takes no part: lse -infinity.  A row with
  * a NaN or +infinity gets labels -1 and NaN weights, and makes probs and loss NaN.
  * Sums are held in 32 bits or more, in an order that N, E, k and dtype set: results are bitwise reproducible.
- * workspace: ftk_route_gate_workspace_bytes(N, E); up to FTK_ROUTE_GATE_FEW rows none is needed: NULL will do.
+ * workspace: ftk_route_gate_workspace_bytes(N, E); up to FTK_ROUTE_GATE_FEW logits (N * E) none is needed: NULL will do.
  * Limits: 1 <= E <= 8192, 1 <= k <= 64, k <= E, N * k < 2^31.  N = 0 is a valid call (T = 0). */
-#define FTK_ROUTE_GATE_FEW 64
+#define FTK_ROUTE_GATE_FEW 16384
 size_t ftk_route_gate_workspace_bytes(int64_t N, int32_t E); /* 0: bad arguments */
 ftk_status ftk_route_gate(ftk_dtype dtype, const void *logits, int64_t ldz, int64_t N, int32_t E, int32_t k, int32_t normalise,
                           int32_t *labels, float *weights, float *lse, int32_t *counts, float *probs, float *loss,

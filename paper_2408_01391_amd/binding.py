@@ -741,7 +741,7 @@ def mx4_outer(A, B, route=None, out=None, out_dtype=torch.float32):
 
 # ---- a gate that learns ----------------------------------------------------------------------
 
-GATE_FEW = 64  # rows that need no workspace
+GATE_FEW = 16384  # logits that need no workspace
 
 
 class Gate:
@@ -795,7 +795,7 @@ def route_gate(logits, k, normalise=True, gate=None, workspace=None):
         _index(gate.counts, "counts", E + 1), _floats(gate.probs, "probs", E), _floats(gate.loss, "loss", 1)
         gate.normalise = normalise
     _here(logits, gate.labels, workspace)
-    workspace, wp, wn = _workspace(workspace, route_gate_workspace_bytes(N, E) if N > GATE_FEW else 0, dev)
+    workspace, wp, wn = _workspace(workspace, route_gate_workspace_bytes(N, E) if N * E > GATE_FEW else 0, dev)
     _check(load().ftk_route_gate(code, logits.data_ptr(), ld, N, E, k, 1 if normalise else 0, gate.labels.data_ptr(),
                                  gate.weights.data_ptr(), gate.lse.data_ptr(), gate.counts.data_ptr(), gate.probs.data_ptr(),
                                  gate.loss.data_ptr(), wp, wn, _stream()))
@@ -937,8 +937,10 @@ class AdamW:
                 if need:
                     setattr(row, "param" if name == "params" else name, t.data_ptr())
                     spans.append((t.data_ptr(), t.data_ptr() + need * t.element_size()))
-        for p, row in zip(self.params, self._table):
-            row.count = p.numel()
+        self._counts = [p.numel() for p in self.params]
+        for n, row in zip(self._counts, self._table):
+            row.count = n
+        self._grads = (ctypes.c_uint64 * (8 * len(self.params))).from_buffer(self._table)  # the table by words, the gradient's is the second
         spans.sort()
         if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
             raise ValueError("weights or states overlap")
@@ -949,21 +951,19 @@ def adamw_step(state, grads, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, we
     weights'; float32 weights: any), or None: that weight stays.  step: int64 device tensor of one element, 1 at the first
     step.  lr_scale, grad_scale: float32 device tensors of one element that multiply the rate and the gradients.  seed: of the
     rounding of 8-bit states."""
-    params = state.params
-    if len(grads) != len(params):
-        raise ValueError("%d gradients for %d weights" % (len(grads), len(params)))
-    dtype, device = None, params[0].get_device()
-    for g, p, row in zip(grads, params, state._table):
-        if g is None:
-            row.grad = None
-            continue
-        if dtype is None:
-            dtype = g.dtype
-        if g.dtype != dtype or g.numel() != p.numel() or g.get_device() != device or not g.is_contiguous():
-            raise ValueError("gradients must be contiguous tensors of one type with the weights' elements, on their device")
-        row.grad = g.data_ptr()
-    if dtype is None:
+    given = [g for g in grads if g is not None]
+    counts = state._counts
+    if len(grads) != len(counts):
+        raise ValueError("%d gradients for %d weights" % (len(grads), len(counts)))
+    if not given:
         return
+    if len(given) < len(counts):
+        counts = [n for n, g in zip(counts, grads) if g is not None]
+    dtype, device = given[0].dtype, state.params[0].get_device()
+    if ([g.numel() for g in given] != counts or {g.dtype for g in given} != {dtype} or {g.get_device() for g in given} != {device}
+            or not all([g.is_contiguous() for g in given])):
+        raise ValueError("gradients must be contiguous tensors of one type with the weights' elements, on their device")
+    state._grads[1::8] = [0 if g is None else g.data_ptr() for g in grads]
     code = _MX_DTYPES.get(dtype)
     if code is None:
         raise TypeError("gradients: %s is not one of float32, bfloat16, float16" % dtype)
@@ -972,9 +972,9 @@ def adamw_step(state, grads, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, we
     for t, name in ((lr_scale, "lr_scale"), (grad_scale, "grad_scale")):
         if t is not None and (not t.is_cuda or t.dtype != torch.float32 or t.numel() != 1):
             raise ValueError("%s must be a float32 device tensor of one element" % name)
-    _here(params[0], step, lr_scale, grad_scale)
+    _here(state.params[0], step, lr_scale, grad_scale)
     options = _AdamwOptions(lr, beta1, beta2, eps, weight_decay, _ptr(lr_scale), _ptr(grad_scale), step.data_ptr(), seed & (2**64 - 1))
-    _check(load().ftk_adamw_step(state.code, code, state.bits, state._table, len(params), ctypes.byref(options), _stream()))
+    _check(load().ftk_adamw_step(state.code, code, state.bits, state._table, len(grads), ctypes.byref(options), _stream()))
 
 
 def adamw_moments(state, out=None, dtype=torch.float32):
@@ -983,15 +983,14 @@ def adamw_moments(state, out=None, dtype=torch.float32):
         raise ValueError("states in 32 bits are their own values")
     if out is None:
         out = [[torch.empty_like(p, dtype=dtype) for p in state.params] for _ in range(2)]
-    dtype = out[0][0].dtype
-    lists = []
+    dtype, device, lists = out[0][0].dtype, state.params[0].get_device(), []
     for ts in out:
-        if len(ts) != len(state.params):
-            raise ValueError("out must be two lists of %d tensors" % len(state.params))
-        for t, p in zip(ts, state.params):
-            if t.dtype != dtype or t.numel() != p.numel() or t.get_device() != p.get_device() or not t.is_contiguous():
-                raise ValueError("out must be contiguous tensors of one type with the weights' elements, on their device")
-        lists.append((ctypes.c_void_p * len(ts))(*[t.data_ptr() for t in ts]))
+        if ([t.numel() for t in ts] != state._counts or {t.dtype for t in ts} != {dtype} or {t.get_device() for t in ts} != {device}
+                or not all([t.is_contiguous() for t in ts])):
+            raise ValueError("out must be two lists of contiguous tensors of one type with the weights' elements, on their device")
+        pointers = (ctypes.c_void_p * len(ts))()
+        pointers[:] = [t.data_ptr() for t in ts]
+        lists.append(pointers)
     _here(state.params[0])
     _check(load().ftk_adamw_moments(_row_code(out[0][0], "out", _MX_DTYPES), state._table, len(state.params), lists[0], lists[1], _stream()))
     return out
