@@ -317,6 +317,110 @@ struct SumEnd {
     }
 };
 
+// Few rows (up to 16 MT): what takes time is reading W once.  A workgroup's eight waves share D out between them, RUN steps of 32
+// each, whose part of the rows stays in registers; W goes from memory straight to registers, 16 / RUN / MT column tiles of 16 classes
+// at a time, the next ones requested before these are used.  The waves' sums meet in LDS, where the first waves, one
+// for a tile, take the softmax on.  (16 rows, 65536 classes of 2048 bf16, 268 MB: TODO us.)
+template <typename H, int MT, int RUN>
+__global__ __launch_bounds__(512, 2) void xent_few_kernel(const H *__restrict__ X, int64_t ldx, const H *__restrict__ W, int64_t ldw, int D,
+                                                          SumEnd end)
+{
+    constexpr int CT = 16 / RUN / MT, WAVES = 8;
+    __shared__ float4v part[2][WAVES][CT][MT][64];
+    __shared__ float2 last[CT][MT * 16];
+    const Logits &z = end.z;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
+    typedef H piece __attribute__((ext_vector_type(8), aligned(2)));
+    half8 x[MT][RUN], b[2][CT][RUN];
+    const int k0 = w * RUN * 32 + q * 8;
+    auto request = [&](int64_t v0, half8 (&to)[CT][RUN]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+            const H *row = W + min(v0 + c * 16 + r, z.V - 1) * ldw;
+#pragma unroll
+            for (int s = 0; s < RUN; ++s) to[c][s] = *reinterpret_cast<const half8 *>(row + (k0 + s * 32 < D ? k0 + s * 32 : 0));
+        }
+    };
+    const int64_t step = (int64_t)gridDim.x * 16 * CT;
+    int64_t v0 = (int64_t)blockIdx.x * 16 * CT;
+    request(v0, b[0]);
+    int64_t label[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int64_t n = 16 * i + r;
+        label[i] = n < z.N ? z.labels[n] : -1;
+        const bool live = label[i] >= 0 && label[i] < z.V;
+#pragma unroll
+        for (int s = 0; s < RUN; ++s) {
+            const int k = k0 + s * 32;
+            x[i][s] = half8{0, 0, 0, 0, 0, 0, 0, 0};
+            if (live && k < D) x[i][s] = __builtin_bit_cast(half8, *reinterpret_cast<const piece *>(X + n * ldx + k));
+        }
+    }
+    float2 sum[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) sum[i] = float2{-__builtin_inff(), 0.f};
+    auto tile = [&](half8 (&now)[CT][RUN], half8 (&next)[CT][RUN], int turn) __attribute__((always_inline)) {
+        if (v0 + step < z.V) request(v0 + step, next);
+        float4v acc[CT][MT];
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                acc[c][i] = float4v{0, 0, 0, 0};
+#pragma unroll
+                for (int s = 0; s < RUN; ++s) acc[c][i] = mma<H>(now[c][s], x[i][s], acc[c][i]);
+                part[turn][w][c][i][lane] = acc[c][i];
+            }
+        __syncthreads();
+        if (w < CT) {
+            const int64_t v = v0 + 16 * w + 4 * q;
+            float bias[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) bias[e] = z.bias_of(v + e);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                float4v a = part[turn][0][w][i][lane];
+#pragma unroll
+                for (int k = 1; k < WAVES; ++k) a += part[turn][k][w][i][lane];
+                float top = sum[i].x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    a[e] = v + e < z.V ? fmaf(z.scale, a[e], bias[e]) : -__builtin_inff();
+                    if (v + e == label[i] && v + e < z.V) end.z_store(16 * i + r, a[e]);
+                    top = fmaxf(top, a[e]);
+                }
+                const float shift = top > -__builtin_inff() ? top : 0.f;
+                float t = sum[i].y * exp2_of(sum[i].x - shift);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t += exp2_of(a[e] - shift);
+                sum[i] = float2{top, t};
+            }
+        }
+        v0 += step;
+    };
+    while (v0 < z.V) {
+        tile(b[0], b[1], 0);
+        if (v0 < z.V) tile(b[1], b[0], 1);
+    }
+    if (w < CT) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+#pragma unroll
+            for (int d = 16; d < 64; d *= 2)
+                sum[i] = SumEnd::joined(sum[i], float2{__shfl_xor(sum[i].x, d, 64), __shfl_xor(sum[i].y, d, 64)});
+            if (q == 0) last[w][16 * i + r] = sum[i];
+        }
+    }
+    __syncthreads();
+    const int n = threadIdx.x;
+    if (n >= 16 * MT || n >= z.N) return;
+    float2 p = last[0][n];
+#pragma unroll
+    for (int c = 1; c < CT; ++c) p = SumEnd::joined(p, last[c][n]);
+    end.parts[n * end.tiles + blockIdx.x] = p;
+}
+
 // A wave a row: its parts together.
 __global__ __launch_bounds__(256) void xent_loss_kernel(const float2 *parts, int64_t tiles, const float *label_logit,
                                                         const int32_t *labels, int64_t N, int64_t V, float *loss, float *lse)
@@ -606,6 +710,7 @@ __global__ __launch_bounds__(256) void dloss_top_kernel(const float *dloss, cons
 
 struct XentPlan {
     bool direct;      // W is read where it lies
+    bool few;         // one pass over it for all rows
     int planes;
     int64_t rows;     // N rounded up to whole stages
     int Dp;           // D rounded up to whole stages
@@ -622,6 +727,11 @@ using Large = Shape<8, 4, 2, 4>;   // 256 x 256, eight waves
 using Middle = Shape<4, 4, 2, 2>;  // 128 x 128
 using Small = Shape<2, 2, 2, 2>;   // 64 x 64
 constexpr int XENT_TILE = 64;      // columns that a sum's part stands for at least
+
+constexpr int FEW_GROUPS = 256;    // workgroups of few rows' logits: one a compute unit
+
+// Sums of logits of up to 32 rows (16, where half of D fills the registers).
+static bool few_rows(int64_t N, int D) { return N <= 16 ? D <= 4096 : N <= 32 && D <= 2048; }
 
 static bool rows_direct(ftk_dtype dtype, const void *p, int64_t ld, int D)
 {
@@ -660,6 +770,7 @@ static XentPlan plan_xent(ftk_dtype dtype, int64_t N, int64_t V, int D, bool gra
 {
     XentPlan p;
     p.direct = direct;
+    p.few = !grad && direct && few_rows(N, D);
     p.planes = dtype == FTK_F32 ? 3 : 1;
     p.rows = ceil_div(N > 0 ? N : 1, XENT_STAGE) * XENT_STAGE;  // (without rows gradients are zeros)
     p.Dp = (int)(ceil_div(D, XENT_STAGE) * XENT_STAGE);
@@ -683,6 +794,13 @@ static XentPlan plan_xent(ftk_dtype dtype, int64_t N, int64_t V, int D, bool gra
     p.logits = cut_of(grad ? p.rows : N, classes, p.Dp / XENT_STAGE * segments, false);
     p.rows_grad = cut_of(p.rows, D, ceil_div(classes, XENT_STAGE) * segments, true);
     p.classes_grad = cut_of(classes, D, p.rows / XENT_STAGE * segments, true);
+    if (p.few) {
+        p.tiles = ceil_div(V, 16) < FEW_GROUPS ? ceil_div(V, 16) : FEW_GROUPS;
+        p.parts = take((size_t)N * p.tiles * 8);
+        p.label_logit = take((size_t)N * 4);
+        p.total = at;
+        return p;
+    }
     p.X = take((size_t)p.planes * p.rows * p.Dp * 2);
     p.W = direct ? at : take((size_t)p.planes * p.width * p.Dp * 2);
     p.parts = p.label_logit = p.d = p.sums = p.shares = p.dbias = p.top = at;
@@ -777,14 +895,44 @@ struct XentCall {
     }
 };
 
+static ftk_status launch_loss(const XentCall &c, const SumEnd &end, float *loss, float *lse)
+{
+    xent_loss_kernel<<<(unsigned)ceil_div(c.N, 4), 256, 0, c.st>>>(end.parts, end.tiles, end.label_logit, c.labels, c.N, c.V, loss, lse);
+    FTK_TRY_HIP(hipGetLastError());
+    return FTK_OK;
+}
+
+template <typename H, int MT, int RUN>
+static ftk_status launch_few_shape(const XentCall &c, SumEnd end, float *loss, float *lse)
+{
+    const int64_t tiles = ceil_div(c.V, 16 * (16 / RUN / MT));
+    end.tiles = tiles < FEW_GROUPS ? tiles : FEW_GROUPS;
+    xent_few_kernel<H, MT, RUN><<<(unsigned)end.tiles, 512, 0, c.st>>>((const H *)c.X, c.ldx, (const H *)c.W, c.ldw, c.D, end);
+    FTK_TRY_HIP(hipGetLastError());
+    return launch_loss(c, end, loss, lse);
+}
+template <typename H>
+static ftk_status launch_few(const XentCall &c, const SumEnd &end, float *loss, float *lse)
+{
+    if (c.N > 16) return c.D <= 1024 ? launch_few_shape<H, 2, 4>(c, end, loss, lse) : launch_few_shape<H, 2, 8>(c, end, loss, lse);
+    if (c.D <= 1024) return launch_few_shape<H, 1, 4>(c, end, loss, lse);
+    return c.D <= 2048 ? launch_few_shape<H, 1, 8>(c, end, loss, lse) : launch_few_shape<H, 1, 16>(c, end, loss, lse);
+}
+
 template <typename T, typename H, int PLANES>
 static ftk_status xent_forward(const XentCall &c, float *loss, float *lse)
 {
     const XentPlan &p = c.p;
-    uint16_t *x = (uint16_t *)(c.ws + p.X);
-    FTK_TRY((launch_pack<T, H, PLANES>((const T *)c.X, c.ldx, c.N, c.D, p.rows, p.Dp, c.labels, c.V, x, nullptr, c.st)));
     float2 *parts = (float2 *)(c.ws + p.parts);
     float *label_logit = (float *)(c.ws + p.label_logit);
+    if constexpr (PLANES == 1) {
+        if (p.few) {
+            const SumEnd end{Logits{c.bias, c.labels, c.N, 0, c.V, c.V, c.scale}, parts, 0, 0, label_logit};
+            return launch_few<H>(c, end, loss, lse);
+        }
+    }
+    uint16_t *x = (uint16_t *)(c.ws + p.X);
+    FTK_TRY((launch_pack<T, H, PLANES>((const T *)c.X, c.ldx, c.N, c.D, p.rows, p.Dp, c.labels, c.V, x, nullptr, c.st)));
     Product g;
     g.a = Operand{x, p.Dp, p.rows * p.Dp, c.N, p.Dp};
     g.stages = p.Dp / XENT_STAGE;
@@ -799,9 +947,7 @@ static ftk_status xent_forward(const XentCall &c, float *loss, float *lse)
         const SumEnd end{Logits{c.bias, c.labels, c.N, first, first + n, c.V, c.scale}, parts, tiles, first / tile, label_logit};
         FTK_TRY((launch_product<H, false, false>(g, tile, end, c.st)));
     }
-    xent_loss_kernel<<<(unsigned)ceil_div(c.N, 4), 256, 0, c.st>>>(parts, tiles, label_logit, c.labels, c.N, c.V, loss, lse);
-    FTK_TRY_HIP(hipGetLastError());
-    return FTK_OK;
+    return launch_loss(c, SumEnd{Logits{}, parts, tiles, 0, label_logit}, loss, lse);
 }
 
 template <typename T, typename H, int PLANES>

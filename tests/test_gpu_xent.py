@@ -91,6 +91,14 @@ def test_large_tiles(N, V, D, rows, cols, dtype):
     check(*problem(N, V, D, dtype, bias=True))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("N,V,D", [(1, 17, 1024), (1, 9001, 1032), (2, 4097, 2048), (16, 8200, 2040), (15, 20000, 520), (16, 3000, 4096),
+                                   (9, 5003, 4088), (17, 9000, 1000), (32, 8191, 2048), (31, 12345, 64), (1, 70000, 32)])
+def test_few_rows(N, V, D, dtype):
+    """Rows that stay in registers while the classes pass: one, sixteen, up to thirty-two, and lengths that end within a step."""
+    check(*problem(N, V, D, dtype, bias=V % 2 == 1))
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_pieces_of_the_classes(dtype):
     """So many rows that the classes go in several pieces: gradients of the rows are added up over them."""
