@@ -256,6 +256,14 @@ __device__ __forceinline__ void to_lds16_from(const uint8_t *base, uint32_t offs
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(base) : "memory", "m0");
 }
 
+// A pointer that is the same in all lanes, where the compiler cannot see it.
+__device__ __forceinline__ const uint8_t *uniform(const uint8_t *p)
+{
+    const uint64_t b = (uint64_t)p;
+    return (const uint8_t *)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)b) |
+                             (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) << 32);
+}
+
 // wait until all but the youngest N memory loads, and all LDS accesses, are done
 template <int N>
 __device__ __forceinline__ void wait_loads()

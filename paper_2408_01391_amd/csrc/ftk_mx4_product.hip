@@ -297,14 +297,6 @@ static ftk_status launch_direct(MxProduct a, hipStream_t st)
 __device__ __forceinline__ int place_of_piece(int p) { return (p & 1) * 4 + (p >> 1); }
 __device__ __forceinline__ int piece_at(int place) { return (place & 3) * 2 + (place >> 2); }
 
-// A pointer that is the same in all lanes, where the compiler cannot see it.
-__device__ __forceinline__ const uint8_t *uniform(const uint8_t *p)
-{
-    const uint64_t b = (uint64_t)p;
-    return (const uint8_t *)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)b) |
-                             (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) << 32);
-}
-
 // Many rows: TM = 32 * MT rows by TN = 32 * NT columns a workgroup, a quarter of them a wave.  k goes in stages of 256
 // elements, one 128-byte line of codes a row, copied straight to LDS a stage ahead of their use; scales go two
 // stages (16 bytes a row) at a time.  A stage is two steps of the instruction.  Which 128 of its elements a step takes is

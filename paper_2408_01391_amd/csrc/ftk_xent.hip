@@ -113,25 +113,25 @@ struct Copies {
             }
         }
     }
-    // stage st of a segment's `stages`, from piece `plane` of the rows
-    __device__ __forceinline__ void copy(const Operand &o, int plane, int st, int stages, uint32_t lds, int w, int lane) const
+    // where stage st of a segment begins, for piece `plane` of the rows
+    __device__ __forceinline__ const uint8_t *from(const Operand &o, int plane, int st) const
     {
-        const uint8_t *from = base + plane * o.plane * 2 + st * step;
-        const int64_t left = o.inner - (int64_t)st * XENT_STAGE;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            uint32_t at = off[i];
-            if (left < XENT_STAGE) {
-                const int c = w * N + i;
-                if (ACROSS) {
-                    const int k = k_of(c, lane);
-                    if (k >= left) at -= (uint32_t)(k - (int)left + 1) * (uint32_t)o.ld * 2;
-                } else if (piece_of(c, lane) * 8 >= left) {
-                    at -= piece_of(c, lane) * 16;
-                }
+        return uniform(base + plane * o.plane * 2 + st * step);
+    }
+    // copy i of a stage, of whose elements of k `left` are left
+    __device__ __forceinline__ void copy(const Operand &o, const uint8_t *stage, int left, uint32_t lds, int w, int lane, int i) const
+    {
+        const int c = w * N + i;
+        uint32_t at = off[i];
+        if (left < XENT_STAGE) {
+            if (ACROSS) {
+                const int k = k_of(c, lane);
+                if (k >= left) at -= (uint32_t)(k - left + 1) * (uint32_t)o.ld * 2;
+            } else if (piece_of(c, lane) * 8 >= left) {
+                at -= piece_of(c, lane) * 16;
             }
-            to_lds16_from(from, at, lds + (w * N + i) * 1024);
         }
+        to_lds16_from(stage, at, lds + c * 1024);
     }
 };
 
@@ -208,34 +208,86 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product g, End e
     const int64_t all = (int64_t)g.stages * g.segments;
     const int begin = (int)(all * at.split / g.splits), total = (int)(all * (at.split + 1) / g.splits) - begin;
     int seg = begin / g.stages, st = begin - seg * g.stages;  // of the next copy
-    auto copy = [&](int buffer) __attribute__((always_inline)) {
+    constexpr int COPIES = ca.N + cb.N;
+    const uint8_t *from_a, *from_b;
+    int left_a, left_b;
+    auto aim = [&]() __attribute__((always_inline)) {
+        from_a = ca.from(g.a, plane_a(g.segments, seg), st);
+        from_b = cb.from(g.b, plane_b(g.segments, seg), st);
+        const int64_t k = (int64_t)st * XENT_STAGE;
+        left_a = (int)min((int64_t)XENT_STAGE, g.a.inner - k);
+        left_b = (int)min((int64_t)XENT_STAGE, g.b.inner - k);
+    };
+    auto copy = [&](int buffer, int c) __attribute__((always_inline)) {
         const uint32_t to = lds0 + buffer * S::STAGE;
-        ca.copy(g.a, plane_a(g.segments, seg), st, g.stages, to, w, lane);
-        cb.copy(g.b, plane_b(g.segments, seg), st, g.stages, to + S::A, w, lane);
+        if (c < ca.N) ca.copy(g.a, from_a, left_a, to, w, lane, c);
+        else cb.copy(g.b, from_b, left_b, to + S::A, w, lane, c - ca.N);
+    };
+    auto copied = [&]() __attribute__((always_inline)) {
         if (++st == g.stages) {
             st = 0;
             ++seg;
         }
+        aim();
     };
-    if (total > 0) copy(0);
-    for (int n = 0; n < total; ++n) {
-        // stage n has arrived, and the one before it is read, in all waves
-        wait_loads<0>();
-        __syncthreads();
-        if (n + 1 < total) copy((n + 1) & 1);
-        const uint8_t *const la = lds + (n & 1) * S::STAGE, *const lb = la + S::A;
+    aim();
+    half8 a[S::MT], b[2][S::NT];
+    auto read_a = [&](int n, int s, int i) __attribute__((always_inline)) {
+        a[i] = Fragments<S::TM, AT, false>::read(lds + (n & 1) * S::STAGE, at.wm, i, s, lane);
+    };
+    auto read_b = [&](int n, int s, int j) __attribute__((always_inline)) {
+        b[s][j] = Fragments<S::TN, BT, true>::read(lds + (n & 1) * S::STAGE + S::A, at.wn, j, s, lane);
+    };
+    // One step's products, row tile by row tile.  Behind each the next step's fragments of that number are read, those of the rows
+    // into the registers just used, and a share of the copies is requested.
+    auto step = [&](auto which, auto reads, auto copies, int n) __attribute__((always_inline)) {
+        constexpr int s = decltype(which)::value, next = 1 - s;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            half8 a[S::MT], b[S::NT];
+        for (int i = 0; i < S::MT; ++i) {
 #pragma unroll
-            for (int j = 0; j < S::NT; ++j) b[j] = Fragments<S::TN, BT, true>::read(lb, at.wn, j, s, lane);
+            for (int j = 0; j < S::NT; ++j) acc[i][j] = mma<H>(b[s][j], a[i], acc[i][j]);
+            if constexpr (decltype(reads)::value) {
+                read_a(n + s, next, i);
 #pragma unroll
-            for (int i = 0; i < S::MT; ++i) a[i] = Fragments<S::TM, AT, false>::read(la, at.wm, i, s, lane);
+                for (int j = i * S::NT / S::MT; j < (i + 1) * S::NT / S::MT; ++j) read_b(n + s, next, j);
+            }
+            if constexpr (decltype(copies)::value) {
 #pragma unroll
-            for (int i = 0; i < S::MT; ++i)
-#pragma unroll
-                for (int j = 0; j < S::NT; ++j) acc[i][j] = mma<H>(b[j], a[i], acc[i][j]);
+                for (int c = i * COPIES / S::MT; c < (i + 1) * COPIES / S::MT; ++c) copy(n & 1, c);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
+    };
+    using Zero = std::integral_constant<int, 0>;
+    using One = std::integral_constant<int, 1>;
+    auto stage = [&](auto more, auto copies, int n) __attribute__((always_inline)) {
+        step(Zero{}, One{}, Zero{}, n);
+        // this stage is in registers and the next one has arrived, in all waves: its place is free for the one after that
+        if constexpr (decltype(more)::value) {
+            wait_loads<0>();
+            __syncthreads();
+        }
+        step(One{}, more, copies, n);
+        if constexpr (decltype(copies)::value) copied();
+    };
+    if (total > 0) {
+        for (int n = 0; n < 2 && n < total; ++n) {
+#pragma unroll
+            for (int c = 0; c < COPIES; ++c) copy(n, c);
+            copied();
+            if (n == 0) {
+                wait_loads<0>();
+                __syncthreads();
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < S::NT; ++j) read_b(0, 0, j);
+#pragma unroll
+        for (int i = 0; i < S::MT; ++i) read_a(0, 0, i);
+        int n = 0;
+        for (; n + 2 < total; ++n) stage(One{}, One{}, n);
+        if (n + 1 < total) stage(One{}, Zero{}, n++);
+        stage(Zero{}, Zero{}, n);
     }
     __syncthreads();
     end.template run<S, AT>(acc, at, lds);
