@@ -124,6 +124,7 @@ struct Copies {
         const int c = w * N + i;
         uint32_t at = off[i];
         if (left < XENT_STAGE) {
+            asm volatile("");  // (a branch that is hardly ever taken, rather than its arithmetic every time)
             if (ACROSS) {
                 const int k = k_of(c, lane);
                 if (k >= left) at -= (uint32_t)(k - left + 1) * (uint32_t)o.ld * 2;
@@ -206,7 +207,8 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product g, End e
     ca.begin(g.a, at.m0, w, lane);
     cb.begin(g.b, at.n0, w, lane);
     const int64_t all = (int64_t)g.stages * g.segments;
-    const int begin = (int)(all * at.split / g.splits), total = (int)(all * (at.split + 1) / g.splits) - begin;
+    const int begin = __builtin_amdgcn_readfirstlane((int)(all * at.split / g.splits));
+    const int total = __builtin_amdgcn_readfirstlane((int)(all * (at.split + 1) / g.splits)) - begin;
     int seg = begin / g.stages, st = begin - seg * g.stages;  // of the next copy
     constexpr int COPIES = ca.N + cb.N;
     const uint8_t *from_a, *from_b;
@@ -214,9 +216,8 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product g, End e
     auto aim = [&]() __attribute__((always_inline)) {
         from_a = ca.from(g.a, plane_a(g.segments, seg), st);
         from_b = cb.from(g.b, plane_b(g.segments, seg), st);
-        const int64_t k = (int64_t)st * XENT_STAGE;
-        left_a = (int)min((int64_t)XENT_STAGE, g.a.inner - k);
-        left_b = (int)min((int64_t)XENT_STAGE, g.b.inner - k);
+        left_a = (int)(g.a.inner - (int64_t)st * XENT_STAGE);
+        left_b = (int)(g.b.inner - (int64_t)st * XENT_STAGE);
     };
     auto copy = [&](int buffer, int c) __attribute__((always_inline)) {
         const uint32_t to = lds0 + buffer * S::STAGE;
@@ -224,11 +225,16 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product g, End e
         else cb.copy(g.b, from_b, left_b, to + S::A, w, lane, c - ca.N);
     };
     auto copied = [&]() __attribute__((always_inline)) {
-        if (++st == g.stages) {
+        if (++st < g.stages) {
+            from_a += ca.step;
+            from_b += cb.step;
+            left_a -= XENT_STAGE;
+            left_b -= XENT_STAGE;
+        } else {
             st = 0;
             ++seg;
+            aim();
         }
-        aim();
     };
     aim();
     half8 a[S::MT], b[2][S::NT];
@@ -239,21 +245,37 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product g, End e
         b[s][j] = Fragments<S::TN, BT, true>::read(lds + (n & 1) * S::STAGE + S::A, at.wn, j, s, lane);
     };
     // One step's products, row tile by row tile.  Behind each the next step's fragments of that number are read, those of the rows
-    // into the registers just used, and a share of the copies is requested.
+    // into the registers just used, and those of the columns, which the next step needs first, behind the first ones.  The first step of a stage reads the second one's.  The second step reads the next stage's:
+    // after its first row tiles all waves meet, when what the first step read has long come, this stage's place is free for
+    // the one after the next, and the next one has arrived.
+    constexpr int MEET = S::MT / 4;
     auto step = [&](auto which, auto reads, auto copies, int n) __attribute__((always_inline)) {
-        constexpr int s = decltype(which)::value, next = 1 - s;
+        constexpr int s = decltype(which)::value, next = 1 - s, FROM = s ? MEET : 0;
+        constexpr bool READS = decltype(reads)::value, COPY = decltype(copies)::value;
+        auto meet = [&]() __attribute__((always_inline)) {
+            wait_loads<0>();
+            __syncthreads();
+        };
+        if constexpr (READS && s == 1 && MEET == 0) meet();
 #pragma unroll
         for (int i = 0; i < S::MT; ++i) {
 #pragma unroll
             for (int j = 0; j < S::NT; ++j) acc[i][j] = mma<H>(b[s][j], a[i], acc[i][j]);
-            if constexpr (decltype(reads)::value) {
-                read_a(n + s, next, i);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (READS) {
+                if (s == 1 && MEET > 0 && i == MEET - 1) meet();
+                constexpr int BEGIN = FROM ? FROM - 1 : 0, GROUPS = S::MT - BEGIN;
+                if (i >= BEGIN) {
+                    const int g = i - BEGIN;
 #pragma unroll
-                for (int j = i * S::NT / S::MT; j < (i + 1) * S::NT / S::MT; ++j) read_b(n + s, next, j);
-            }
-            if constexpr (decltype(copies)::value) {
+                    for (int k = g == 0 ? 0 : i; k <= i; ++k) read_a(n + s, next, k);
 #pragma unroll
-                for (int c = i * COPIES / S::MT; c < (i + 1) * COPIES / S::MT; ++c) copy(n & 1, c);
+                    for (int j = 2 * g; j < 2 * g + 2 && j < S::NT; ++j) read_b(n + s, next, j);
+                    if constexpr (COPY) {
+#pragma unroll
+                        for (int c = g * COPIES / GROUPS; c < (g + 1) * COPIES / GROUPS; ++c) copy(n & 1, c);
+                    }
+                }
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -262,11 +284,6 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product g, End e
     using One = std::integral_constant<int, 1>;
     auto stage = [&](auto more, auto copies, int n) __attribute__((always_inline)) {
         step(Zero{}, One{}, Zero{}, n);
-        // this stage is in registers and the next one has arrived, in all waves: its place is free for the one after that
-        if constexpr (decltype(more)::value) {
-            wait_loads<0>();
-            __syncthreads();
-        }
         step(One{}, more, copies, n);
         if constexpr (decltype(copies)::value) copied();
     };
@@ -295,7 +312,8 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product g, End e
 
 // ---- ends -----------------------------------------------------------------------------------
 
-__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+constexpr float XENT_LOG2E = 1.44269504f;
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x * XENT_LOG2E); }
 
 struct Logits {
     const float *bias;      // NULL: none
@@ -304,7 +322,13 @@ struct Logits {
     int64_t first, last;    // classes of this call: `first` is the products' first one
     int64_t V;
     float scale;
-    __device__ __forceinline__ float bias_of(int64_t v) const { return bias && v < V ? bias[v] : 0.f; }
+    // (what lies behind the last class of the call is closed)
+    __device__ __forceinline__ float bias_of(int64_t v) const { return v >= last ? -__builtin_inff() : bias ? bias[v] : 0.f; }
+    // number of the label among the columns from v0 on
+    __device__ __forceinline__ int label_from(int32_t label, int64_t v0) const
+    {
+        return label >= 0 && label < last ? (int)max((int64_t)-1, label - v0) : -1;
+    }
 };
 
 // The tile's part of a row: its largest logit, the sum of exponentials below it, and the label's logit.
@@ -328,25 +352,29 @@ struct SumEnd {
         for (int i = 0; i < S::MT; ++i) {
             const int row = at.wm + line_of<AT>(i, r);
             const int64_t n = at.m0 + row;
-            const int64_t label = n < z.N ? z.labels[n] : -1;
+            const int rel = z.label_from(n < z.N ? z.labels[n] : -1, v0);
             float top = -__builtin_inff(), sum = 0.f;
 #pragma unroll
             for (int j = 0; j < S::NT; ++j)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    const int64_t v = v0 + 32 * (j >> 1) + 4 * (j & 1) + c;
-                    const float x = v < z.last ? fmaf(z.scale, acc[i][j][c], bias[j][c]) : -__builtin_inff();
-                    if (v == label && v < z.last) z_store(n, x);
-                    acc[i][j][c] = x;
-                    top = fmaxf(top, x);
+                    acc[i][j][c] = fmaf(z.scale, acc[i][j][c], bias[j][c]);
+                    top = fmaxf(top, acc[i][j][c]);
                 }
+            if (__any(rel >= 0 && rel < 16 * S::NT)) {
+#pragma unroll
+                for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if (rel == 32 * (j >> 1) + 4 * (j & 1) + c) z_store(n, acc[i][j][c]);
+            }
             top = fmaxf(top, __shfl_xor(top, 16, 64));
             top = fmaxf(top, __shfl_xor(top, 32, 64));
-            const float shift = top > -__builtin_inff() ? top : 0.f;
+            const float shift = top > -__builtin_inff() ? top * XENT_LOG2E : 0.f;
 #pragma unroll
             for (int j = 0; j < S::NT; ++j)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) sum += exp2_of(acc[i][j][c] - shift);
+                for (int c = 0; c < 4; ++c) sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][c], XENT_LOG2E, -shift));
             sum += __shfl_xor(sum, 16, 64);
             sum += __shfl_xor(sum, 32, 64);
             if (q == 0) part[at.wn / (16 * S::NT) * S::TM + row] = float2{top, sum};
@@ -438,7 +466,7 @@ __global__ __launch_bounds__(512, 2) void xent_few_kernel(const H *__restrict__ 
                 float top = sum[i].x;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    a[e] = v + e < z.V ? fmaf(z.scale, a[e], bias[e]) : -__builtin_inff();
+                    a[e] = fmaf(z.scale, a[e], bias[e]);
                     if (v + e == label[i] && v + e < z.V) end.z_store(16 * i + r, a[e]);
                     top = fmaxf(top, a[e]);
                 }
@@ -534,19 +562,30 @@ struct GradEnd {
         for (int i = 0; i < S::MT; ++i) {
             const int64_t n = at.m0 + at.wm + line_of<AT>(i, r);
             const bool in = n < z.N;
-            const int64_t label = in ? z.labels[n] : -1;
+            const int32_t label = in ? z.labels[n] : -1;
             const bool live = label >= 0 && label < z.V;
-            const float l = in ? lse[n] : 0.f, g = in ? dloss[n] : 0.f;
+            // (an ignored row's, and that of a row without any finite logit: all probabilities are 0)
+            const float l = live ? lse[n] : -__builtin_inff(), shift = l == -__builtin_inff() ? __builtin_inff() : l * XENT_LOG2E;
+            const float g = live ? dloss[n] * factor : 0.f;
+            const int rel = z.label_from(label, v0);
+#pragma unroll
+            for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    acc[i][j][c] = __builtin_amdgcn_exp2f(fmaf(fmaf(z.scale, acc[i][j][c], bias[j][c]), XENT_LOG2E, -shift));
+            if (__any(rel >= 0 && rel < 16 * S::NT)) {
+#pragma unroll
+                for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if (rel == 32 * (j >> 1) + 4 * (j & 1) + c) acc[i][j][c] -= 1.f;
+            }
 #pragma unroll
             for (int j = 0; j < S::NT; ++j)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    const int64_t v = v0 + 32 * (j >> 1) + 4 * (j & 1) + c;
-                    const float x = fmaf(z.scale, acc[i][j][c], bias[j][c]);
-                    float p = l == -__builtin_inff() ? 0.f : exp2_of(x - l);
-                    p = live && v < z.last ? (p - (v == label ? 1.f : 0.f)) * g : 0.f;
-                    sum[j][c] += p;
-                    acc[i][j][c] = p * factor;
+                    acc[i][j][c] *= g;
+                    sum[j][c] += acc[i][j][c];
                 }
             if (n >= rows) continue;
             uint16_t *const to = d + n * ld + at.n0 + at.wn + 8 * q;
@@ -573,7 +612,7 @@ struct GradEnd {
         for (int j = 0; j < S::NT; ++j)
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                const float s = group_sum<16>(sum[j][c]);
+                const float s = group_sum<16>(sum[j][c]) / factor;
                 if (r == 0) part[at.wm / (16 * S::MT) * S::TN + at.wn + 32 * (j >> 1) + 8 * q + 4 * (j & 1) + c] = s;
             }
         __syncthreads();
