@@ -473,7 +473,7 @@ ftk_status ftk_route_gate_grad(ftk_dtype dtype, const void *logits, int64_t ldz,
  * Logits and sums are held in 32 bits; FTK_F32 operands are taken to 24 bits.  A bias of -infinity closes a class of finite
  * w.  A row all of whose logits are -infinity has lse -infinity, a NaN loss and no gradient; a NaN or +infinity among its
  * logits makes a row's loss, lse and gradients NaN.  Results are bitwise reproducible.
- * workspace: ftk_xent_workspace_bytes(dtype, N, V, D, grad); it grows with N * D, never with N * V beyond 128 MB, or 128 MB of
+ * workspace: ftk_xent_workspace_bytes(dtype, N, V, D, grad); it grows with N * D, never with N * V beyond 256 MB, or 256 MB of
  * W laid out anew (rows whose address, stride or length is no multiple of 16 bytes, and FTK_F32).
  * Limits: N, V < 2^31, D <= 2^20. */
 int64_t ftk_xent_workspace_bytes(ftk_dtype dtype, int64_t N, int64_t V, int32_t D, int32_t grad); /* -1: bad arguments */

@@ -39,7 +39,7 @@ struct Operand {
 };
 struct Product {
     Operand a, b;  // the result's rows and columns
-    int64_t mt, nt;
+    uint32_t mt, nt;  // tiles
     int stages;  // of a segment
     int segments;  // 1, or 6: products of pieces
     int splits;  // workgroups that share a tile's stages out between them
@@ -56,7 +56,7 @@ struct Shape {
 struct Place {
     int64_t m0, n0;  // of the tile
     int wm, wn;      // of the wave within it
-    int64_t mtile, ntile;
+    uint32_t mtile, ntile;
     int split;
 };
 
@@ -174,12 +174,12 @@ __device__ __forceinline__ int plane_b(int segments, int g) { return segments ==
 
 // Workgroups are dealt to the eight XCDs in turn; each XCD gets a run of tiles, eight rows of tiles high, so that the 32 tiles
 // under way there share their operands in its L2.
-__device__ __forceinline__ void tile_of(const Product &g, int64_t t, int64_t &mtile, int64_t &ntile)
+__device__ __forceinline__ void tile_of(const Product &g, uint32_t t, uint32_t &mtile, uint32_t &ntile)
 {
-    const int64_t all = g.mt * g.nt, each = (all + 7) / 8;
-    const int64_t x = t & 7, full = all & 7;  // the first `full` XCDs have one more where all is no multiple
+    const uint32_t all = g.mt * g.nt, each = (all + 7) / 8;
+    const uint32_t x = t & 7, full = all & 7;  // the first `full` XCDs have one more where all is no multiple
     t = full ? x * (each - 1) + min(x, full) + (t >> 3) : x * each + (t >> 3);
-    const int64_t panel = t / (8 * g.nt), in = t - panel * 8 * g.nt, high = min((int64_t)8, g.mt - panel * 8);
+    const uint32_t panel = t / (8 * g.nt), in = t - panel * 8 * g.nt, high = min(8u, g.mt - panel * 8);
     ntile = in / high;
     mtile = panel * 8 + (in - ntile * high);
 }
@@ -191,10 +191,10 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product g, End e
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Place at;
-    at.split = (int)(blockIdx.x / (g.mt * g.nt));
+    at.split = g.splits > 1 ? (int)(blockIdx.x / (g.mt * g.nt)) : 0;
     tile_of(g, blockIdx.x - at.split * (g.mt * g.nt), at.mtile, at.ntile);
-    at.m0 = at.mtile * S::TM;
-    at.n0 = at.ntile * S::TN;
+    at.m0 = (int64_t)at.mtile * S::TM;
+    at.n0 = (int64_t)at.ntile * S::TN;
     at.wm = w / S::WN * 16 * S::MT;
     at.wn = w % S::WN * 16 * S::NT;
     float4v acc[S::MT][S::NT];
@@ -206,10 +206,14 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product g, End e
     Copies<S::TN, S::WAVES, BT, true> cb;
     ca.begin(g.a, at.m0, w, lane);
     cb.begin(g.b, at.n0, w, lane);
-    const int64_t all = (int64_t)g.stages * g.segments;
-    const int begin = __builtin_amdgcn_readfirstlane((int)(all * at.split / g.splits));
-    const int total = __builtin_amdgcn_readfirstlane((int)(all * (at.split + 1) / g.splits)) - begin;
-    int seg = begin / g.stages, st = begin - seg * g.stages;  // of the next copy
+    const int all = g.stages * g.segments;
+    int seg = 0, st = 0, total = all;  // of the next copy; stages of this workgroup
+    if (g.splits > 1) {
+        const uint32_t begin = (uint64_t)all * at.split / (uint32_t)g.splits;
+        total = (int)((uint64_t)all * (at.split + 1) / (uint32_t)g.splits - begin);
+        seg = (int)(begin / g.stages);
+        st = (int)(begin - seg * g.stages);
+    }
     constexpr int COPIES = ca.N + cb.N;
     const uint8_t *from_a, *from_b;
     int left_a, left_b;
@@ -865,9 +869,9 @@ static XentPlan plan_xent(ftk_dtype dtype, int64_t N, int64_t V, int D, bool gra
     p.planes = dtype == FTK_F32 ? 3 : 1;
     p.rows = ceil_div(N > 0 ? N : 1, XENT_STAGE) * XENT_STAGE;  // (without rows gradients are zeros)
     p.Dp = (int)(ceil_div(D, XENT_STAGE) * XENT_STAGE);
-    // d, or the packed rows of W, of a piece: about 128 MB, which the memory-side cache holds
+    // d, or the packed rows of W, of a piece: about 256 MB
     const int64_t rows = direct ? p.rows : grad && p.rows > p.Dp ? p.rows : p.Dp;
-    int64_t width = (64ll << 20) / p.planes / rows / 256 * 256;
+    int64_t width = (128ll << 20) / p.planes / rows / 256 * 256;
     width = width < 256 ? 256 : width;
     const int64_t whole = ceil_div(V, 256) * 256;
     if (!grad && direct) width = whole;
@@ -914,14 +918,15 @@ static XentPlan plan_xent(ftk_dtype dtype, int64_t N, int64_t V, int D, bool gra
 template <typename S, typename H, bool AT, bool BT, typename End>
 static ftk_status launch_shape(Product g, const End &end, hipStream_t st)
 {
-    g.mt = ceil_div(g.a.outer, S::TM);
-    g.nt = ceil_div(g.b.outer, S::TN);
-    if (g.mt * g.nt * g.splits > 0x7fffffffLL) {
-        set_error("too many tiles: %lld x %lld", (long long)g.mt, (long long)g.nt);
+    const int64_t mt = ceil_div(g.a.outer, S::TM), nt = ceil_div(g.b.outer, S::TN), work = mt * nt * g.splits;
+    if (work > 0x7fffffffLL) {
+        set_error("too many tiles: %lld x %lld", (long long)mt, (long long)nt);
         return FTK_EINVAL;
     }
+    g.mt = (uint32_t)mt;
+    g.nt = (uint32_t)nt;
     FTK_TRY(allow_lds<S::LDS>((const void *)product_kernel<S, H, AT, BT, End>));
-    product_kernel<S, H, AT, BT, End><<<(unsigned)(g.mt * g.nt * g.splits), S::THREADS, S::LDS, st>>>(g, end);
+    product_kernel<S, H, AT, BT, End><<<(unsigned)work, S::THREADS, S::LDS, st>>>(g, end);
     FTK_TRY_HIP(hipGetLastError());
     return FTK_OK;
 }
