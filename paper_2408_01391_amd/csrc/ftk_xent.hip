@@ -505,30 +505,24 @@ __global__ __launch_bounds__(512, 2) void xent_few_kernel(const H *__restrict__ 
     end.parts[n * end.tiles + blockIdx.x] = p;
 }
 
-// A wave a row: its parts together.
+// L lanes a row: its parts together.
+template <int L>
 __global__ __launch_bounds__(256) void xent_loss_kernel(const float2 *parts, int64_t tiles, const float *label_logit,
                                                         const int32_t *labels, int64_t N, int64_t V, float *loss, float *lse)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (n >= N) return;
-    float top = -__builtin_inff();
-    for (int64_t t = lane; t < tiles; t += 64) top = fmaxf(top, parts[n * tiles + t].x);
-    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-    const float shift = top > -__builtin_inff() ? top : 0.f;
-    float sum = 0.f;
-    for (int64_t t = lane; t < tiles; t += 64) {
-        const float2 p = parts[n * tiles + t];
-        sum += p.y * exp2_of(p.x - shift);
-    }
-    sum = group_sum<64>(sum);
-    if (lane == 0) {
-        const int64_t label = labels[n];
-        const bool live = label >= 0 && label < V;
-        const float l = sum == 0.f ? -__builtin_inff() : shift + logf(sum);
-        lse[n] = live ? l : 0.f;
-        loss[n] = live ? l - label_logit[n] : 0.f;
-    }
+    const int lane = threadIdx.x & (L - 1);
+    const int64_t row = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L, n = min(row, N - 1);
+    float2 sum{-__builtin_inff(), 0.f};
+#pragma unroll 4
+    for (int64_t t = lane; t < tiles; t += L) sum = SumEnd::joined(sum, parts[n * tiles + t]);
+#pragma unroll
+    for (int d = 1; d < L; d *= 2) sum = SumEnd::joined(sum, float2{__shfl_xor(sum.x, d, 64), __shfl_xor(sum.y, d, 64)});
+    if (lane || row >= N) return;
+    const int64_t label = labels[n];
+    const bool live = label >= 0 && label < V;
+    const float l = sum.y == 0.f ? -__builtin_inff() : (sum.x > -__builtin_inff() ? sum.x : 0.f) + logf(sum.y);
+    lse[n] = live ? l : 0.f;
+    loss[n] = live ? l - label_logit[n] : 0.f;
 }
 
 // Power of two that brings the largest |dloss| to [2^14, 2^15) (fp16 rows), else 1.
@@ -757,21 +751,32 @@ __global__ __launch_bounds__(256) void join_kernel(const float *__restrict__ par
 
 // Rows to whole lines of 64 elements (three bf16 pieces where PLANES is 3), zeros beyond the row and in rows that are not looked at:
 // those whose label lies outside [0, V), and those from N on.
+struct PackJob {
+    const void *X;
+    int64_t ldx, N, rows;
+    int D, Dp;
+    const int32_t *labels;  // NULL: all rows are looked at
+    int64_t V;
+    uint16_t *out;
+    uint32_t groups;
+};
+// One array, or two in one launch: the second one's workgroups behind the first's.
 template <typename T, typename H, int PLANES>
-__global__ __launch_bounds__(256) void pack_kernel(const T *__restrict__ X, int64_t ldx, int64_t N, int D, int64_t rows, int Dp,
-                                                   const int32_t *labels, int64_t V, uint16_t *__restrict__ out, uint32_t *zero)
+__global__ __launch_bounds__(256) void pack_kernel(PackJob first, PackJob second, uint32_t *zero)
 {
     if (zero && blockIdx.x == 0 && threadIdx.x == 0) *zero = 0;
-    const int pieces = Dp / 8;
-    const int64_t all = rows * pieces;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    const bool other = blockIdx.x >= first.groups;
+    const PackJob j = other ? second : first;
+    const int pieces = j.Dp / 8;
+    const int64_t all = j.rows * pieces;
+    for (int64_t i = (int64_t)(blockIdx.x - (other ? first.groups : 0)) * 256 + threadIdx.x; i < all; i += (int64_t)j.groups * 256) {
         const int64_t n = i / pieces;
         const int d = (int)(i - n * pieces) * 8;
-        bool live = n < N;
-        if (live && labels) live = labels[n] >= 0 && labels[n] < V;
+        bool live = n < j.N;
+        if (live && j.labels) live = j.labels[n] >= 0 && j.labels[n] < j.V;
         T v[8];
         if (live) {
-            load8(X + n * ldx, d, D, v);
+            load8((const T *)j.X + n * j.ldx, d, j.D, v);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = (T)0.f;
@@ -788,7 +793,7 @@ __global__ __launch_bounds__(256) void pack_kernel(const T *__restrict__ X, int6
             }
         }
 #pragma unroll
-        for (int k = 0; k < PLANES; ++k) *reinterpret_cast<half8 *>(out + k * rows * Dp + n * Dp + d) = o[k];
+        for (int k = 0; k < PLANES; ++k) *reinterpret_cast<half8 *>(j.out + k * j.rows * j.Dp + n * j.Dp + d) = o[k];
     }
 }
 
@@ -954,11 +959,14 @@ static ftk_status launch_gradient(Product g, const XentPlan::Cut &cut, const Sto
 }
 
 template <typename T, typename H, int PLANES>
-static ftk_status launch_pack(const T *X, int64_t ldx, int64_t N, int D, int64_t rows, int Dp, const int32_t *labels, int64_t V,
-                              uint16_t *out, uint32_t *zero, hipStream_t st)
+static ftk_status launch_pack(PackJob first, PackJob second, uint32_t *zero, hipStream_t st)
 {
-    const int64_t groups = ceil_div(rows * (Dp / 8), 256);
-    pack_kernel<T, H, PLANES><<<(unsigned)(groups < 4096 ? groups : 4096), 256, 0, st>>>(X, ldx, N, D, rows, Dp, labels, V, out, zero);
+    for (PackJob *j : {&first, &second}) {
+        const int64_t groups = ceil_div(j->rows * (j->Dp / 8), 256);
+        j->groups = (uint32_t)(groups < 4096 ? groups : 4096);
+    }
+    if (first.groups + second.groups == 0) return FTK_OK;
+    pack_kernel<T, H, PLANES><<<first.groups + second.groups, 256, 0, st>>>(first, second, zero);
     FTK_TRY_HIP(hipGetLastError());
     return FTK_OK;
 }
@@ -973,29 +981,38 @@ struct XentCall {
     uint8_t *ws;
     XentPlan p;
     hipStream_t st;
-    // one piece's rows of W: packed, or where they lie
+    PackJob rows_job() const { return PackJob{X, ldx, N, p.rows, D, p.Dp, labels, V, (uint16_t *)(ws + p.X), 0}; }
+    // One piece's rows of W: packed, in one launch with `rows` (the first piece: those of X), or where they lie.
     template <typename T, typename H, int PLANES>
-    ftk_status classes(int64_t first, int64_t n, Operand &along, Operand &across) const
+    ftk_status classes(int64_t first, int64_t n, const PackJob &rows, uint32_t *zero, Operand &along, Operand &across) const
     {
+        PackJob job{};
         if (p.direct) {
             const uint16_t *w = (const uint16_t *)W + first * ldw;
             along = Operand{w, ldw, 0, n, D};
             across = Operand{w, ldw, 0, D, n};
-            return FTK_OK;
+        } else {
+            uint16_t *w = (uint16_t *)(ws + p.W);
+            job = PackJob{(const T *)W + first * ldw, ldw, n, n, D, p.Dp, nullptr, 0, w, 0};
+            along = Operand{w, p.Dp, n * p.Dp, n, p.Dp};
+            across = Operand{w, p.Dp, n * p.Dp, p.Dp, n};
         }
-        uint16_t *w = (uint16_t *)(ws + p.W);
-        FTK_TRY((launch_pack<T, H, PLANES>((const T *)W + first * ldw, ldw, n, D, n, p.Dp, nullptr, 0, w, nullptr, st)));
-        along = Operand{w, p.Dp, n * p.Dp, n, p.Dp};
-        across = Operand{w, p.Dp, n * p.Dp, p.Dp, n};
-        return FTK_OK;
+        return launch_pack<T, H, PLANES>(rows, job, zero, st);
     }
 };
 
 static ftk_status launch_loss(const XentCall &c, const SumEnd &end, float *loss, float *lse)
 {
-    xent_loss_kernel<<<(unsigned)ceil_div(c.N, 4), 256, 0, c.st>>>(end.parts, end.tiles, end.label_logit, c.labels, c.N, c.V, loss, lse);
-    FTK_TRY_HIP(hipGetLastError());
-    return FTK_OK;
+    auto go = [&](auto lanes) {
+        constexpr int L = decltype(lanes)::value;
+        xent_loss_kernel<L><<<(unsigned)ceil_div(c.N, 256 / L), 256, 0, c.st>>>(end.parts, end.tiles, end.label_logit, c.labels, c.N, c.V,
+                                                                              loss, lse);
+        FTK_TRY_HIP(hipGetLastError());
+        return FTK_OK;
+    };
+    // (two parts a lane where there are few)
+    if (end.tiles <= 8) return go(std::integral_constant<int, 4>{});
+    return end.tiles <= 64 ? go(std::integral_constant<int, 16>{}) : go(std::integral_constant<int, 64>{});
 }
 
 template <typename H, int MT, int RUN>
@@ -1028,9 +1045,10 @@ static ftk_status xent_forward(const XentCall &c, float *loss, float *lse)
         }
     }
     uint16_t *x = (uint16_t *)(c.ws + p.X);
-    FTK_TRY((launch_pack<T, H, PLANES>((const T *)c.X, c.ldx, c.N, c.D, p.rows, p.Dp, c.labels, c.V, x, nullptr, c.st)));
     Product g;
-    g.a = Operand{x, p.Dp, p.rows * p.Dp, c.N, p.Dp};
+    // (rows of whole stages are read where they lie: what an ignored one holds stays in its own sums, which are not looked at)
+    const bool direct = PLANES == 1 && p.direct && c.D % XENT_STAGE == 0 && rows_direct(FTK_BF16, c.X, c.ldx, c.D);
+    g.a = direct ? Operand{(const uint16_t *)c.X, c.ldx, 0, c.N, c.D} : Operand{x, p.Dp, p.rows * p.Dp, c.N, p.Dp};
     g.stages = p.Dp / XENT_STAGE;
     g.segments = PLANES == 3 ? 6 : 1;
     g.splits = 1;
@@ -1039,7 +1057,7 @@ static ftk_status xent_forward(const XentCall &c, float *loss, float *lse)
     for (int64_t first = 0; first < c.V; first += p.width) {
         const int64_t n = c.V - first < p.width ? c.V - first : p.width;
         Operand across;
-        FTK_TRY((c.classes<T, H, PLANES>(first, n, g.b, across)));
+        FTK_TRY((c.classes<T, H, PLANES>(first, n, first == 0 && !direct ? c.rows_job() : PackJob{}, nullptr, g.b, across)));
         const SumEnd end{Logits{c.bias, c.labels, c.N, first, first + n, c.V, c.scale}, parts, tiles, first / tile, label_logit};
         FTK_TRY((launch_product<H, false, false>(g, tile, end, c.st)));
     }
@@ -1054,18 +1072,17 @@ static ftk_status xent_backward(const XentCall &c, const float *lse, const float
     uint16_t *x = (uint16_t *)(c.ws + p.X), *d = (uint16_t *)(c.ws + p.d);
     uint32_t *top = std::is_same<T, _Float16>::value ? (uint32_t *)(c.ws + p.top) : nullptr;
     float *parts = (float *)(c.ws + p.dbias), *shares = (float *)(c.ws + p.shares);
-    FTK_TRY((launch_pack<T, H, PLANES>((const T *)c.X, c.ldx, c.N, c.D, p.rows, p.Dp, c.labels, c.V, x, top, c.st)));
-    if (top) {
-        const int64_t groups = ceil_div(c.N, 1024);
-        dloss_top_kernel<<<(unsigned)(groups < 256 ? groups : 256), 256, 0, c.st>>>(dloss, c.labels, c.N, c.V, top);
-        FTK_TRY_HIP(hipGetLastError());
-    }
     const int segments = PLANES == 3 ? 6 : 1;
     for (int64_t first = 0; first < c.V; first += p.width) {
         const int64_t n = c.V - first < p.width ? c.V - first : p.width, np = ceil_div(n, XENT_STAGE) * XENT_STAGE;
         const int64_t plane = p.rows * p.width;
         Operand along, across;
-        FTK_TRY((c.classes<T, H, PLANES>(first, n, along, across)));
+        FTK_TRY((c.classes<T, H, PLANES>(first, n, first == 0 ? c.rows_job() : PackJob{}, first == 0 ? top : nullptr, along, across)));
+        if (top && first == 0) {
+            const int64_t groups = ceil_div(c.N > 0 ? c.N : 1, 1024);
+            dloss_top_kernel<<<(unsigned)(groups < 256 ? groups : 256), 256, 0, c.st>>>(dloss, c.labels, c.N, c.V, top);
+            FTK_TRY_HIP(hipGetLastError());
+        }
         Product g{Operand{x, p.Dp, p.rows * p.Dp, p.rows, p.Dp}, along, 0, 0, p.Dp / XENT_STAGE, segments, 1};
         const int tile = p.logits.tile;
         const GradEnd<H, PLANES> grad{Logits{c.bias, c.labels, c.N, first, first + n, c.V, c.scale}, lse, dloss, top, d, p.width, plane,
