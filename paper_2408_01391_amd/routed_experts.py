@@ -3,9 +3,10 @@
 The centroids come from a Lloyd fit over sample rows.  A token has two slots: the matrix of its cluster, weighted by
 how near the centroid is, and one that all tokens share.  The matrices are held in 4 bits.
 
-    python -m paper_2408_01391_amd.routed_experts [--tokens N] [--features D] [--outputs F] [--clusters K]
+    python -m paper_2408_01391_amd.routed_experts [--tokens N] [--features D] [--outputs F] [--clusters K] [--classes V] [--steps S]
 
-runs a fit, a forward and a backward pass and prints times and the distance from the same layer in 32 bits.
+runs a fit, a forward and a backward pass and prints times and the distance from the same layer in 32 bits; then S
+training steps of LearnedExperts, experts with a gate that learns, which are to name the clusters of a finer fit.
 """
 from __future__ import annotations
 
@@ -16,10 +17,42 @@ import torch
 from . import binding as ftk
 
 
-class RoutedExperts:
-    """out[t] = sum over the slots (t, j) of g[t, j] * W[label[t, j]] x[t] with W packed to 4 bits.
+class Experts:
+    """out[t] = sum over the slots (t, j) of g[t, j] * W[label[t, j]] x[t] with W [E, F, D] packed to 4 bits, once for either direction."""
 
-    weights: [K + 1, F, D]: one matrix a cluster, the last one shared.  Packed once for either direction.
+    def __init__(self, weights):
+        self.E, self.F, self.D = weights.shape
+        self.W = self.WT = None
+        self.pack(weights)
+
+    def pack(self, weights):
+        """Packs the matrices anew, where they were packed before: a captured graph finds them there."""
+        E, F, D = weights.shape
+        self.W = ftk.mx4_quantize(weights.reshape(E * F, D), out=self.W)
+        self.WT = ftk.mx4_quantize(weights.transpose(1, 2).reshape(E * D, F), out=self.WT)
+
+    def products(self, x, labels, gates, training=False):
+        """Returns (out [N, F], what gradients() needs, or None)."""
+        # (the weights' gradient sums over whole steps of the matrix instruction)
+        route = ftk.route_plan(labels, self.E, align=128 if training else 1)
+        y = ftk.mx4_linear(x, self.W, route=route, gather=True)
+        return ftk.route_combine(y, route, gates), (x, y, route, gates) if training else None
+
+    def gradients(self, dout, saved, out_dtype=torch.float32):
+        """Gradients (dx [N, D], dgates [N, k], dweights [E, F, D] of out_dtype) of sum(dout * out) with labels and gates held fixed;
+        rounding to 4 bits counts as the identity."""
+        x, y, route, gates = saved
+        dy, dgates = ftk.route_combine_grad(dout, y, route, gates)
+        dx = ftk.route_combine(ftk.mx4_linear(dy, self.WT, route=route), route)
+        rows = ftk.route_gather(x, route)
+        dweights = ftk.mx4_outer(ftk.mx4_quantize(dy, transpose=True), ftk.mx4_quantize(rows, transpose=True), route, out_dtype=out_dtype)
+        return dx, dgates, dweights
+
+
+class RoutedExperts(Experts):
+    """Experts whose tokens go to the matrix of their nearest centroid and to one that all share.
+
+    weights: [K + 1, F, D]: one matrix a cluster, the last one shared.
     width: squared distance at which a cluster's weight has fallen to 1 / e; without one the mean squared distance of the centroids
     from their own mean.  It belongs to the layer: what a token gets does not depend on its batch."""
 
@@ -27,15 +60,13 @@ class RoutedExperts:
         E, F, D = weights.shape
         if centroids.shape != (E - 1, D):
             raise ValueError("need a matrix for each of the %d centroids and a shared one, got %d" % (centroids.shape[0], E))
-        self.E, self.F, self.D = E, F, D
         self.centroids = centroids.float().contiguous()
         if width is None:
             width = self._width((self.centroids - self.centroids.mean(0)).square().sum(1), self.centroids)
         if not width > 0:
             raise ValueError("width must be above 0, got %s" % width)
         self.width = float(width)
-        self.W = ftk.mx4_quantize(weights.reshape(E * F, D))
-        self.WT = ftk.mx4_quantize(weights.transpose(1, 2).reshape(E * D, F))
+        super().__init__(weights)
 
     @classmethod
     def fitted(cls, weights, samples, iters=10, seed=0):
@@ -60,21 +91,62 @@ class RoutedExperts:
         """Returns (out [N, F], what backward needs, or None)."""
         if labels is None:
             labels, gates = self.gate(x)
-        # (the weights' gradient sums over whole steps of the matrix instruction)
-        route = ftk.route_plan(labels, self.E, align=128 if training else 1)
-        y = ftk.mx4_linear(x, self.W, route=route, gather=True)
-        return ftk.route_combine(y, route, gates), (x, y, route, gates) if training else None
+        return self.products(x, labels, gates, training)
 
     def backward(self, dout, saved):
         """Gradients (dx [N, D], dgates [N, 2], dweights [E, F, D] in 32 bits) of sum(dout * out) with labels and gates held fixed;
         rounding to 4 bits counts as the identity.  Where the gates depend on x, as those of gate() do, what reaches x through
         them is not in dx: it is dgates through whatever made them."""
-        x, y, route, gates = saved
-        dy, dgates = ftk.route_combine_grad(dout, y, route, gates)
-        dx = ftk.route_combine(ftk.mx4_linear(dy, self.WT, route=route), route)
-        rows = ftk.route_gather(x, route)
-        dweights = ftk.mx4_outer(ftk.mx4_quantize(dy, transpose=True), ftk.mx4_quantize(rows, transpose=True), route)
-        return dx, dgates, dweights
+        return self.gradients(dout, saved)
+
+
+class LearnedExperts(Experts):
+    """Experts with a gate that learns, and a loss over many classes: a token goes to the k experts whose logits x Wg^T are largest,
+    weighted by the softmax over them, and their sum is held against the classes' vectors.
+
+    gate [E, D], experts [E, F, D], classes [V, F]: weights of one type, float32 or bfloat16, which the layer updates in place
+    (AdamW; 16-bit weights beside 32-bit masters, states of `bits` bits).  bias [V] float: of the classes' logits.
+    balance: weight of the balance loss."""
+
+    def __init__(self, gate, experts, classes, k=2, balance=0.01, bits=8, bias=None, **options):
+        E, F, D = experts.shape
+        if gate.shape != (E, D) or classes.shape[1] != F:
+            raise ValueError("need gate [%d, %d] and classes [V, %d], got %s and %s" % (E, D, F, list(gate.shape), list(classes.shape)))
+        if not 1 <= k <= E:
+            raise ValueError("need 1 <= k <= %d experts, got %d" % (E, k))
+        self.gate, self.experts, self.classes, self.k, self.bias, self.options = gate, experts, classes, k, bias, options
+        self.state = ftk.AdamW([gate, experts, classes], bits, master=gate.dtype != torch.float32)
+        self.count = torch.zeros(1, dtype=torch.int64, device=gate.device)
+        self.balance = torch.full((1,), float(balance), device=gate.device)
+        super().__init__(experts)
+
+    def forward(self, x, training=False):
+        """Returns (out [N, F], what gradients of the weights need)."""
+        logits = x @ self.gate.t()
+        gate = ftk.route_gate(logits, self.k)
+        out, saved = self.products(x, gate.labels, gate.weights, training)
+        return out, (logits, gate, saved)
+
+    def loss(self, x, labels, weights=None):
+        """Returns (sum of the rows' losses by their weights float [N], by default 1 / N; gradients of it and the balance loss by
+        gate, experts and classes; the Gate).  Rows with a label outside [0, V) are ignored."""
+        N = x.shape[0]
+        out, (logits, gate, saved) = self.forward(x, training=True)
+        loss, lse = ftk.xent(out, self.classes, labels, bias=self.bias)
+        if weights is None:
+            weights = torch.full((N,), 1.0 / max(N, 1), device=x.device)
+        dout, dclasses, _ = ftk.xent_grad(out, self.classes, labels, lse, weights, bias=self.bias, need=(True, True, False))
+        _, dgates, dexperts = self.gradients(dout, saved, x.dtype)
+        dlogits = ftk.route_gate_grad(logits, gate, dgates, self.balance)
+        return torch.dot(loss, weights), [dlogits.t() @ x, dexperts, dclasses], gate
+
+    def step(self, x, labels, weights=None):
+        """One update of all weights; returns (loss, Gate)."""
+        loss, grads, gate = self.loss(x, labels, weights)
+        self.count.add_(1)
+        ftk.adamw_step(self.state, grads, self.count, **self.options)
+        self.pack(self.experts)
+        return loss, gate
 
 
 def main():
@@ -83,6 +155,8 @@ def main():
     ap.add_argument("--features", type=int, default=1024)
     ap.add_argument("--outputs", type=int, default=2048)
     ap.add_argument("--clusters", type=int, default=15)
+    ap.add_argument("--classes", type=int, default=512)
+    ap.add_argument("--steps", type=int, default=20)
     a = ap.parse_args()
     g = torch.Generator(device="cuda:0").manual_seed(1)
     rand = lambda *s: torch.randn(*s, generator=g, device="cuda:0")  # noqa: E731
@@ -115,6 +189,18 @@ def main():
             plain[t] += gates[t, j].unsqueeze(1) * (x[t].float() @ weights[e].t().contiguous())
     print("from 32-bit matrices and rows: %.3f of the output" % float((out.float() - plain).norm() / plain.norm()))
     print("gradients: " + ", ".join("%s %s" % (list(t.shape), str(t.dtype)[6:]) for t in grads))
+
+    # the clusters of a finer fit are the classes that experts with a gate of their own learn to name
+    V = a.classes
+    fine = ftk.kmeans_fit(x.float(), V, 5, seed=1, want_inertia=False)["C"]
+    names = ftk.kmeans_assign(x.float(), fine)[0]
+    learner = LearnedExperts((rand(E, D) * D ** -0.5).bfloat16(), weights.bfloat16(), (rand(V, F) * F ** -0.5).bfloat16(), lr=1e-3)
+    first, gate = learner.step(x, names)
+    for _ in range(a.steps - 1):
+        last, gate = learner.step(x, names)
+    if a.steps > 1:
+        print("%d steps towards %d classes: loss %.3f, then %.3f; balance loss %.3f" % (a.steps, V, float(first), float(last), float(gate.loss)))
+    print("a training step %.0f us" % timed(lambda: learner.step(x, names)))
 
 
 if __name__ == "__main__":
