@@ -470,11 +470,11 @@ ftk_status ftk_route_gate_grad(ftk_dtype dtype, const void *logits, int64_t ldz,
  *   X [N x D], W [V x D] of `dtype` (FTK_F32, FTK_BF16 or FTK_F16), row strides ldx and ldw; bias [V] or NULL: 0
  *   labels [N]: a row whose label lies outside [0, V) is ignored: nothing of it is looked at, loss and lse are 0
  *   loss, lse [N]
- * Logits and sums are held in 32 bits; FTK_F32 operands are taken to 24 bits.  A bias of -infinity closes a class of finite
- * w.  A row all of whose logits are -infinity has lse -infinity, a NaN loss and no gradient; a NaN or +infinity among its
- * logits makes a row's loss, lse and gradients NaN.  Results are bitwise reproducible.
- * workspace: ftk_xent_workspace_bytes(dtype, N, V, D, grad); it grows with N * D, never with N * V beyond 256 MB, or 256 MB of
- * W laid out anew (rows whose address, stride or length is no multiple of 16 bytes, and FTK_F32).
+ * Logits and sums are held in 32 bits; FTK_F32 operands (below 2^127) are taken to 24 bits.  W has to be finite.  A bias of
+ * -infinity closes a class.  A row all of whose logits are -infinity has lse -infinity, a NaN loss and no gradient; a NaN or
+ * +infinity among its logits makes a row's loss, lse and gradients NaN.  Results are bitwise reproducible.
+ * workspace: ftk_xent_workspace_bytes(dtype, N, V, D, grad); it grows with N * max(D, 256), not with N * V: the classes go in pieces
+ * of up to 256 MB (gradients, or W laid out anew: FTK_F32, or rows whose address, stride or length is no multiple of 16 bytes).
  * Limits: N, V < 2^31, D <= 2^20. */
 int64_t ftk_xent_workspace_bytes(ftk_dtype dtype, int64_t N, int64_t V, int32_t D, int32_t grad); /* -1: bad arguments */
 ftk_status ftk_xent(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N, const void *W, int64_t ldw, int64_t V, int32_t D,

@@ -339,7 +339,7 @@ struct Logits {
 struct SumEnd {
     Logits z;
     float2 *parts;  // [N][tiles]
-    int64_t tiles, first_tile;
+    int64_t tiles;
     float *label_logit;  // [N]
     template <typename S, bool AT>
     __device__ __forceinline__ void run(float4v (&acc)[S::MT][S::NT], const Place &at, uint8_t *lds) const
@@ -390,7 +390,7 @@ struct SumEnd {
             float2 p = part[row];
 #pragma unroll
             for (int k = 1; k < S::WN; ++k) p = joined(p, part[k * S::TM + row]);
-            parts[n * tiles + first_tile + at.ntile] = p;
+            parts[n * tiles + at.ntile] = p;
         }
     }
     __device__ __forceinline__ void z_store(int64_t n, float x) const { label_logit[n] = x; }
@@ -505,10 +505,11 @@ __global__ __launch_bounds__(512, 2) void xent_few_kernel(const H *__restrict__ 
     end.parts[n * end.tiles + blockIdx.x] = p;
 }
 
-// L lanes a row: its parts together.
+// L lanes a row: its parts together, with those of earlier pieces of the classes (running, NULL: there are no other pieces).
 template <int L>
-__global__ __launch_bounds__(256) void xent_loss_kernel(const float2 *parts, int64_t tiles, const float *label_logit,
-                                                        const int32_t *labels, int64_t N, int64_t V, float *loss, float *lse)
+__global__ __launch_bounds__(256) void xent_loss_kernel(const float2 *parts, int64_t tiles, float2 *running, bool first, bool end,
+                                                        const float *label_logit, const int32_t *labels, int64_t N, int64_t V,
+                                                        float *loss, float *lse)
 {
     const int lane = threadIdx.x & (L - 1);
     const int64_t row = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L, n = min(row, N - 1);
@@ -518,6 +519,13 @@ __global__ __launch_bounds__(256) void xent_loss_kernel(const float2 *parts, int
 #pragma unroll
     for (int d = 1; d < L; d *= 2) sum = SumEnd::joined(sum, float2{__shfl_xor(sum.x, d, 64), __shfl_xor(sum.y, d, 64)});
     if (lane || row >= N) return;
+    if (running) {
+        if (!first) sum = SumEnd::joined(running[n], sum);
+        if (!end) {
+            running[n] = sum;
+            return;
+        }
+    }
     const int64_t label = labels[n];
     const bool live = label >= 0 && label < V;
     const float l = sum.y == 0.f ? -__builtin_inff() : (sum.x > -__builtin_inff() ? sum.x : 0.f) + logf(sum.y);
@@ -815,12 +823,12 @@ struct XentPlan {
     int64_t rows;     // N rounded up to whole stages
     int Dp;           // D rounded up to whole stages
     int64_t width;    // classes of a piece
-    int64_t tiles;    // column tiles of the logits' sums, all classes
+    int64_t tiles;    // parts of a row's sums, of a piece
     // how products are cut: logits (or d), the rows' gradients, the classes'
     struct Cut {
         int tile, splits;
     } logits, rows_grad, classes_grad;
-    size_t X, W, parts, label_logit, d, sums, shares, dbias, top, total;
+    size_t X, W, parts, running, label_logit, d, sums, shares, dbias, top, total;
 };
 
 using Large = Shape<8, 4, 2, 4>;   // 256 x 256, eight waves
@@ -879,11 +887,14 @@ static XentPlan plan_xent(ftk_dtype dtype, int64_t N, int64_t V, int D, bool gra
     int64_t width = (128ll << 20) / p.planes / rows / 256 * 256;
     width = width < 256 ? 256 : width;
     const int64_t whole = ceil_div(V, 256) * 256;
-    if (!grad && direct) width = whole;
+    if (!grad) {
+        // a part of the sums stands for 64 classes at least; 64 MB of them
+        const int64_t parts = (8ll << 20) / (N > 0 ? N : 1) * XENT_TILE / 256 * 256;
+        if (direct || parts < width) width = parts < 256 ? 256 : parts;
+    }
     p.width = width < whole ? width : whole;
     // (pieces of equal width)
     p.width = ceil_div(ceil_div(V, ceil_div(V, p.width)), 256) * 256;
-    p.tiles = ceil_div(V, XENT_TILE);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t a = at;
@@ -903,7 +914,7 @@ static XentPlan plan_xent(ftk_dtype dtype, int64_t N, int64_t V, int D, bool gra
     }
     p.X = take((size_t)p.planes * p.rows * p.Dp * 2);
     p.W = direct ? at : take((size_t)p.planes * p.width * p.Dp * 2);
-    p.parts = p.label_logit = p.d = p.sums = p.shares = p.dbias = p.top = at;
+    p.parts = p.running = p.label_logit = p.d = p.sums = p.shares = p.dbias = p.top = at;
     if (grad) {
         p.d = take((size_t)p.planes * p.rows * p.width * 2);
         p.sums = dtype == FTK_F32 ? at : take((size_t)N * D * 4);
@@ -913,7 +924,9 @@ static XentPlan plan_xent(ftk_dtype dtype, int64_t N, int64_t V, int D, bool gra
         p.dbias = take((size_t)ceil_div(p.rows, XENT_TILE) * p.width * 4);
         p.top = take(256);
     } else {
+        p.tiles = ceil_div(classes, p.logits.tile);
         p.parts = take((size_t)N * p.tiles * 8);
+        p.running = p.width < V ? take((size_t)N * 8) : at;
         p.label_logit = take((size_t)N * 4);
     }
     p.total = at;
@@ -1001,12 +1014,12 @@ struct XentCall {
     }
 };
 
-static ftk_status launch_loss(const XentCall &c, const SumEnd &end, float *loss, float *lse)
+static ftk_status launch_loss(const XentCall &c, const SumEnd &end, float2 *running, bool first, bool last, float *loss, float *lse)
 {
     auto go = [&](auto lanes) {
         constexpr int L = decltype(lanes)::value;
-        xent_loss_kernel<L><<<(unsigned)ceil_div(c.N, 256 / L), 256, 0, c.st>>>(end.parts, end.tiles, end.label_logit, c.labels, c.N, c.V,
-                                                                              loss, lse);
+        xent_loss_kernel<L><<<(unsigned)ceil_div(c.N, 256 / L), 256, 0, c.st>>>(end.parts, end.tiles, running, first, last, end.label_logit,
+                                                                              c.labels, c.N, c.V, loss, lse);
         FTK_TRY_HIP(hipGetLastError());
         return FTK_OK;
     };
@@ -1022,7 +1035,7 @@ static ftk_status launch_few_shape(const XentCall &c, SumEnd end, float *loss, f
     end.tiles = tiles < FEW_GROUPS ? tiles : FEW_GROUPS;
     xent_few_kernel<H, MT, RUN><<<(unsigned)end.tiles, 512, 0, c.st>>>((const H *)c.X, c.ldx, (const H *)c.W, c.ldw, c.D, end);
     FTK_TRY_HIP(hipGetLastError());
-    return launch_loss(c, end, loss, lse);
+    return launch_loss(c, end, nullptr, true, true, loss, lse);
 }
 template <typename H>
 static ftk_status launch_few(const XentCall &c, const SumEnd &end, float *loss, float *lse)
@@ -1040,7 +1053,7 @@ static ftk_status xent_forward(const XentCall &c, float *loss, float *lse)
     float *label_logit = (float *)(c.ws + p.label_logit);
     if constexpr (PLANES == 1) {
         if (p.few) {
-            const SumEnd end{Logits{c.bias, c.labels, c.N, 0, c.V, c.V, c.scale}, parts, 0, 0, label_logit};
+            const SumEnd end{Logits{c.bias, c.labels, c.N, 0, c.V, c.V, c.scale}, parts, 0, label_logit};
             return launch_few<H>(c, end, loss, lse);
         }
     }
@@ -1053,15 +1066,16 @@ static ftk_status xent_forward(const XentCall &c, float *loss, float *lse)
     g.segments = PLANES == 3 ? 6 : 1;
     g.splits = 1;
     const int tile = p.logits.tile;
-    const int64_t tiles = ceil_div(c.V, tile);
+    float2 *running = p.width < c.V ? (float2 *)(c.ws + p.running) : nullptr;
     for (int64_t first = 0; first < c.V; first += p.width) {
         const int64_t n = c.V - first < p.width ? c.V - first : p.width;
         Operand across;
         FTK_TRY((c.classes<T, H, PLANES>(first, n, first == 0 && !direct ? c.rows_job() : PackJob{}, nullptr, g.b, across)));
-        const SumEnd end{Logits{c.bias, c.labels, c.N, first, first + n, c.V, c.scale}, parts, tiles, first / tile, label_logit};
+        const SumEnd end{Logits{c.bias, c.labels, c.N, first, first + n, c.V, c.scale}, parts, ceil_div(n, tile), label_logit};
         FTK_TRY((launch_product<H, false, false>(g, tile, end, c.st)));
+        FTK_TRY(launch_loss(c, end, running, first == 0, first + n == c.V, loss, lse));
     }
-    return launch_loss(c, SumEnd{Logits{}, parts, tiles, 0, label_logit}, loss, lse);
+    return FTK_OK;
 }
 
 template <typename T, typename H, int PLANES>

@@ -158,6 +158,40 @@ def test_states_of_all_magnitudes():
         assert np.array_equal(numpy(vs[0]), decode(numpy(state.v[0]), numpy(state.v_scales[0]), 4))
 
 
+def test_more_elements_than_32_bits_count():
+    """The end of a tensor of 2^32 elements and some: its states exactly, from bits of their own."""
+    n, tail = (1 << 32) + 5000, 4500
+    p = torch.zeros(n, dtype=torch.bfloat16, device=DEV)
+    g = torch.zeros(n, dtype=torch.bfloat16, device=DEV)
+    rng = np.random.default_rng(3)
+    g[-tail:] = torch.from_numpy(rng.standard_normal(tail)).to(DEV)
+    state = ftk.AdamW([p], 8)
+    ftk.adamw_step(state, [g], torch.ones(1, dtype=torch.int64, device=DEV), seed=6)
+    assert not p[:n - tail].any() and not state.v[0][:n - tail].any()
+    lead = (n - tail) % 32  # whole blocks
+    grads = np.concatenate([np.zeros(lead), numpy(g[-tail:])])
+    m, v, w, _ = one_step(0 * grads, grads, 0 * grads, 0 * grads, 1)
+    key = mix64((mix64((mix64((6 + 0x9E3779B97F4A7C15) & M64) + 0) & M64) + 1) & M64)
+    x = np.arange(n - tail - lead - (1 << 32), n - (1 << 32), dtype=np.uint64) ^ np.uint64(key & 0xFFFFFFFF)
+    for shift, factor in ((16, 0xC8E1ED59), (15, 0x876BA2B3), (16, 1)):
+        x = ((x ^ (x >> np.uint64(shift))) * np.uint64(factor)) & np.uint64(0xFFFFFFFF)
+    r = x.astype(np.int64)
+    for codes, want in ((state.m[0], encode(m, 3, (r >> 16) / 65536.0)[0]), (state.v[0], encode(v, 4, (r & 0xFFFF) / 65536.0)[0])):
+        assert np.array_equal(numpy(codes[n - tail - lead:]), want)
+
+
+def test_empty_tensors_and_shared_gradients():
+    """Tensors without elements are passed over; one gradient may serve two weights."""
+    a, b, none = torch.ones(50, device=DEV), torch.ones(50, device=DEV), torch.ones(0, device=DEV)
+    state = ftk.AdamW([a, none, b], 8)
+    g = torch.linspace(-1, 1, 50, device=DEV)
+    ftk.adamw_step(state, [g, none.clone(), g], torch.ones(1, dtype=torch.int64, device=DEV))
+    assert torch.equal(a, b) and not torch.equal(a, torch.ones_like(a))
+    assert [t.numel() for t in ftk.adamw_moments(state)[0]] == [50, 0, 50]
+    ftk.adamw_step(state, [None, None, None], torch.ones(1, dtype=torch.int64, device=DEV))
+    assert torch.equal(a, b)
+
+
 def test_more_tensors_than_a_launch_takes():
     """With tensors left out here and there: those stay, the others keep their place in the list."""
     sizes = [1 + (i * 37) % 300 for i in range(170)]

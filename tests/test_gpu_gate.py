@@ -219,6 +219,44 @@ def test_graph_and_streams():
         torch.cuda.synchronize()
 
 
+def test_rows_far_apart():
+    """Row strides of 2^31 elements, and a million rows."""
+    for dtype in TYPES.values():
+        far = torch.empty((1 << 32) + 64, dtype=dtype, device=DEV)
+        z = far.as_strided((3, 20), (1 << 31, 1))
+        z.copy_(torch.randn(3, 20, device=DEV))
+        a, b = ftk.route_gate(z, 3), ftk.route_gate(z.contiguous(), 3)
+        assert torch.equal(a.labels, b.labels) and torch.equal(a.loss, b.loss)
+        dw, dl = torch.randn(3, 3, device=DEV), torch.ones(1, device=DEV)
+        want = ftk.route_gate_grad(z.contiguous(), b, dw, dl)
+        assert torch.equal(ftk.route_gate_grad(z, a, dw, dl, out=z), want)
+        del far, z
+    z = torch.randn(1 << 20, 8, device=DEV)
+    gate = ftk.route_gate(z, 2)
+    top = z.double().topk(2, dim=1)
+    assert torch.equal(gate.labels.long(), top.indices) and int(gate.counts[-1]) == 1 << 20
+    p = torch.softmax(z.double(), 1).mean(0)
+    assert ((gate.probs.double() - p).abs() <= 1e-5 * p).all()
+    assert torch.equal(gate.counts[:-1].long(), torch.bincount(gate.labels.flatten(), minlength=8))
+
+
+def test_calls_at_once():
+    """Two streams, each with its own workspace."""
+    g = torch.Generator(device=DEV).manual_seed(11)
+    zs = [torch.randn(3000, 100, generator=g, device=DEV) for _ in range(2)]
+    want = [ftk.route_gate(z, 4) for z in zs]
+    streams = [torch.cuda.Stream() for _ in zs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = []
+        for z, st in zip(zs, streams):
+            with torch.cuda.stream(st):
+                got.append(ftk.route_gate(z, 4))
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert all(torch.equal(getattr(a, n), getattr(b, n)) for n in ("labels", "weights", "lse", "counts", "probs", "loss"))
+
+
 def test_counts_of_several_parts():
     """Counts summed over parts of a batch give every part the whole batch's gradient."""
     g = torch.Generator(device=DEV).manual_seed(4)

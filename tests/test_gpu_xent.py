@@ -99,17 +99,20 @@ def test_few_rows(N, V, D, dtype):
     check(*problem(N, V, D, dtype, bias=V % 2 == 1))
 
 
-@pytest.mark.parametrize("dtype", TYPES)
-def test_pieces_of_the_classes(dtype):
-    """So many rows that the classes go in several pieces: gradients of the rows are added up over them."""
-    check(*problem(12000, 9000, 72, dtype, bias=True))
+@pytest.mark.parametrize("N,V,D,dtype", [(12000, 9000, 72, "f32"), (12000, 14000, 72, "bf16"), (12000, 14000, 64, "f16"),
+                                         (150000, 1700, 16, "bf16"), (150000, 4000, 16, "f32")])
+def test_pieces_of_the_classes(N, V, D, dtype):
+    """So many rows that the classes go in several pieces: sums and gradients of the rows are added up over them."""
+    check(*problem(N, V, D, dtype, bias=True))
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("D,ldx,ldw,shift", [(64, 80, 72, 8), (64, 64, 67, 0), (33, 40, 50, 1), (40, 41, 40, 3), (1, 3, 5, 1)])
-def test_strides_and_addresses(D, ldx, ldw, shift, dtype):
+@pytest.mark.parametrize("N", [90, 10])
+@pytest.mark.parametrize("D,ldx,ldw,shift", [(64, 80, 72, 8), (64, 64, 67, 0), (33, 40, 50, 1), (40, 41, 40, 3), (1, 3, 5, 1),
+                                             (128, 131, 136, 8)])
+def test_strides_and_addresses(D, ldx, ldw, shift, N, dtype):
     """Rows of wider arrays, NaN between and around them, at addresses of every alignment; results likewise."""
-    N, V, t = 90, 140, TYPES[dtype]
+    V, t = 140, TYPES[dtype]
     X, W, labels, b, dloss = problem(N, V, D, dtype, bias=True)
 
     def inside(a, ld):
@@ -122,8 +125,9 @@ def test_strides_and_addresses(D, ldx, ldw, shift, dtype):
     got, grads = check(x, w, labels, b, dloss, scale=0.7, dX=dX, dW=dW)
     assert grads[0] is dX and grads[1] is dW
     assert int(around.isnan().sum()) == around.numel() - N * D and int(beside.isnan().sum()) == beside.numel() - V * D
-    plain = ftk.xent(X, W, labels, bias=b, scale=0.7)
-    assert torch.equal(plain[0], got[0]) and torch.equal(plain[1], got[1])
+    plain, _ = check(X, W, labels, b, dloss, scale=0.7)
+    if N > 32:  # (few rows are added up in another order where their classes lie aligned)
+        assert torch.equal(plain[0], got[0]) and torch.equal(plain[1], got[1])
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -170,6 +174,43 @@ def test_large_logits():
     """Logits of some thousands: nothing overflows, the loss is their difference."""
     X, W, labels, b, dloss = problem(50, 300, 64, "bf16", spread=800.0)
     check(X, W, labels, b, dloss)
+
+
+def test_offsets_beyond_32_bits():
+    """Classes' rows of more than 2^32 elements, and few rows at strides as long: what lies at the end is read and written."""
+    V, D = (1 << 21) + 777, 2048
+    W = torch.empty(V, D, dtype=torch.bfloat16, device=DEV)
+    W[:V - 1000] = 0  # (equal logits but for the last classes)
+    W[V - 1000:] = torch.randn(1000, D, device=DEV)
+    for N in (8, 70):
+        X = (torch.randn(N, D, device=DEV) * D ** -0.5).bfloat16()
+        labels = torch.arange(V - N, V, dtype=torch.int32, device=DEV)
+        loss, lse = ftk.xent(X, W, labels)
+        z = X.double() @ W[V - 1000:].double().t()
+        want = (z.exp().sum(1) + (V - 1000)).log()
+        assert ((lse.double() - want).abs() < 1e-5).all()
+        assert ((loss.double() - (want - z[torch.arange(N), torch.arange(1000 - N, 1000)])).abs() < 2e-5).all()
+    dloss = torch.ones(N, device=DEV)
+    dX, dW, _ = ftk.xent_grad(X, W, labels, lse, dloss)
+    d = (z - want.unsqueeze(1)).exp()
+    d[torch.arange(N), torch.arange(1000 - N, 1000)] -= 1
+    x = X.double()
+    size = d.abs() @ W[V - 1000:].double().abs()
+    assert ((dX.double() - d @ W[V - 1000:].double()).abs() <= 2 * 2.0 ** -8 * size + 1e-30).all()
+    assert ((dW[V - 1000:].double() - d.t() @ x).abs() <= 2 * 2.0 ** -8 * (d.t().abs() @ x.abs()) + 1e-30).all()
+    del W, dW
+    for dtype in TYPES.values():
+        far = torch.empty((1 << 32) // dtype.itemsize * 2 + 64, dtype=dtype, device=DEV)
+        ld = (1 << 32) // dtype.itemsize
+        x, w = far.as_strided((3, 32), (ld, 1)), far.as_strided((3, 32), (ld, 1), 32)
+        x.copy_(torch.randn(3, 32, device=DEV)), w.copy_(torch.randn(3, 32, device=DEV))
+        labels = torch.tensor([0, 2, 1], dtype=torch.int32, device=DEV)
+        a, b = ftk.xent(x, w, labels), ftk.xent(x.contiguous(), w.contiguous(), labels)
+        assert torch.equal(a[0], b[0])
+        for p, q in zip(ftk.xent_grad(x, w, labels, a[1], torch.ones(3, device=DEV)),
+                        ftk.xent_grad(x.contiguous(), w.contiguous(), labels, a[1], torch.ones(3, device=DEV))):
+            assert p is None or torch.equal(p, q)
+        del far, x, w
 
 
 def test_assignment_scores():
