@@ -252,7 +252,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product g, End e
     // into the registers just used, and those of the columns, which the next step needs first, behind the first ones.  The first step of a stage reads the second one's.  The second step reads the next stage's:
     // after its first row tiles all waves meet, when what the first step read has long come, this stage's place is free for
     // the one after the next, and the next one has arrived.
-    constexpr int MEET = S::MT / 4;
+    constexpr int MEET = S::MT / 8;
     auto step = [&](auto which, auto reads, auto copies, int n) __attribute__((always_inline)) {
         constexpr int s = decltype(which)::value, next = 1 - s, FROM = s ? MEET : 0;
         constexpr bool READS = decltype(reads)::value, COPY = decltype(copies)::value;
@@ -859,7 +859,7 @@ static XentPlan::Cut cut_of(int64_t rows, int64_t cols, int64_t stages, bool sha
     double least = 1e300;
     for (const auto &s : shapes) {
         const int64_t tiles = ceil_div(rows, s.tile) * ceil_div(cols, s.tile);
-        for (int splits = 1; splits <= (shares ? 64 : 1) && splits * 4 - 3 <= stages; splits *= 2) {
+        for (int splits = 1; splits <= (shares ? 64 : 1) && splits * 4 - 3 <= stages; ++splits) {
             if (splits > 1 && tiles * splits > 256 * s.at_once) break;
             const int64_t groups = ceil_div(tiles * splits, 256);  // of a compute unit
             const double each = groups < s.at_once ? groups : s.at_once, stage = s.shared * each > s.alone ? s.shared * each : s.alone;
