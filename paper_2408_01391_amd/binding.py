@@ -946,6 +946,13 @@ class AdamW:
             raise ValueError("weights or states overlap")
 
 
+def _alike(tensors, counts, dtype, device):
+    """Contiguous tensors of so many elements, one type and one device (a list of hundreds is gone through at every step)."""
+    T = torch.Tensor
+    return (list(map(T.numel, tensors)) == counts and set(map(T.get_device, tensors)) == {device} and all(map(T.is_contiguous, tensors))
+            and {t.dtype for t in tensors} == {dtype})
+
+
 def adamw_step(state, grads, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, seed=0, lr_scale=None, grad_scale=None):
     """One AdamW step over all of state's weights, in place.  grads: a contiguous tensor for each weight, of one type (float32 or the
     weights'; float32 weights: any), or None: that weight stays.  step: int64 device tensor of one element, 1 at the first
@@ -960,8 +967,7 @@ def adamw_step(state, grads, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, we
     if len(given) < len(counts):
         counts = [n for n, g in zip(counts, grads) if g is not None]
     dtype, device = given[0].dtype, state.params[0].get_device()
-    if ([g.numel() for g in given] != counts or {g.dtype for g in given} != {dtype} or {g.get_device() for g in given} != {device}
-            or not all([g.is_contiguous() for g in given])):
+    if not _alike(given, counts, dtype, device):
         raise ValueError("gradients must be contiguous tensors of one type with the weights' elements, on their device")
     state._grads[1::8] = [0 if g is None else g.data_ptr() for g in grads]
     code = _MX_DTYPES.get(dtype)
@@ -985,11 +991,10 @@ def adamw_moments(state, out=None, dtype=torch.float32):
         out = [[torch.empty_like(p, dtype=dtype) for p in state.params] for _ in range(2)]
     dtype, device, lists = out[0][0].dtype, state.params[0].get_device(), []
     for ts in out:
-        if ([t.numel() for t in ts] != state._counts or {t.dtype for t in ts} != {dtype} or {t.get_device() for t in ts} != {device}
-                or not all([t.is_contiguous() for t in ts])):
+        if not _alike(ts, state._counts, dtype, device):
             raise ValueError("out must be two lists of contiguous tensors of one type with the weights' elements, on their device")
         pointers = (ctypes.c_void_p * len(ts))()
-        pointers[:] = [t.data_ptr() for t in ts]
+        pointers[:] = list(map(torch.Tensor.data_ptr, ts))
         lists.append(pointers)
     _here(state.params[0])
     _check(load().ftk_adamw_moments(_row_code(out[0][0], "out", _MX_DTYPES), state._table, len(state.params), lists[0], lists[1], _stream()))
