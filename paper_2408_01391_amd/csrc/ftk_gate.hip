@@ -48,6 +48,8 @@ struct GateGradArgs {
 };
 
 constexpr float LOG2E = 1.44269504f;
+// (of differences: a largest logit of the type's lowest value times LOG2E would be no number)
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
 
 // Largest over the L lanes of a group.
 template <int L>
@@ -197,10 +199,10 @@ __device__ __forceinline__ void join_softmax(const uint32_t *at, int stride, flo
         t[i] = __uint_as_float(at[i * stride]);
         all = fmaxf(all, t[i]);
     }
-    const float shift = all > NONE ? all * LOG2E : 0.f;
+    const float shift = all > NONE ? all : 0.f;
     sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sum += __uint_as_float(at[i * stride + 1]) * __builtin_amdgcn_exp2f(fmaf(t[i], LOG2E, -shift));
+    for (int i = 0; i < 4; ++i) sum += __uint_as_float(at[i * stride + 1]) * exp_of(t[i] - shift);
     top = all;
 }
 
@@ -351,11 +353,11 @@ __global__ __launch_bounds__((64 * GATE_WAVES<T, L, NP>), (NP * PIECE<T> > 16 ? 
         constexpr int W = Group<L>::WIDTH;
         top = group_max<W>(top);
         const bool any = top > NONE;
-        const float own = any ? top * LOG2E : 0.f;
+        const float own = any ? top : 0.f;
         float e[R::V];
 #pragma unroll
         for (int i = 0; i < R::V; ++i) {
-            e[i] = __builtin_amdgcn_exp2f(fmaf(v[i], LOG2E, -own));
+            e[i] = exp_of(v[i] - own);
             sum += e[i];
         }
         sum = group_sum<W>(sum);
@@ -370,16 +372,16 @@ __global__ __launch_bounds__((64 * GATE_WAVES<T, L, NP>), (NP * PIECE<T> > 16 ? 
         }
         if constexpr (!LIST_FIRST) best_of<T, L, NP, K>(group, l, a.k, v, top, sum, value, label);
         const bool some = top > NONE;
-        const float shift = some ? top * LOG2E : 0.f;
+        const float shift = some ? top : 0.f;
         // a NaN among the logits, or +infinity, makes the sum NaN: no labels, and weights and loss tell
         const bool bad = sum != sum;
         const float inv = some || bad ? 1.f / sum : 0.f;
         float mine = here ? inv : 0.f;
-        if (L > 64) mine *= any || bad ? __builtin_amdgcn_exp2f(own - shift) : 0.f;
+        if (L > 64) mine *= any || bad ? exp_of(own - shift) : 0.f;
 #pragma unroll
         for (int i = 0; i < R::V; ++i) acc[i] = fmaf(e[i], mine, acc[i]);
         const bool held = value > NONE && !bad && l < a.k;
-        const float ev = held ? __builtin_amdgcn_exp2f(fmaf(value, LOG2E, -shift)) : 0.f;
+        const float ev = held ? exp_of(value - shift) : 0.f;
         const float chosen = group_sum<Group<L>::WIDTH>(ev);
         if (here && l < a.k) {
             const float wt = bad ? __builtin_nanf("") : !held ? 0.f : a.normalise ? ev / chosen : ev * inv;
@@ -545,7 +547,7 @@ __global__ __launch_bounds__(64 * GATE_GRAD_WAVES, (NP * PIECE<T> > 16 ? 2 : 4))
     for (; first < a.N; first += step, t += step) {
         const bool here = t < a.N, chosen = label < (uint32_t)a.E;
         const uint32_t at_label = label;
-        const float shift = lse * LOG2E, w_here = wt;
+        const float shift = lse, w_here = wt;
         const bool none = lse == NONE;
         float p[R::V], add = chosen ? wt * dw : 0.f, dot = 0.f;
 #pragma unroll
@@ -556,10 +558,21 @@ __global__ __launch_bounds__(64 * GATE_GRAD_WAVES, (NP * PIECE<T> > 16 ? 2 : 4))
         if (chosen) atomicAdd(&add_of[at_label], add);
 #pragma unroll
         for (int i = 0; i < R::V; ++i) {
-            p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], LOG2E, -shift));
+            p[i] = exp_of(p[i] - shift);
             p[i] = none ? 0.f : p[i];
-            dot = fmaf(p[i], c[i], dot);
         }
+        // where half a step of lse is no longer small: by their own sum (a row of masks of the type's lowest value)
+        if (__any(fabsf(shift) > 64.f)) {
+            float all = 0.f;
+#pragma unroll
+            for (int i = 0; i < R::V; ++i) all += p[i];
+            all = group.sum(all);
+            all = none || !(fabsf(shift) > 64.f) ? 1.f : 1.f / all;
+#pragma unroll
+            for (int i = 0; i < R::V; ++i) p[i] *= all;
+        }
+#pragma unroll
+        for (int i = 0; i < R::V; ++i) dot = fmaf(p[i], c[i], dot);
         dot = group.sum(dot) + (a.normalise ? 0.f : inner);
         if (a.dweights) {
 #pragma unroll

@@ -374,11 +374,12 @@ struct SumEnd {
             }
             top = fmaxf(top, __shfl_xor(top, 16, 64));
             top = fmaxf(top, __shfl_xor(top, 32, 64));
-            const float shift = top > -__builtin_inff() ? top * XENT_LOG2E : 0.f;
+            // (subtracted before the factor: a part may hold masks of the type's lowest value alone)
+            const float shift = top > -__builtin_inff() ? top : 0.f;
 #pragma unroll
             for (int j = 0; j < S::NT; ++j)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][c], XENT_LOG2E, -shift));
+                for (int c = 0; c < 4; ++c) sum += exp2_of(acc[i][j][c] - shift);
             sum += __shfl_xor(sum, 16, 64);
             sum += __shfl_xor(sum, 32, 64);
             if (q == 0) part[at.wn / (16 * S::NT) * S::TM + row] = float2{top, sum};
@@ -571,14 +572,14 @@ struct GradEnd {
             const int32_t label = in ? z.labels[n] : -1;
             const bool live = label >= 0 && label < z.V;
             // (an ignored row's, and that of a row without any finite logit: all probabilities are 0)
-            const float l = live ? lse[n] : -__builtin_inff(), shift = l == -__builtin_inff() ? __builtin_inff() : l * XENT_LOG2E;
+            const float l = live ? lse[n] : -__builtin_inff(), shift = l == -__builtin_inff() ? __builtin_inff() : l;
             const float g = live ? dloss[n] * factor : 0.f;
             const int rel = z.label_from(label, v0);
 #pragma unroll
             for (int j = 0; j < S::NT; ++j)
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
-                    acc[i][j][c] = __builtin_amdgcn_exp2f(fmaf(fmaf(z.scale, acc[i][j][c], bias[j][c]), XENT_LOG2E, -shift));
+                    acc[i][j][c] = exp2_of(fmaf(z.scale, acc[i][j][c], bias[j][c]) - shift);
             if (__any(rel >= 0 && rel < 16 * S::NT)) {
 #pragma unroll
                 for (int j = 0; j < S::NT; ++j)

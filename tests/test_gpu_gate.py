@@ -285,3 +285,37 @@ def test_refusals():
         ftk.route_gate(z.double(), 2)
     with pytest.raises(ftk.FtkError):
         ftk.route_gate_grad(z, gate)
+
+
+@pytest.mark.parametrize("normalise", [True, False])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,E,k", [(9, 5, 2), (70, 64, 4), (300, 65, 8), (33, 600, 9), (6, 2100, 2), (5, 8192, 64)])
+def test_masks_of_the_lowest_value(N, E, k, dtype, normalise):
+    """Experts masked by the type's lowest value: long runs of them, all but one, and whole rows, whose experts are all alike."""
+    rng = np.random.default_rng(N + E)
+    t = TYPES[dtype]
+    logits = logits_of(rng, N, E, t, masked=False)
+    low = torch.finfo(t).min
+    logits[::2, E // 4:] = low
+    logits[1, :-1] = low
+    logits[2] = low
+    logits[N - 1, : E // 2 + 1] = low
+    logits[4] = 1e4  # (equal ones as large as fp16 holds)
+    z = f64(logits)
+    gate = ftk.route_gate(logits, k, normalise=normalise)
+    labels = choice(z, k)
+    assert np.array_equal(gate.labels.cpu().numpy(), labels)
+    p, lse = probabilities(z)
+    counts = np.concatenate([np.bincount(labels.ravel(), minlength=E), [N]])
+    assert np.array_equal(gate.counts.cpu().numpy(), counts)
+    w, loss = outputs(z, labels, counts, normalise)
+    tol = relative(E)
+    assert (abs(f64(gate.weights) - w) <= 3 * tol * w).all()
+    assert (abs(f64(gate.lse) - lse) <= tol + 2.0 ** -23 * abs(lse)).all()
+    assert abs(float(gate.loss) - loss) <= (4 * tol + (N + 40) * 2.0 ** -24) * loss
+    dw = torch.from_numpy(rng.standard_normal((N, k))).to(DEV).float()
+    dloss = torch.tensor([0.7], device=DEV)
+    dz = ftk.route_gate_grad(logits, gate, dw, dloss)
+    want, size = gradient(z, labels, counts, normalise, f64(dw), 0.7)
+    # as elsewhere; a probability divided by the sum of them (E / 16 additions in a lane at most) is off by its rounding besides
+    assert (abs(f64(dz) - want) <= (6 * tol + (E / 16 + 16) * 2.0 ** -24) * size + HALF[t] * abs(want) * 1.01 + 2.0 ** -25).all()

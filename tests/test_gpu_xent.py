@@ -291,3 +291,26 @@ def test_refusals():
         ftk.xent(X, W, labels, scale=INF)
     with pytest.raises(ftk.FtkError):
         ftk.xent(X, W, labels, workspace=torch.empty(300, dtype=torch.uint8, device=DEV))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,V,D", [(7, 900, 128), (30, 3000, 256), (300, 900, 72), (2500, 4000, 256)])
+def test_masks_of_the_lowest_value(N, V, D, dtype):
+    """A bias of the 32-bit type's lowest value, on whole tiles and single classes, closes them as -infinity does."""
+    X, W, labels, b, dloss = problem(N, V, D, dtype, bias=True)
+    shut = torch.zeros(V, dtype=torch.bool, device=DEV)
+    shut[V // 3:V // 3 + 600] = True
+    shut[::5] = True
+    labels = torch.where(shut[labels.clamp(0, V - 1).long()], 1 + 0 * labels, labels)  # (an open class)
+    low, closed = b.masked_fill(shut, torch.finfo(torch.float32).min), b.masked_fill(shut, -INF)
+    got, want = ftk.xent(X, W, labels, bias=low), ftk.xent(X, W, labels, bias=closed)
+    assert got[0].isfinite().all() and all(torch.equal(a, c) for a, c in zip(got, want))
+    grads = [ftk.xent_grad(X, W, labels, got[1], dloss, bias=bias, need=(True, True, True)) for bias in (low, closed)]
+    assert all(a.isfinite().all() and torch.equal(a, c) for a, c in zip(*grads))
+    # a label there: its loss is as large; and all classes: their logits are that value, the logarithm of their number vanishes
+    labels[N // 2] = V // 3 + 7
+    loss, lse = ftk.xent(X, W, labels, bias=low)
+    assert loss[N // 2] > 3e38 and lse[N // 2].isfinite()
+    loss, lse = ftk.xent(X, W, labels, bias=torch.full_like(b, torch.finfo(torch.float32).min))
+    live = (labels >= 0) & (labels < V)
+    assert (lse[live] == torch.finfo(torch.float32).min).all() and (loss == 0).all()
