@@ -899,7 +899,8 @@ class _AdamwOptions(ctypes.Structure):
 
 
 class AdamW:
-    """Weights and their states for adamw_step: contiguous device tensors of one type (float32, bfloat16 or float16), not overlapping.
+    """Weights and their states for adamw_step: contiguous device tensors of one type (float32, bfloat16 or float16), not overlapping,
+    which stay where they are in memory.
 
     bits: 32 (m, v float32) or 8 (m, v uint8 codes and a scale byte for every 32 elements).  States that are not given start at
     zero.  master: float32 copies of 16-bit weights; True makes them from the weights."""
@@ -938,6 +939,7 @@ class AdamW:
                     setattr(row, "param" if name == "params" else name, t.data_ptr())
                     spans.append((t.data_ptr(), t.data_ptr() + need * t.element_size()))
         self._counts = [p.numel() for p in self.params]
+        self._places = [p.data_ptr() for p in self.params]
         for n, row in zip(self._counts, self._table):
             row.count = n
         self._grads = (ctypes.c_uint64 * (8 * len(self.params))).from_buffer(self._table)  # the table by words, the gradient's is the second
@@ -969,6 +971,8 @@ def adamw_step(state, grads, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, we
     dtype, device = given[0].dtype, state.params[0].get_device()
     if not _alike(given, counts, dtype, device):
         raise ValueError("gradients must be contiguous tensors of one type with the weights' elements, on their device")
+    if list(map(torch.Tensor.data_ptr, state.params)) != state._places:
+        raise ValueError("weights have moved since their state was made")
     state._grads[1::8] = [0 if g is None else g.data_ptr() for g in grads]
     code = _MX_DTYPES.get(dtype)
     if code is None:

@@ -322,3 +322,14 @@ def test_refusals():
         ftk.adamw_step(state, [p.double()], step)
     with pytest.raises(ftk.FtkError):
         ftk.adamw_step(state, [p.clone()], step, beta1=1.0)
+
+
+def test_weights_that_moved():
+    """Weights that a program laid elsewhere are not looked for at their old place."""
+    p = torch.nn.Parameter(torch.ones(40, device=DEV))
+    state, step = ftk.AdamW([p]), torch.ones(1, dtype=torch.int64, device=DEV)
+    old = p.data
+    p.data = old.clone()
+    with pytest.raises(ValueError):
+        ftk.adamw_step(state, [torch.ones_like(old)], step)
+    assert (old == 1).all() and (p == 1).all()
