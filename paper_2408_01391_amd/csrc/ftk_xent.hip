@@ -41,7 +41,6 @@ struct Product {
     Operand a, b;  // the result's rows and columns
     uint32_t mt, nt;  // tiles
     int stages;  // of a segment
-    int segments;  // 1, or 6: products of pieces
     int splits;  // workgroups that share a tile's stages out between them
 };
 
@@ -50,6 +49,8 @@ struct Shape {
     static constexpr int MT = MT_, NT = NT_, WM = WM_, WN = WN_, WAVES = WM * WN, THREADS = 64 * WAVES;
     static constexpr int TM = 16 * MT * WM, TN = 16 * NT * WN;
     static constexpr int A = TM * 128, STAGE = (TM + TN) * 128, LDS = 2 * STAGE;
+    // of 32 elements of three pieces
+    static constexpr int A3 = TM * 64, B3 = TN * 64, STAGE3 = 3 * (A3 + B3), LDS3 = 3 * STAGE3;
 };
 
 // What a workgroup's end knows of its place.
@@ -69,10 +70,14 @@ __device__ __forceinline__ int line_of(int i, int r)
 }
 
 // Pieces of 16 bytes are stored at their place xor a key, so that lanes that read together meet all banks.
-// Along k (lines of 8 pieces): the rows that 16 lanes read differ in the key or in parity.
-template <bool PERMUTED>
+// Along k: the rows that 16 lanes read differ in the key or in their place among 256 bytes (lines of 8 pieces, or of 4).
+template <bool PERMUTED, int K>
 __device__ __forceinline__ int line_key(int row)
 {
+    if (K == 32) {  // (of four rows: 0, 2, 3, 1; quarters of 64 lanes are read crosswise)
+        const int x = row >> (PERMUTED ? 3 : 2);
+        return (x >> 1 & 1) | ((x ^ x >> 1) & 1) << 1;
+    }
     return PERMUTED ? ((row >> 1) & 1) | ((row >> 3) & 3) << 1 : (row >> 1) & 7;
 }
 // Across k (T columns, T / 8 pieces a row): four rows of k, four pieces each.
@@ -82,10 +87,11 @@ __device__ __forceinline__ int across_key(int k)
     return T >= 128 ? (k & 3) * 4 : (k >> 1 & 1) * 4;
 }
 
-// Copies of one operand's tile of T rows (columns) to LDS, a share of them a wave.
-template <int T, int WAVES, bool ACROSS, bool PERMUTED>
+// Copies of one operand's tile of T rows (columns) by K elements of k to LDS, a share of them a wave.
+template <int T, int WAVES, bool ACROSS, bool PERMUTED, int K>
 struct Copies {
-    static constexpr int N = T / 8 / WAVES;  // of a wave
+    static constexpr int N = T * K / 512 / WAVES;  // of a wave
+    static constexpr int LINE = K / 8;             // pieces of a line along k
     uint32_t off[N];
     const uint8_t *base;
     int64_t step;  // bytes of a stage
@@ -93,12 +99,13 @@ struct Copies {
     static __device__ __forceinline__ int piece_of(int c, int lane)
     {
         if (ACROSS) return (lane & (T / 8 - 1)) ^ across_key<T>(k_of(c, lane));
-        return (lane & 7) ^ line_key<PERMUTED>(c * 8 + (lane >> 3));
+        return (lane & (LINE - 1)) ^ line_key<PERMUTED, K>(row_of(c, lane));
     }
+    static __device__ __forceinline__ int row_of(int c, int lane) { return c * (64 / LINE) + lane / LINE; }
     __device__ __forceinline__ void begin(const Operand &o, int64_t first, int w, int lane)
     {
         base = (const uint8_t *)(o.p + (ACROSS ? first : first * o.ld));
-        step = ACROSS ? XENT_STAGE * o.ld * 2 : XENT_STAGE * 2;
+        step = ACROSS ? K * o.ld * 2 : K * 2;
         const int64_t left = o.outer - first;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -108,12 +115,12 @@ struct Copies {
                 if (piece * 8 >= left) piece = 0;
                 off[i] = (uint32_t)k_of(c, lane) * (uint32_t)o.ld * 2 + piece * 16;
             } else {
-                const int64_t row = c * 8 + (lane >> 3);
+                const int64_t row = row_of(c, lane);
                 off[i] = (uint32_t)(row < left ? row : left - 1) * (uint32_t)o.ld * 2 + piece * 16;
             }
         }
     }
-    // where stage st of a segment begins, for piece `plane` of the rows
+    // where stage st begins, of piece `plane` of the rows
     __device__ __forceinline__ const uint8_t *from(const Operand &o, int plane, int st) const
     {
         return uniform(base + plane * o.plane * 2 + st * step);
@@ -123,7 +130,7 @@ struct Copies {
     {
         const int c = w * N + i;
         uint32_t at = off[i];
-        if (left < XENT_STAGE) {
+        if (left < K) {
             asm volatile("");  // (a branch that is hardly ever taken, rather than its arithmetic every time)
             if (ACROSS) {
                 const int k = k_of(c, lane);
@@ -137,7 +144,7 @@ struct Copies {
 };
 
 // Fragments of one operand: 16 rows (columns), lane quarter q has elements 8 q ... of a step of 32.
-template <int T, bool ACROSS, bool PERMUTED>
+template <int T, bool ACROSS, bool PERMUTED, int K>
 struct Fragments {
     // first: of the wave's rows within the tile
     static __device__ __forceinline__ half8 read(const uint8_t *lds, int first, int i, int s, int lane)
@@ -153,7 +160,7 @@ struct Fragments {
             return __builtin_bit_cast(half8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
             const int row = first + line_of<PERMUTED>(i, r);
-            return *reinterpret_cast<const half8 *>(lds + row * 128 + ((s * 4 + q) ^ line_key<PERMUTED>(row)) * 16);
+            return *reinterpret_cast<const half8 *>(lds + row * (K * 2) + ((s * 4 + q) ^ line_key<PERMUTED, K>(row)) * 16);
         }
     }
 };
@@ -168,20 +175,36 @@ __device__ __forceinline__ float4v mma(half8 b, half8 a, float4v c)
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(vec, b), __builtin_bit_cast(vec, a), c, 0, 0, 0);
 }
 
-// The pieces of segment g, the small products first.
-__device__ __forceinline__ int plane_a(int segments, int g) { return segments == 1 ? 0 : g == 0 ? 2 : g == 1 || g == 3 ? 1 : 0; }
-__device__ __forceinline__ int plane_b(int segments, int g) { return segments == 1 ? 0 : g == 2 ? 2 : g == 1 || g == 4 ? 1 : 0; }
-
 // Workgroups are dealt to the eight XCDs in turn; each XCD gets a run of tiles, eight rows of tiles high, so that the 32 tiles
-// under way there share their operands in its L2.
-__device__ __forceinline__ void tile_of(const Product &g, uint32_t t, uint32_t &mtile, uint32_t &ntile)
+// under way there share their operands in its L2.  Shares of the stages come one after the other: those of one share read the same.
+template <typename S>
+__device__ __forceinline__ Place place_of(const Product &g, int w)
 {
-    const uint32_t all = g.mt * g.nt, each = (all + 7) / 8;
-    const uint32_t x = t & 7, full = all & 7;  // the first `full` XCDs have one more where all is no multiple
-    t = full ? x * (each - 1) + min(x, full) + (t >> 3) : x * each + (t >> 3);
+    const uint32_t tiles = g.mt * g.nt, all = tiles * g.splits, each = (all + 7) / 8;
+    const uint32_t x = blockIdx.x & 7, full = all & 7;  // the first `full` XCDs have one more where all is no multiple
+    uint32_t t = full ? x * (each - 1) + min(x, full) + (blockIdx.x >> 3) : x * each + (blockIdx.x >> 3);
+    Place at;
+    at.split = g.splits > 1 ? (int)(t / tiles) : 0;
+    t -= at.split * tiles;
     const uint32_t panel = t / (8 * g.nt), in = t - panel * 8 * g.nt, high = min(8u, g.mt - panel * 8);
-    ntile = in / high;
-    mtile = panel * 8 + (in - ntile * high);
+    at.ntile = in / high;
+    at.mtile = panel * 8 + (in - at.ntile * high);
+    at.m0 = (int64_t)at.mtile * S::TM;
+    at.n0 = (int64_t)at.ntile * S::TN;
+    at.wm = w / S::WN * 16 * S::MT;
+    at.wn = w % S::WN * 16 * S::NT;
+    return at;
+}
+
+// A workgroup's share of the stages.
+struct Run {
+    int first, stages;
+};
+__device__ __forceinline__ Run run_of(const Product &g, int split)
+{
+    if (g.splits == 1) return Run{0, g.stages};
+    const int first = (int)((uint64_t)g.stages * split / (uint32_t)g.splits);
+    return Run{first, (int)((uint64_t)g.stages * (split + 1) / (uint32_t)g.splits) - first};
 }
 
 template <typename S, typename H, bool AT, bool BT, typename End>
@@ -190,63 +213,39 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product g, End e
     extern __shared__ __align__(16) uint8_t lds[];
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    Place at;
-    at.split = g.splits > 1 ? (int)(blockIdx.x / (g.mt * g.nt)) : 0;
-    tile_of(g, blockIdx.x - at.split * (g.mt * g.nt), at.mtile, at.ntile);
-    at.m0 = (int64_t)at.mtile * S::TM;
-    at.n0 = (int64_t)at.ntile * S::TN;
-    at.wm = w / S::WN * 16 * S::MT;
-    at.wn = w % S::WN * 16 * S::NT;
+    const Place at = place_of<S>(g, w);
     float4v acc[S::MT][S::NT];
 #pragma unroll
     for (int i = 0; i < S::MT; ++i)
 #pragma unroll
         for (int j = 0; j < S::NT; ++j) acc[i][j] = float4v{0, 0, 0, 0};
-    Copies<S::TM, S::WAVES, AT, false> ca;
-    Copies<S::TN, S::WAVES, BT, true> cb;
+    Copies<S::TM, S::WAVES, AT, false, XENT_STAGE> ca;
+    Copies<S::TN, S::WAVES, BT, true, XENT_STAGE> cb;
     ca.begin(g.a, at.m0, w, lane);
     cb.begin(g.b, at.n0, w, lane);
-    const int all = g.stages * g.segments;
-    int seg = 0, st = 0, total = all;  // of the next copy; stages of this workgroup
-    if (g.splits > 1) {
-        const uint32_t begin = (uint64_t)all * at.split / (uint32_t)g.splits;
-        total = (int)((uint64_t)all * (at.split + 1) / (uint32_t)g.splits - begin);
-        seg = (int)(begin / g.stages);
-        st = (int)(begin - seg * g.stages);
-    }
+    const Run run = run_of(g, at.split);
+    const int total = run.stages;
     constexpr int COPIES = ca.N + cb.N;
-    const uint8_t *from_a, *from_b;
-    int left_a, left_b;
-    auto aim = [&]() __attribute__((always_inline)) {
-        from_a = ca.from(g.a, plane_a(g.segments, seg), st);
-        from_b = cb.from(g.b, plane_b(g.segments, seg), st);
-        left_a = (int)(g.a.inner - (int64_t)st * XENT_STAGE);
-        left_b = (int)(g.b.inner - (int64_t)st * XENT_STAGE);
-    };
+    // of the next copy
+    const uint8_t *from_a = ca.from(g.a, 0, run.first), *from_b = cb.from(g.b, 0, run.first);
+    int left_a = (int)(g.a.inner - (int64_t)run.first * XENT_STAGE), left_b = (int)(g.b.inner - (int64_t)run.first * XENT_STAGE);
     auto copy = [&](int buffer, int c) __attribute__((always_inline)) {
         const uint32_t to = lds0 + buffer * S::STAGE;
         if (c < ca.N) ca.copy(g.a, from_a, left_a, to, w, lane, c);
         else cb.copy(g.b, from_b, left_b, to + S::A, w, lane, c - ca.N);
     };
     auto copied = [&]() __attribute__((always_inline)) {
-        if (++st < g.stages) {
-            from_a += ca.step;
-            from_b += cb.step;
-            left_a -= XENT_STAGE;
-            left_b -= XENT_STAGE;
-        } else {
-            st = 0;
-            ++seg;
-            aim();
-        }
+        from_a += ca.step;
+        from_b += cb.step;
+        left_a -= XENT_STAGE;
+        left_b -= XENT_STAGE;
     };
-    aim();
     half8 a[S::MT], b[2][S::NT];
     auto read_a = [&](int n, int s, int i) __attribute__((always_inline)) {
-        a[i] = Fragments<S::TM, AT, false>::read(lds + (n & 1) * S::STAGE, at.wm, i, s, lane);
+        a[i] = Fragments<S::TM, AT, false, XENT_STAGE>::read(lds + (n & 1) * S::STAGE, at.wm, i, s, lane);
     };
     auto read_b = [&](int n, int s, int j) __attribute__((always_inline)) {
-        b[s][j] = Fragments<S::TN, BT, true>::read(lds + (n & 1) * S::STAGE + S::A, at.wn, j, s, lane);
+        b[s][j] = Fragments<S::TN, BT, true, XENT_STAGE>::read(lds + (n & 1) * S::STAGE + S::A, at.wn, j, s, lane);
     };
     // One step's products, row tile by row tile.  Behind each the next step's fragments of that number are read, those of the rows
     // into the registers just used, and those of the columns, which the next step needs first, behind the first ones.  The first step of a stage reads the second one's.  The second step reads the next stage's:
@@ -309,6 +308,120 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product g, End e
         for (; n + 2 < total; ++n) stage(One{}, One{}, n);
         if (n + 1 < total) stage(One{}, Zero{}, n++);
         stage(Zero{}, Zero{}, n);
+    }
+    __syncthreads();
+    end.template run<S, AT>(acc, at, lds);
+}
+
+// Rows of three bf16 pieces, all of whole stages: a stage holds 32 elements of all pieces, so that six products are formed of what is read once.
+// While a stage's products are formed, the next one's fragments come from LDS, the one after that is under way, and the third begins
+// to come into the place that this one's fragments have left: one meeting a stage.
+template <typename S, bool AT, bool BT, typename End>
+__global__ __launch_bounds__(S::THREADS, 2) void pieces_kernel(Product g, End end)
+{
+    extern __shared__ __align__(16) uint8_t lds[];
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Place at = place_of<S>(g, w);
+    float4v acc[S::MT][S::NT];
+#pragma unroll
+    for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+        for (int j = 0; j < S::NT; ++j) acc[i][j] = float4v{0, 0, 0, 0};
+    constexpr int K = 32;
+    Copies<S::TM, S::WAVES, AT, false, K> ca;
+    Copies<S::TN, S::WAVES, BT, true, K> cb;
+    ca.begin(g.a, at.m0, w, lane);
+    cb.begin(g.b, at.n0, w, lane);
+    const Run run = run_of(g, at.split);
+    constexpr int COPIES = 3 * (ca.N + cb.N), READS = 3 * (S::MT + S::NT);
+    // of the next copy
+    const uint8_t *from_a[3], *from_b[3];
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+        from_a[p] = ca.from(g.a, p, run.first);
+        from_b[p] = cb.from(g.b, p, run.first);
+    }
+    auto copy = [&](uint32_t place, int c) __attribute__((always_inline)) {
+        const uint32_t to = lds0 + place;
+        if (c < 3 * ca.N) ca.copy(g.a, from_a[c / ca.N], K, to + c / ca.N * S::A3, w, lane, c % ca.N);
+        else c -= 3 * ca.N, cb.copy(g.b, from_b[c / cb.N], K, to + 3 * S::A3 + c / cb.N * S::B3, w, lane, c % cb.N);
+    };
+    auto copied = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+            from_a[p] += ca.step;
+            from_b[p] += cb.step;
+        }
+    };
+    half8 a[2][3][S::MT], b[2][3][S::NT];
+    auto read = [&](uint32_t place, int turn, int k) __attribute__((always_inline)) {
+        const uint8_t *const from = lds + place;
+        if (k < 3 * S::MT) {
+            const int p = k / S::MT, i = k % S::MT;
+            a[turn][p][i] = Fragments<S::TM, AT, false, K>::read(from + p * S::A3, at.wm, i, 0, lane);
+        } else {
+            const int p = (k - 3 * S::MT) / S::NT, j = (k - 3 * S::MT) % S::NT;
+            b[turn][p][j] = Fragments<S::TN, BT, true, K>::read(from + 3 * S::A3 + p * S::B3, at.wn, j, 0, lane);
+        }
+    };
+    using Zero = std::integral_constant<int, 0>;
+    using One = std::integral_constant<int, 1>;
+    uint32_t place = 0;  // of this stage
+    int left = run.stages;
+    auto stage = [&](auto turn, auto full) __attribute__((always_inline)) {
+        constexpr int now = decltype(turn)::value;
+        const bool copies = decltype(full)::value || left > 3;
+        if (decltype(full)::value || left > 2) wait_loads<COPIES>();
+        else wait_loads<0>();
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+        const uint32_t next = place == 2 * S::STAGE3 ? 0 : place + S::STAGE3;
+        // (the small products first)
+        constexpr int PA[6] = {2, 1, 0, 1, 0, 0}, PB[6] = {0, 1, 2, 0, 1, 0};
+#pragma unroll
+        for (int s = 0; s < 6; ++s) {
+#pragma unroll
+            for (int i = 0; i < S::MT; ++i) {
+                const int part = s * S::MT + i;
+                constexpr int PARTS = 6 * S::MT;
+#pragma unroll
+                for (int k = part * READS / PARTS; k < (part + 1) * READS / PARTS; ++k) read(next, 1 - now, k);
+                if (copies) {
+#pragma unroll
+                    for (int c = part * COPIES / PARTS; c < (part + 1) * COPIES / PARTS; ++c) copy(place, c);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int j = 0; j < S::NT; ++j) acc[i][j] = mma<__bf16>(b[now][PB[s]][j], a[now][PA[s]][i], acc[i][j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        copied();
+        place = next;
+        --left;
+    };
+    if (left > 0) {
+        for (int n = 0; n < 3 && n < left; ++n) {
+#pragma unroll
+            for (int c = 0; c < COPIES; ++c) copy(n * S::STAGE3, c);
+            copied();
+        }
+        if (left > 2) wait_loads<2 * COPIES>();
+        else wait_loads<0>();
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < READS; ++k) read(0, 0, k);
+        while (left > 4) {
+            stage(Zero{}, One{});
+            stage(One{}, One{});
+        }
+        while (left > 1) {
+            stage(Zero{}, Zero{});
+            stage(One{}, Zero{});
+        }
+        if (left) stage(Zero{}, Zero{});
     }
     __syncthreads();
     end.template run<S, AT>(acc, at, lds);
@@ -835,6 +948,7 @@ struct XentPlan {
 using Large = Shape<8, 4, 2, 4>;   // 256 x 256, eight waves
 using Middle = Shape<4, 4, 2, 2>;  // 128 x 128
 using Small = Shape<2, 2, 2, 2>;   // 64 x 64
+using Middle3 = Shape<4, 2, 2, 4>; // 128 x 128 of three pieces: eight waves, as there is room for one workgroup
 constexpr int XENT_TILE = 64;      // columns that a sum's part stands for at least
 
 constexpr int FEW_GROUPS = 256;    // workgroups of few rows' logits: one a compute unit
@@ -847,18 +961,24 @@ static bool rows_direct(ftk_dtype dtype, const void *p, int64_t ld, int D)
     return dtype != FTK_F32 && (uintptr_t)p % 16 == 0 && ld % 8 == 0 && D % 8 == 0 && ld < XENT_MAX_LD;
 }
 
+// Elements of k of a stage: three pieces come together.
+constexpr int stage_of(int planes) { return planes == 3 ? 32 : XENT_STAGE; }
+
 // How a product of rows x cols over so many stages of k is cut: the shape of the tiles, and shares of the stages where there are few.
 // In microseconds: a stage of a tile of 256, 128 or 64 takes 1.85, 0.65 or 0.5 with a compute unit for itself, 1.1 and 0.85 where
 // two and four share one, and begin and end take some more; joining shares is a launch and moves them once.
-static XentPlan::Cut cut_of(int64_t rows, int64_t cols, int64_t stages, bool shares)
+static XentPlan::Cut cut_of(int planes, int64_t rows, int64_t cols, int64_t k, bool shares)
 {
     static const struct {
-        int tile, at_once;
+        int planes, tile, at_once;
         double ends, alone, shared;
-    } shapes[] = {{256, 1, 7, 1.85, 1.85}, {128, 2, 5, 0.65, 0.55}, {64, 4, 4, 0.5, 0.21}};
+    } shapes[] = {{1, 256, 1, 7, 1.85, 1.85}, {1, 128, 2, 5, 0.65, 0.55}, {1, 64, 4, 4, 0.5, 0.21}, 
+                  {3, 128, 1, 4.5, 1.1, 1.1}, {3, 64, 2, 4, 0.6, 0.43}};
+    const int64_t stages = ceil_div(k, stage_of(planes));
     XentPlan::Cut best{64, 1};
     double least = 1e300;
     for (const auto &s : shapes) {
+        if (s.planes != planes) continue;
         const int64_t tiles = ceil_div(rows, s.tile) * ceil_div(cols, s.tile);
         for (int splits = 1; splits <= (shares ? 64 : 1) && splits * 4 - 3 <= stages; ++splits) {
             if (splits > 1 && tiles * splits > 256 * s.at_once) break;
@@ -902,10 +1022,10 @@ static XentPlan plan_xent(ftk_dtype dtype, int64_t N, int64_t V, int D, bool gra
         at += align_up(bytes, 256);
         return a;
     };
-    const int64_t segments = p.planes == 3 ? 6 : 1, classes = p.width < V ? p.width : V;
-    p.logits = cut_of(grad ? p.rows : N, classes, p.Dp / XENT_STAGE * segments, false);
-    p.rows_grad = cut_of(p.rows, D, ceil_div(classes, XENT_STAGE) * segments, true);
-    p.classes_grad = cut_of(classes, D, p.rows / XENT_STAGE * segments, true);
+    const int64_t classes = p.width < V ? p.width : V;
+    p.logits = cut_of(p.planes, grad ? p.rows : N, classes, p.Dp, false);
+    p.rows_grad = cut_of(p.planes, p.rows, D, classes, true);
+    p.classes_grad = cut_of(p.planes, classes, D, p.rows, true);
     if (p.few) {
         p.tiles = ceil_div(V, 16) < FEW_GROUPS ? ceil_div(V, 16) : FEW_GROUPS;
         p.parts = take((size_t)N * p.tiles * 8);
@@ -934,7 +1054,7 @@ static XentPlan plan_xent(ftk_dtype dtype, int64_t N, int64_t V, int D, bool gra
     return p;
 }
 
-template <typename S, typename H, bool AT, bool BT, typename End>
+template <typename S, typename H, int PLANES, bool AT, bool BT, typename End>
 static ftk_status launch_shape(Product g, const End &end, hipStream_t st)
 {
     const int64_t mt = ceil_div(g.a.outer, S::TM), nt = ceil_div(g.b.outer, S::TN), work = mt * nt * g.splits;
@@ -944,27 +1064,33 @@ static ftk_status launch_shape(Product g, const End &end, hipStream_t st)
     }
     g.mt = (uint32_t)mt;
     g.nt = (uint32_t)nt;
-    FTK_TRY(allow_lds<S::LDS>((const void *)product_kernel<S, H, AT, BT, End>));
-    product_kernel<S, H, AT, BT, End><<<(unsigned)work, S::THREADS, S::LDS, st>>>(g, end);
+    if constexpr (PLANES == 3) {
+        FTK_TRY(allow_lds<S::LDS3>((const void *)pieces_kernel<S, AT, BT, End>));
+        pieces_kernel<S, AT, BT, End><<<(unsigned)work, S::THREADS, S::LDS3, st>>>(g, end);
+    } else {
+        FTK_TRY(allow_lds<S::LDS>((const void *)product_kernel<S, H, AT, BT, End>));
+        product_kernel<S, H, AT, BT, End><<<(unsigned)work, S::THREADS, S::LDS, st>>>(g, end);
+    }
     FTK_TRY_HIP(hipGetLastError());
     return FTK_OK;
 }
 
-template <typename H, bool AT, bool BT, typename End>
+template <typename H, int PLANES, bool AT, bool BT, typename End>
 static ftk_status launch_product(const Product &g, int tile, const End &end, hipStream_t st)
 {
-    if (tile == 256) return launch_shape<Large, H, AT, BT>(g, end, st);
-    if (tile == 128) return launch_shape<Middle, H, AT, BT>(g, end, st);
-    return launch_shape<Small, H, AT, BT>(g, end, st);
+    if constexpr (PLANES == 1)
+        if (tile == 256) return launch_shape<Large, H, PLANES, AT, BT>(g, end, st);
+    if (tile == 128) return launch_shape<std::conditional_t<PLANES == 3, Middle3, Middle>, H, PLANES, AT, BT>(g, end, st);
+    return launch_shape<Small, H, PLANES, AT, BT>(g, end, st);
 }
 
 // A gradient's product, in shares where it is cut into them.
-template <typename H, bool AT, typename T>
+template <typename H, int PLANES, bool AT, typename T>
 static ftk_status launch_gradient(Product g, const XentPlan::Cut &cut, const StoreEnd<T> &end, float *shares, hipStream_t st)
 {
     g.splits = cut.splits;
-    if (cut.splits == 1) return launch_product<H, AT, true>(g, cut.tile, end, st);
-    FTK_TRY((launch_product<H, AT, true>(g, cut.tile, PartEnd{shares, end.rows, end.cols}, st)));
+    if (cut.splits == 1) return launch_product<H, PLANES, AT, true>(g, cut.tile, end, st);
+    FTK_TRY((launch_product<H, PLANES, AT, true>(g, cut.tile, PartEnd{shares, end.rows, end.cols}, st)));
     const int64_t groups = ceil_div(end.rows * end.cols, 256);
     if (groups == 0) return FTK_OK;
     join_kernel<T><<<(unsigned)(groups < 2048 ? groups : 2048), 256, 0, st>>>(shares, cut.splits, end);
@@ -1007,9 +1133,10 @@ struct XentCall {
             across = Operand{w, ldw, 0, D, n};
         } else {
             uint16_t *w = (uint16_t *)(ws + p.W);
-            job = PackJob{(const T *)W + first * ldw, ldw, n, n, D, p.Dp, nullptr, 0, w, 0};
-            along = Operand{w, p.Dp, n * p.Dp, n, p.Dp};
-            across = Operand{w, p.Dp, n * p.Dp, p.Dp, n};
+            const int64_t rows = ceil_div(n, XENT_STAGE) * XENT_STAGE;
+            job = PackJob{(const T *)W + first * ldw, ldw, n, rows, D, p.Dp, nullptr, 0, w, 0};
+            along = Operand{w, p.Dp, rows * p.Dp, n, p.Dp};
+            across = Operand{w, p.Dp, rows * p.Dp, p.Dp, rows};
         }
         return launch_pack<T, H, PLANES>(rows, job, zero, st);
     }
@@ -1063,8 +1190,7 @@ static ftk_status xent_forward(const XentCall &c, float *loss, float *lse)
     // (rows of whole stages are read where they lie: what an ignored one holds stays in its own sums, which are not looked at)
     const bool direct = PLANES == 1 && p.direct && c.D % XENT_STAGE == 0 && rows_direct(FTK_BF16, c.X, c.ldx, c.D);
     g.a = direct ? Operand{(const uint16_t *)c.X, c.ldx, 0, c.N, c.D} : Operand{x, p.Dp, p.rows * p.Dp, c.N, p.Dp};
-    g.stages = p.Dp / XENT_STAGE;
-    g.segments = PLANES == 3 ? 6 : 1;
+    g.stages = p.Dp / stage_of(PLANES);
     g.splits = 1;
     const int tile = p.logits.tile;
     float2 *running = p.width < c.V ? (float2 *)(c.ws + p.running) : nullptr;
@@ -1073,7 +1199,7 @@ static ftk_status xent_forward(const XentCall &c, float *loss, float *lse)
         Operand across;
         FTK_TRY((c.classes<T, H, PLANES>(first, n, first == 0 && !direct ? c.rows_job() : PackJob{}, nullptr, g.b, across)));
         const SumEnd end{Logits{c.bias, c.labels, c.N, first, first + n, c.V, c.scale}, parts, ceil_div(n, tile), label_logit};
-        FTK_TRY((launch_product<H, false, false>(g, tile, end, c.st)));
+        FTK_TRY((launch_product<H, PLANES, false, false>(g, tile, end, c.st)));
         FTK_TRY(launch_loss(c, end, running, first == 0, first + n == c.V, loss, lse));
     }
     return FTK_OK;
@@ -1087,7 +1213,7 @@ static ftk_status xent_backward(const XentCall &c, const float *lse, const float
     uint16_t *x = (uint16_t *)(c.ws + p.X), *d = (uint16_t *)(c.ws + p.d);
     uint32_t *top = std::is_same<T, _Float16>::value ? (uint32_t *)(c.ws + p.top) : nullptr;
     float *parts = (float *)(c.ws + p.dbias), *shares = (float *)(c.ws + p.shares);
-    const int segments = PLANES == 3 ? 6 : 1;
+    constexpr int K = stage_of(PLANES);
     for (int64_t first = 0; first < c.V; first += p.width) {
         const int64_t n = c.V - first < p.width ? c.V - first : p.width, np = ceil_div(n, XENT_STAGE) * XENT_STAGE;
         const int64_t plane = p.rows * p.width;
@@ -1098,28 +1224,28 @@ static ftk_status xent_backward(const XentCall &c, const float *lse, const float
             dloss_top_kernel<<<(unsigned)(groups < 256 ? groups : 256), 256, 0, c.st>>>(dloss, c.labels, c.N, c.V, top);
             FTK_TRY_HIP(hipGetLastError());
         }
-        Product g{Operand{x, p.Dp, p.rows * p.Dp, p.rows, p.Dp}, along, 0, 0, p.Dp / XENT_STAGE, segments, 1};
+        Product g{Operand{x, p.Dp, p.rows * p.Dp, p.rows, p.Dp}, along, 0, 0, p.Dp / K, 1};
         const int tile = p.logits.tile;
         const GradEnd<H, PLANES> grad{Logits{c.bias, c.labels, c.N, first, first + n, c.V, c.scale}, lse, dloss, top, d, p.width, plane,
                                       p.rows, dbias ? parts : nullptr};
-        FTK_TRY((launch_product<H, false, false>(g, tile, grad, c.st)));
+        FTK_TRY((launch_product<H, PLANES, false, false>(g, tile, grad, c.st)));
         if (dbias) {
             dbias_kernel<<<(unsigned)ceil_div(n, 64), 1024, 0, c.st>>>(parts, p.width, (int)ceil_div(p.rows, tile), n, dbias + first);
             FTK_TRY_HIP(hipGetLastError());
         }
         if (dX) {
-            Product r{Operand{d, p.width, plane, p.rows, np}, across, 0, 0, (int)(np / XENT_STAGE), segments, 1};
+            Product r{Operand{d, p.width, plane, p.rows, np}, across, 0, 0, (int)ceil_div(n, K), 1};
             const bool one = p.width >= c.V;
             // (in 32 bits dX itself holds them)
             float *sums = one ? nullptr : PLANES == 3 ? (float *)dX : (float *)(c.ws + p.sums);
             StoreEnd<T> end{dX, lddx, c.N, c.D, sums, PLANES == 3 ? lddx : c.D, first == 0, first + n == c.V, c.scale, top};
-            FTK_TRY((launch_gradient<H, false>(r, p.rows_grad, end, shares, c.st)));
+            FTK_TRY((launch_gradient<H, PLANES, false>(r, p.rows_grad, end, shares, c.st)));
         }
         if (dW) {
             Product r{Operand{d, p.width, plane, np, p.rows}, Operand{x, p.Dp, p.rows * p.Dp, p.Dp, p.rows}, 0, 0,
-                      (int)(p.rows / XENT_STAGE), segments, 1};
+                      (int)(p.rows / K), 1};
             StoreEnd<T> end{dW + first * lddw, lddw, n, c.D, nullptr, 0, true, true, c.scale, top};
-            FTK_TRY((launch_gradient<H, true>(r, p.classes_grad, end, shares, c.st)));
+            FTK_TRY((launch_gradient<H, PLANES, true>(r, p.classes_grad, end, shares, c.st)));
         }
     }
     return FTK_OK;
