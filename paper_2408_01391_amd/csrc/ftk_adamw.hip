@@ -6,6 +6,8 @@
 // One pass: every byte is read and written once, and memory is the bound.  A workgroup has a run of ADAMW_CHUNK elements of one
 // tensor, a lane eight consecutive ones at a time; the tensors' addresses travel as the kernel's arguments, so that a call
 // needs no table in device memory and nothing waits for one.
+// 50 M bf16 weights with 32-bit states and masters, 30 bytes an element: three launches (as many tensors as the arguments hold) of together
+// 272 to 312 us, 4.8 to 5.5 TB/s; 134 M with 8-bit states, 10 bytes: 288 to 302 us, 4.5 to 4.7 TB/s; a copy reaches 5.0.
 //
 // 8-bit states (ftkmeans.h has the format): the lanes that have a block of 32 exchange its largest magnitude.
 #include <math.h>
@@ -40,6 +42,7 @@ template <int BITS, bool MASTER>
 struct AdamwArgs : AdamwList<4 + (BITS == 8 ? 2 : 0) + MASTER>, AdamwRates {};
 static_assert(sizeof(AdamwArgs<8, true>) <= 4096 && sizeof(AdamwArgs<32, false>) <= 4096, "a kernel's arguments hold 4 KB");
 
+// (the key of a tensor at a step: SplitMix64)
 constexpr uint64_t GOLDEN = 0x9E3779B97F4A7C15ull;
 __device__ __forceinline__ uint64_t mix64(uint64_t z)
 {

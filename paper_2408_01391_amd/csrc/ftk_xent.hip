@@ -40,7 +40,7 @@ struct Operand {
 struct Product {
     Operand a, b;  // the result's rows and columns
     uint32_t mt, nt;  // tiles
-    int stages;  // of a segment
+    int stages;  // of k
     int splits;  // workgroups that share a tile's stages out between them
 };
 
@@ -207,6 +207,13 @@ __device__ __forceinline__ Run run_of(const Product &g, int split)
     return Run{first, (int)((uint64_t)g.stages * (split + 1) / (uint32_t)g.splits) - first};
 }
 
+// 16-bit rows.  Stages of 64 elements of k, two in LDS, copied there without passing through registers.  Tiles of 256 x 256 by
+// eight waves need 128 KB of LDS, of which 2 x 64 KB pass for 8.4 MF: matrix instructions are the bound, with what a tile's
+// begin and end take (10 and 5 of 47 us at 32 stages), when none are issued.  8192 rows x 65536 classes x 2048, bf16: the sums 1775 us, 1.24 PF; d
+// and its store in 16 bits 1957; rows' gradient 1719, classes' 1736, 1.27 PF.  The instruction alone, fed from registers, reaches
+// 1.95 PF on such numbers, a library's product of that size 1.40 to 1.48.  Slower: five stages of 32 in a ring (by 20 %), workgroups that
+// go on to further tiles (26 %), four waves of 128 x 128 (45 %), tiles of 128 x 128 (30 %), the 32 x 32 x 16 instruction (its own
+// rate is 10 % less).
 template <typename S, typename H, bool AT, bool BT, typename End>
 __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product g, End end)
 {
@@ -248,9 +255,10 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product g, End e
         b[s][j] = Fragments<S::TN, BT, true, XENT_STAGE>::read(lds + (n & 1) * S::STAGE + S::A, at.wn, j, s, lane);
     };
     // One step's products, row tile by row tile.  Behind each the next step's fragments of that number are read, those of the rows
-    // into the registers just used, and those of the columns, which the next step needs first, behind the first ones.  The first step of a stage reads the second one's.  The second step reads the next stage's:
-    // after its first row tiles all waves meet, when what the first step read has long come, this stage's place is free for
-    // the one after the next, and the next one has arrived.
+    // into the registers just used, and those of the columns, which the next step needs first, behind the first ones.  The
+    // first step of a stage reads the second one's.  The second step reads the next stage's: after its first row tiles all waves
+    // meet, when what the first step read has long come, this stage's place is free for the one after the next, and the
+    // next one has arrived.
     constexpr int MEET = S::MT / 8;
     auto step = [&](auto which, auto reads, auto copies, int n) __attribute__((always_inline)) {
         constexpr int s = decltype(which)::value, next = 1 - s, FROM = s ? MEET : 0;
@@ -315,7 +323,10 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product g, End e
 
 // Rows of three bf16 pieces, all of whole stages: a stage holds 32 elements of all pieces, so that six products are formed of what is read once.
 // While a stage's products are formed, the next one's fragments come from LDS, the one after that is under way, and the third begins
-// to come into the place that this one's fragments have left: one meeting a stage.
+// to come into the place that this one's fragments have left: one meeting a stage.  777 rows x 10007 classes x 333: the sums 54 us, d 63, the
+// rows' and the classes' gradient 37 each (31 GF each by six products, 0.84 PF); matrix instructions are busy for 60 % of that, the rest is begin,
+// end and a last round of tiles that does not fill the card.  (One piece's product after the other reads LDS twice as often: 63, 70,
+// 56 and 69 us.)
 template <typename S, bool AT, bool BT, typename End>
 __global__ __launch_bounds__(S::THREADS, 2) void pieces_kernel(Product g, End end)
 {
@@ -518,7 +529,8 @@ struct SumEnd {
 // Few rows (up to 16 MT): what takes time is reading W once.  A workgroup's eight waves share D out between them, RUN steps of 32
 // each, whose part of the rows stays in registers; W goes from memory straight to registers, 16 / RUN / MT column tiles of 16 classes
 // at a time, the next ones requested before these are used.  The waves' sums meet in LDS, where the first waves, one
-// for a tile, take the softmax on.  (16 rows, 65536 classes of 2048 bf16, 268 MB: TODO us.)
+// for a tile, take the softmax on.  (16 rows, 65536 classes of 2048 bf16, 268 MB: 51 us, 5.2 TB/s; two
+// launches' time is the rest of the call's 54.)
 template <typename H, int MT, int RUN>
 __global__ __launch_bounds__(512, 2) void xent_few_kernel(const H *__restrict__ X, int64_t ldx, const H *__restrict__ W, int64_t ldw, int D,
                                                           SumEnd end)
@@ -946,9 +958,8 @@ struct XentPlan {
 };
 
 using Large = Shape<8, 4, 2, 4>;   // 256 x 256, eight waves
-using Middle = Shape<4, 4, 2, 2>;  // 128 x 128
+using Middle = Shape<4, 2, 2, 4>;  // 128 x 128, eight waves (four of 64 x 64: 2 to 4 % more)
 using Small = Shape<2, 2, 2, 2>;   // 64 x 64
-using Middle3 = Shape<4, 2, 2, 4>; // 128 x 128 of three pieces: eight waves, as there is room for one workgroup
 constexpr int XENT_TILE = 64;      // columns that a sum's part stands for at least
 
 constexpr int FEW_GROUPS = 256;    // workgroups of few rows' logits: one a compute unit
@@ -1080,7 +1091,7 @@ static ftk_status launch_product(const Product &g, int tile, const End &end, hip
 {
     if constexpr (PLANES == 1)
         if (tile == 256) return launch_shape<Large, H, PLANES, AT, BT>(g, end, st);
-    if (tile == 128) return launch_shape<std::conditional_t<PLANES == 3, Middle3, Middle>, H, PLANES, AT, BT>(g, end, st);
+    if (tile == 128) return launch_shape<Middle, H, PLANES, AT, BT>(g, end, st);
     return launch_shape<Small, H, PLANES, AT, BT>(g, end, st);
 }
 
