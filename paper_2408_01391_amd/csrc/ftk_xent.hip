@@ -758,23 +758,31 @@ struct GradEnd {
     }
 };
 
-// 64 classes a workgroup, a sixteenth of the row tiles a wave.
-__global__ __launch_bounds__(1024) void dbias_kernel(const float *__restrict__ parts, int64_t ld, int tiles, int64_t n, float *out)
-{
-    __shared__ double sums[16][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t v = (int64_t)blockIdx.x * 64 + lane;
-    double s = 0;
-    if (v < n) {
+// The bias' gradient from the sums of all row tiles: 16 classes a workgroup, a sixteenth of the tiles 16 lanes.
+struct BiasJob {
+    const float *parts;  // [tiles][ld]
+    int64_t ld;
+    int tiles;
+    int64_t n;
+    float *out;
+    __device__ __forceinline__ void run(uint32_t group) const
+    {
+        __shared__ double sums[16][16];
+        const int lane = threadIdx.x & 15, share = threadIdx.x >> 4;
+        const int64_t v = (int64_t)group * 16 + lane;
+        double s = 0;
+        if (v < n) {
 #pragma unroll 8
-        for (int t = w; t < tiles; t += 16) s += parts[t * ld + v];
+            for (int t = share; t < tiles; t += 16) s += parts[t * ld + v];
+        }
+        sums[share][lane] = s;
+        __syncthreads();
+        if (share || v >= n) return;
+        for (int i = 1; i < 16; ++i) s += sums[i][lane];
+        out[v] = (float)s;
     }
-    sums[w][lane] = s;
-    __syncthreads();
-    if (w || v >= n) return;
-    for (int i = 1; i < 16; ++i) s += sums[i][lane];
-    out[v] = (float)s;
-}
+};
+__global__ __launch_bounds__(256) void dbias_kernel(BiasJob job) { job.run(blockIdx.x); }
 
 // A gradient: the sums times `scale` (and what d was multiplied by taken out), added to those of earlier pieces of the classes.
 template <typename T>
@@ -861,13 +869,14 @@ struct PartEnd {
         StoreEnd<float>{parts + at.split * rows * cols, cols, rows, cols, nullptr, 0, true, true, 1.f, nullptr}.template run<S, AT>(acc, at, lds);
     }
 };
-// All shares together, and what StoreEnd does.
+// All shares together, and what StoreEnd does; workgroups behind those: the bias' gradient.
 template <typename T>
-__global__ __launch_bounds__(256) void join_kernel(const float *__restrict__ parts, int splits, StoreEnd<T> end)
+__global__ __launch_bounds__(256) void join_kernel(const float *__restrict__ parts, int splits, StoreEnd<T> end, uint32_t groups, BiasJob bias)
 {
+    if (blockIdx.x >= groups) return bias.run(blockIdx.x - groups);
     const int64_t all = end.rows * end.cols;
     const float f = end.scale / factor_of(end.top);
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)groups * 256) {
         float s = 0.f;
 #pragma unroll 4
         for (int k = 0; k < splits; ++k) s += parts[k * all + i];
@@ -1096,17 +1105,19 @@ static ftk_status launch_product(const Product &g, int tile, const End &end, hip
     return launch_shape<Small, H, PLANES, AT, BT>(g, end, st);
 }
 
-// A gradient's product, in shares where it is cut into them.
+// A gradient's product, in shares where it is cut into them; their joining takes the bias' gradient along.
 template <typename H, int PLANES, bool AT, typename T>
-static ftk_status launch_gradient(Product g, const XentPlan::Cut &cut, const StoreEnd<T> &end, float *shares, hipStream_t st)
+static ftk_status launch_gradient(Product g, const XentPlan::Cut &cut, const StoreEnd<T> &end, float *shares, BiasJob &bias, hipStream_t st)
 {
     g.splits = cut.splits;
     if (cut.splits == 1) return launch_product<H, PLANES, AT, true>(g, cut.tile, end, st);
     FTK_TRY((launch_product<H, PLANES, AT, true>(g, cut.tile, PartEnd{shares, end.rows, end.cols}, st)));
     const int64_t groups = ceil_div(end.rows * end.cols, 256);
     if (groups == 0) return FTK_OK;
-    join_kernel<T><<<(unsigned)(groups < 2048 ? groups : 2048), 256, 0, st>>>(shares, cut.splits, end);
+    const uint32_t join = groups < 2048 ? groups : 2048;
+    join_kernel<T><<<join + (unsigned)ceil_div(bias.n, 16), 256, 0, st>>>(shares, cut.splits, end, join, bias);
     FTK_TRY_HIP(hipGetLastError());
+    bias.n = 0;
     return FTK_OK;
 }
 
@@ -1241,23 +1252,24 @@ static ftk_status xent_backward(const XentCall &c, const float *lse, const float
         const GradEnd<H, PLANES> grad{Logits{c.bias, c.labels, c.N, first, first + n, c.V, c.scale}, lse, dloss, top, d, p.width, plane,
                                       p.rows, dbias ? parts : nullptr};
         FTK_TRY((launch_product<H, PLANES, false, false>(g, tile, grad, c.st)));
-        if (dbias) {
-            dbias_kernel<<<(unsigned)ceil_div(n, 64), 1024, 0, c.st>>>(parts, p.width, (int)ceil_div(p.rows, tile), n, dbias + first);
-            FTK_TRY_HIP(hipGetLastError());
-        }
+        BiasJob bias{parts, p.width, (int)ceil_div(p.rows, tile), dbias ? n : 0, dbias ? dbias + first : nullptr};
         if (dX) {
             Product r{Operand{d, p.width, plane, p.rows, np}, across, 0, 0, (int)ceil_div(n, K), 1};
             const bool one = p.width >= c.V;
             // (in 32 bits dX itself holds them)
             float *sums = one ? nullptr : PLANES == 3 ? (float *)dX : (float *)(c.ws + p.sums);
             StoreEnd<T> end{dX, lddx, c.N, c.D, sums, PLANES == 3 ? lddx : c.D, first == 0, first + n == c.V, c.scale, top};
-            FTK_TRY((launch_gradient<H, PLANES, false>(r, p.rows_grad, end, shares, c.st)));
+            FTK_TRY((launch_gradient<H, PLANES, false>(r, p.rows_grad, end, shares, bias, c.st)));
         }
         if (dW) {
             Product r{Operand{d, p.width, plane, np, p.rows}, Operand{x, p.Dp, p.rows * p.Dp, p.Dp, p.rows}, 0, 0,
                       (int)(p.rows / K), 1};
             StoreEnd<T> end{dW + first * lddw, lddw, n, c.D, nullptr, 0, true, true, c.scale, top};
-            FTK_TRY((launch_gradient<H, PLANES, true>(r, p.classes_grad, end, shares, c.st)));
+            FTK_TRY((launch_gradient<H, PLANES, true>(r, p.classes_grad, end, shares, bias, c.st)));
+        }
+        if (bias.n) {
+            dbias_kernel<<<(unsigned)ceil_div(bias.n, 16), 256, 0, c.st>>>(bias);
+            FTK_TRY_HIP(hipGetLastError());
         }
     }
     return FTK_OK;
