@@ -106,6 +106,13 @@ def test_pieces_of_the_classes(N, V, D, dtype):
     check(*problem(N, V, D, dtype, bias=True))
 
 
+@pytest.mark.parametrize("N,V,D,dtype", [(777, 10007, 333, "f32"), (777, 10007, 333, "bf16"), (9001, 1000, 250, "f16"), (9001, 1000, 250, "f32"),
+                                         (65, 40001, 130, "f32"), (33, 30000, 136, "f16"), (20000, 3, 129, "f32"), (20000, 3, 129, "bf16")])
+def test_products_in_shares(N, V, D, dtype):
+    """Few tiles and long sums, which several workgroups share: shares of unequal length, tiles that are no multiple of the XCDs."""
+    check(*problem(N, V, D, dtype, bias=True))
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("N", [90, 10])
 @pytest.mark.parametrize("D,ldx,ldw,shift", [(64, 80, 72, 8), (64, 64, 67, 0), (33, 40, 50, 1), (40, 41, 40, 3), (1, 3, 5, 1),
