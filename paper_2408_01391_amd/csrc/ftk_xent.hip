@@ -694,13 +694,12 @@ struct GradEnd {
 #pragma unroll
         for (int i = 0; i < S::MT; ++i) {
             const int64_t n = at.m0 + at.wm + line_of<AT>(i, r);
-            const bool in = n < z.N;
-            const int32_t label = in ? z.labels[n] : -1;
-            const bool live = label >= 0 && label < z.V;
-            // (an ignored row's, and that of a row without any finite logit: all probabilities are 0)
-            const float l = live ? lse[n] : -__builtin_inff(), shift = l == -__builtin_inff() ? __builtin_inff() : l;
-            const float g = live ? dloss[n] * factor : 0.f;
-            const int rel = z.label_from(label, v0);
+            const int32_t label = n < z.N ? z.labels[n] : -1;
+            const float l = label >= 0 && label < z.V ? lse[n] : -__builtin_inff();
+            // (an ignored row, and one whose logits are all -infinity, has no gradient, at its label neither)
+            const bool live = l != -__builtin_inff();
+            const float shift = live ? l : __builtin_inff(), g = live ? dloss[n] * factor : 0.f;
+            const int rel = z.label_from(live ? label : -1, v0);
 #pragma unroll
             for (int j = 0; j < S::NT; ++j)
 #pragma unroll

@@ -321,3 +321,16 @@ def test_masks_of_the_lowest_value(N, V, D, dtype):
     loss, lse = ftk.xent(X, W, labels, bias=torch.full_like(b, torch.finfo(torch.float32).min))
     live = (labels >= 0) & (labels < V)
     assert (lse[live] == torch.finfo(torch.float32).min).all() and (loss == 0).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,V,D", [(1, 9, 8), (60, 200, 64), (300, 900, 72), (12000, 14000, 16)])
+def test_rows_without_open_classes_have_no_gradient(N, V, D, dtype):
+    """All logits -infinity: lse says so, and gradients are zeros, at the labels too; over one and several pieces of the classes."""
+    X, W, labels, _, dloss = problem(N, V, D, dtype)
+    bias = torch.full((V,), -INF, device=DEV)
+    _, lse = ftk.xent(X, W, labels, bias=bias)
+    live = (labels >= 0) & (labels < V)
+    assert (lse[live] == -INF).all()
+    for grad in ftk.xent_grad(X, W, labels, lse, dloss, bias=bias, need=(True, True, True)):
+        assert (grad == 0).all()
