@@ -243,7 +243,7 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v)
 }
 
 struct AdamwStep {
-    float b1, b1c, b2, b2c, rate, vc, eps, keep, gs;
+    float b1, b1c, b2, b2c, rate, vc, eps, decay, gs;
     bool scaled;
     uint32_t key;
 };
@@ -295,7 +295,9 @@ __device__ __forceinline__ void adamw_some(const AdamwIn<P, G, BITS, MASTER, E> 
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         const float root = __builtin_amdgcn_sqrtf(v[e] * a.vc) + a.eps;
-        p.v[e] = fmaf(a.keep, (float)in.p.v[e], -(a.rate * m[e]) * __builtin_amdgcn_rcpf(root));
+        // (the decay joins the update before the weight: 1 - lr decay would be rounded to a multiple of 2^-24, for all weights alike)
+        const float w = (float)in.p.v[e];
+        p.v[e] = w - fmaf(a.decay, w, a.rate * m[e] * __builtin_amdgcn_rcpf(root));
         // (the 16-bit weight is the master rounded; an instruction that adds and rounds to 16 bits at once would take the unrounded sum)
         if constexpr (MASTER) asm("" : "+v"(p.v[e]));
     }
@@ -370,7 +372,7 @@ __global__ __launch_bounds__(ADAMW_THREADS) void adamw_kernel(const AdamwArgs<BI
     const int64_t step = max((int64_t)1, *a.step);
     const float c1 = -expm1f((float)step * a.log_b1), c2 = -expm1f((float)step * a.log_b2);
     const float lr = a.lr_scale ? a.lr * *a.lr_scale : a.lr;
-    AdamwStep s{a.b1, a.b1c, a.b2, a.b2c, lr / c1, 1.f / c2, a.eps, 1.f - lr * a.decay, a.grad_scale ? *a.grad_scale : 1.f, a.grad_scale != nullptr, 0};
+    AdamwStep s{a.b1, a.b1c, a.b2, a.b2c, lr / c1, 1.f / c2, a.eps, lr * a.decay, a.grad_scale ? *a.grad_scale : 1.f, a.grad_scale != nullptr, 0};
     if constexpr (BITS == 8)
         s.key = (uint32_t)mix64(mix64(mix64(a.seed + GOLDEN * (uint64_t)step) + (uint64_t)a.place[which]) + (uint64_t)(from >> 32));
     if (from + ADAMW_CHUNK <= count) {

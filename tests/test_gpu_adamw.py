@@ -333,3 +333,28 @@ def test_weights_that_moved():
     with pytest.raises(ValueError):
         ftk.adamw_step(state, [torch.ones_like(old)], step)
     assert (old == 1).all() and (p == 1).all()
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("by_scale", [True, False])
+@pytest.mark.parametrize("decay", [1e-7, 3e-8, 1e-8])
+def test_small_decay(decay, by_scale, bits):
+    """A decay of about half a step of the weights' numbers and less, as at the end of a schedule: beside updates of all sizes, which
+    spread the rounding evenly, it is kept on average, and every weight is off by that one rounding alone."""
+    n = 1 << 20
+    g = torch.Generator(device=DEV).manual_seed(12)
+    p, grad = 1 + torch.rand(n, generator=g, device=DEV), torch.randn(n, generator=g, device=DEV)
+    old, gr = numpy(p), numpy(grad)
+    scale = torch.full((1,), 2.0 ** -10, device=DEV) if by_scale else None
+    rate = 1.024 if by_scale else 1e-3
+    ftk.adamw_step(ftk.AdamW([p], bits), [grad], torch.ones(1, dtype=torch.int64, device=DEV), lr=rate, lr_scale=scale, eps=0.5,
+                   weight_decay=decay / 1e-3)
+    _, _, w, change = one_step(old, gr, 0 * old, 0 * old, 1, lr=1e-3, eps=0.5, weight_decay=decay / 1e-3)
+    off = numpy(p) - w
+    # half a step of the result: 2^-24 in [1, 2), 2^-23 from 2 on, where a weight of less may arrive; a dozen roundings of the change
+    half = np.spacing(w.astype(np.float32)).astype(np.float64) / 2
+    assert (abs(off) <= 1.001 * half + 40 * 2.0 ** -24 * change).all()
+    # a rounding's standard deviation is a step over the root of 12; what the change's roundings have in common (40 at the most) meets
+    # updates of either sign, whose mean is below five of its deviations
+    limit = 5 * (2.0 ** -23 / 12 ** 0.5 + 40 * 2.0 ** -24 * 1e-3) / n ** 0.5 + 40 * 2.0 ** -24 * 2 * decay
+    assert abs(off.mean()) <= limit
