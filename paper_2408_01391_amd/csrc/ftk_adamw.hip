@@ -309,15 +309,15 @@ __device__ __forceinline__ void adamw_some(const AdamwIn<P, G, BITS, MASTER, E> 
         store_some((P *)t[FIELD_PARAM] + i, o, n);
     }
     if constexpr (BITS == 8) {
-        // (elements behind the last one are zeros; v has no sign but a NaN's)
+        // (elements behind the last one are zeros; v has no sign, but a NaN may)
         uint32_t mt = 0, vt = 0;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             mt = max(mt, mag_bits(m[e]));
-            vt = max(vt, __float_as_uint(v[e]));
+            vt = max(vt, mag_bits(v[e]));
         }
         uint32_t mtop, vtop;
-        const uint32_t ms = scale_of<3>(block_max<E>(mt), mtop), vs = min(scale_of<4>(block_max<E>(vt), vtop), 255u);
+        const uint32_t ms = scale_of<3>(block_max<E>(mt), mtop), vs = scale_of<4>(block_max<E>(vt), vtop);
         const float mu = M3::encode(ms), vu = M4::encode(vs);
         const bool wide = __any(ms >= M3::LIMIT || vs >= M4::LIMIT);
         Some<uint32_t, E / 4> mo, vo;

@@ -358,3 +358,23 @@ def test_small_decay(decay, by_scale, bits):
     # updates of either sign, whose mean is below five of its deviations
     limit = 5 * (2.0 ** -23 / 12 ** 0.5 + 40 * 2.0 ** -24 * 1e-3) / n ** 0.5 + 40 * 2.0 ** -24 * 2 * decay
     assert abs(off.mean()) <= limit
+
+
+@pytest.mark.parametrize("grads", [F, B, H])
+@pytest.mark.parametrize("pattern", [0xFFFFFFFF, 0xFFF80001, 0xFFC00000, 0x7FFFFFFF])
+def test_every_nan_marks_its_block(pattern, grads):
+    """Gradients that are NaN of either sign and any payload, all bits set as in memory that nobody wrote among them."""
+    bits = np.full(1, pattern if grads == F else pattern >> 16, dtype=np.uint32 if grads == F else np.uint16)
+    if grads == H:
+        bits |= 0x7C00  # (fp16's exponent)
+    bad = torch.from_numpy(bits.view(np.int32 if grads == F else np.int16)).to(DEV).view(grads)
+    assert bool(bad.isnan())
+    g = torch.full((96,), 0.1, device=DEV).to(grads)
+    g[40] = bad[0]
+    p = torch.ones(96, device=DEV)
+    state = ftk.AdamW([p], 8)
+    ftk.adamw_step(state, [g], torch.ones(1, dtype=torch.int64, device=DEV))
+    assert state.m_scales[0].tolist()[1] == 255 and state.v_scales[0].tolist()[1] == 255
+    for values in ftk.adamw_moments(state):
+        assert values[0].view(3, 32).isnan().all(1).tolist() == [False, True, False] and int(values[0].isnan().sum()) == 32
+    assert int(p.isnan().sum()) == 1
