@@ -18,6 +18,9 @@
 namespace ftk {
 
 constexpr int ADAMW_THREADS = 256, ADAMW_STEP = 8 * ADAMW_THREADS, ADAMW_CHUNK = 4 * ADAMW_STEP;
+// The square root's and the reciprocal's instructions take what lies below the normal numbers for 0, roots below 1.1e-19 that is: of no
+// weight beside an eps of this size or more, 1.1e-19 / 2e-12 being a step of 32 bits.  Below it both go the longer, exact way.
+constexpr float ADAMW_EPS = 2e-12f;
 constexpr int64_t ADAMW_MAX = 1LL << 37;  // elements of a tensor: a launch's chunks are 32-bit numbers
 
 // The tensors of a launch: as many as a kernel's arguments of 4 KB hold addresses of.
@@ -294,10 +297,12 @@ __device__ __forceinline__ void adamw_some(const AdamwIn<P, G, BITS, MASTER, E> 
     Some<float, E> p;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        const float root = __builtin_amdgcn_sqrtf(v[e] * a.vc) + a.eps;
+        float ratio;
+        if (a.eps < ADAMW_EPS) ratio = m[e] / (sqrtf(v[e]) * sqrtf(a.vc) + a.eps);
+        else ratio = m[e] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[e] * a.vc) + a.eps);
         // (the decay joins the update before the weight: 1 - lr decay would be rounded to a multiple of 2^-24, for all weights alike)
         const float w = (float)in.p.v[e];
-        p.v[e] = w - fmaf(a.decay, w, a.rate * m[e] * __builtin_amdgcn_rcpf(root));
+        p.v[e] = w - fmaf(a.decay, w, a.rate * ratio);
         // (the 16-bit weight is the master rounded; an instruction that adds and rounds to 16 bits at once would take the unrounded sum)
         if constexpr (MASTER) asm("" : "+v"(p.v[e]));
     }

@@ -378,3 +378,23 @@ def test_every_nan_marks_its_block(pattern, grads):
     for values in ftk.adamw_moments(state):
         assert values[0].view(3, 32).isnan().all(1).tolist() == [False, True, False] and int(values[0].isnan().sum()) == 32
     assert int(p.isnan().sum()) == 1
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("eps", [0.0, 1e-39, 1e-30, 1e-20, 1.9e-12, 2.1e-12, 1e-8])
+def test_small_gradients_and_small_eps(eps, bits):
+    """Second moments below the normal numbers, beside an eps that is smaller still: the update is the formula's."""
+    rng = np.random.default_rng(3)
+    # (a block of each magnitude, as 8-bit states share their scale)
+    g = np.repeat(10.0 ** np.array([0, -5, -10, -15, -18, -18.7, -19, -19.5, -20, -20.5]), 32) * rng.uniform(0.5, 1, 320)
+    g = (g * rng.choice([-1, 1], 320)).astype(np.float32)
+    if eps:
+        g[::7] = 0
+    p = torch.full((320,), 0.25, device=DEV)
+    ftk.adamw_step(ftk.AdamW([p], bits), [torch.from_numpy(g).to(DEV)], torch.ones(1, dtype=torch.int64, device=DEV), lr=0.5, eps=eps,
+                   weight_decay=0.0)
+    float_eps = float(np.float32(eps))
+    _, _, w, change = one_step(np.full(320, 0.25), g, np.zeros(320), np.zeros(320), 1, lr=0.5, eps=float_eps, weight_decay=0.0)
+    assert np.isfinite(w).all()
+    # a dozen roundings of the change, two of the weight
+    assert (abs(numpy(p) - w) <= 40 * 2.0 ** -24 * change + 2 * 2.0 ** -24 * abs(w)).all()
