@@ -483,7 +483,9 @@ ftk_status ftk_xent(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N, cons
 
 /* Gradients of sum(dloss * loss), d_nv = dloss_n (exp(z_nv - lse_n) - [v = label_n]), zero for ignored rows:
  *   dX = scale * d W [N x D], dW = scale * d^T X [V x D] (type of the rows), dbias_v = sum_n d_nv [V]; each may be NULL.
- * lse as ftk_xent left it; exp(z - lse) is off by half a step of lse, of no weight but for logits that are all beyond 10^5 or so.
+ * lse as ftk_xent left it; exp(z - lse) is off by half a step of lse, 2^-8 at most.  From |lse| = 2^17 on, where that would be more (masks of
+ * the type's lowest value on all classes), the row's probabilities are divided by their own sum, which takes another pass over W for
+ * every 64 rows that have such a one among them.
  * d is rounded to the rows' type (FTK_F32: not at all) before the products; every gradient is written
  * once, in whole, and must not overlap an input. */
 ftk_status ftk_xent_grad(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N, const void *W, int64_t ldw, int64_t V, int32_t D,

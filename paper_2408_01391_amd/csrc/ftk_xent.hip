@@ -668,11 +668,18 @@ __device__ __forceinline__ float factor_of(const uint32_t *top)
     return *top == 0 || e == 255 ? 1.f : __uint_as_float((uint32_t)min(254, max(1, 268 - e)) << 23);
 }
 
+// What a row's part of d takes: d_v = weight (exp(z_v - shift) - [v = label] sum).  shift is lse and sum 1, where that is exact enough
+// (terms_kernel); a row that is ignored, or all of whose logits are -infinity, has no weight and no label.
+struct __align__(16) RowTerms {
+    float shift, sum, weight;
+    int32_t label;
+};
+
 // d of a tile, in 16 bits (or three bf16 pieces), zero in rows and columns that only fill up; sums over the tile's rows.
 template <typename H, int PLANES>
 struct GradEnd {
     Logits z;
-    const float *lse, *dloss;
+    const RowTerms *terms;  // [rows]
     const uint32_t *top;
     uint16_t *d;        // [rows][ld]
     int64_t ld, plane, rows;
@@ -694,12 +701,9 @@ struct GradEnd {
 #pragma unroll
         for (int i = 0; i < S::MT; ++i) {
             const int64_t n = at.m0 + at.wm + line_of<AT>(i, r);
-            const int32_t label = n < z.N ? z.labels[n] : -1;
-            const float l = label >= 0 && label < z.V ? lse[n] : -__builtin_inff();
-            // (an ignored row, and one whose logits are all -infinity, has no gradient, at its label neither)
-            const bool live = l != -__builtin_inff();
-            const float shift = live ? l : __builtin_inff(), g = live ? dloss[n] * factor : 0.f;
-            const int rel = z.label_from(live ? label : -1, v0);
+            const RowTerms row = n < rows ? terms[n] : RowTerms{__builtin_inff(), 0.f, 0.f, -1};
+            const float shift = row.shift, g = row.weight * factor;
+            const int rel = z.label_from(row.label, v0);
 #pragma unroll
             for (int j = 0; j < S::NT; ++j)
 #pragma unroll
@@ -710,7 +714,7 @@ struct GradEnd {
                 for (int j = 0; j < S::NT; ++j)
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
-                        if (rel == 32 * (j >> 1) + 4 * (j & 1) + c) acc[i][j][c] -= 1.f;
+                        if (rel == 32 * (j >> 1) + 4 * (j & 1) + c) acc[i][j][c] -= row.sum;
             }
 #pragma unroll
             for (int j = 0; j < S::NT; ++j)
@@ -892,6 +896,22 @@ __global__ __launch_bounds__(256) void join_kernel(const float *__restrict__ par
     }
 }
 
+// Eight elements in 16 bits, or in pieces of which each takes what the ones before have left.
+template <typename H, typename T, int PLANES>
+__device__ __forceinline__ void pieces_of(const T (&v)[8], half8 (&o)[PLANES])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        float x = (float)v[e];
+#pragma unroll
+        for (int k = 0; k < PLANES; ++k) {
+            const H h = (H)x;
+            o[k][e] = __builtin_bit_cast(uint16_t, h);
+            x -= (float)h;
+        }
+    }
+}
+
 // Rows to whole lines of 64 elements (three bf16 pieces where PLANES is 3), zeros beyond the row and in rows that are not looked at:
 // those whose label lies outside [0, V), and those from N on.
 struct PackJob {
@@ -905,9 +925,9 @@ struct PackJob {
 };
 // One array, or two in one launch: the second one's workgroups behind the first's.
 template <typename T, typename H, int PLANES>
-__global__ __launch_bounds__(256) void pack_kernel(PackJob first, PackJob second, uint32_t *zero)
+__global__ __launch_bounds__(256) void pack_kernel(PackJob first, PackJob second, uint32_t *zero, uint32_t zeros)
 {
-    if (zero && blockIdx.x == 0 && threadIdx.x == 0) *zero = 0;
+    for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < zeros; i += gridDim.x * 256) zero[i] = 0;
     const bool other = blockIdx.x >= first.groups;
     const PackJob j = other ? second : first;
     const int pieces = j.Dp / 8;
@@ -925,28 +945,158 @@ __global__ __launch_bounds__(256) void pack_kernel(PackJob first, PackJob second
             for (int e = 0; e < 8; ++e) v[e] = (T)0.f;
         }
         half8 o[PLANES];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            float x = (float)v[e];
-#pragma unroll
-            for (int k = 0; k < PLANES; ++k) {
-                const H h = (H)x;
-                o[k][e] = __builtin_bit_cast(uint16_t, h);
-                x -= (float)h;
-            }
-        }
+        pieces_of<H>(v, o);
 #pragma unroll
         for (int k = 0; k < PLANES; ++k) *reinterpret_cast<half8 *>(j.out + k * j.rows * j.Dp + n * j.Dp + d) = o[k];
     }
 }
 
-__global__ __launch_bounds__(256) void dloss_top_kernel(const float *dloss, const int32_t *labels, int64_t N, int64_t V, uint32_t *top)
+// The terms of 64 rows, and the largest |dloss| where it is asked for.
+// exp(z - lse) is off by half a step of lse, 2^-8 at most below XENT_FAR.  Beyond it the logarithm of the sum is lost in lse little
+// by little (masks of the type's lowest value on all classes: every class would have probability 1), and the
+// rows of a group that has such a one are gone through anew: the logits of all classes in the products' order, with the same roundings, and
+// from them the largest one and the sum of exponentials below it.  W is read as it lies, in full for every 64 rows; where those are few, in
+// shares of the classes, whose last workgroup to end joins them, in order.  Other groups end at once (30000 rows: 4.6 us, a launch).
+// All classes masked: 8192 rows x 65536 classes x 2048 in bf16 take 23.5 ms instead of 5.5, 30000 x 1024 x 256 in fp16 285 us instead of 121.
+constexpr float XENT_FAR = 131072.f;
+constexpr int TERMS_ROWS = 64, TERMS_WAVES = 8;
+template <typename T>
+struct TermsArgs {
+    Logits z;  // of all classes
+    const float *lse, *dloss;
+    const uint16_t *X;  // packed
+    int64_t plane;
+    int Dp, D;
+    const T *W;
+    int64_t ldw;
+    RowTerms *terms;
+    uint32_t *top;  // NULL: not asked for
+    int groups, shares;
+    int64_t each;      // classes of a share
+    uint64_t *parts;   // [groups][shares][64], and how many of a group have ended
+    uint32_t *tickets;
+};
+template <typename T, typename H, int PLANES>
+__global__ __launch_bounds__(64 * TERMS_WAVES, 2) void terms_kernel(TermsArgs<T> a)
 {
-    uint32_t m = 0;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < N; i += (int64_t)gridDim.x * 256)
-        if (labels[i] >= 0 && labels[i] < V) m = max(m, mag_bits(dloss[i]));
-    for (int d = 32; d; d >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d, 64));
-    if ((threadIdx.x & 63) == 0 && m) atomicMax(top, m);
+    constexpr int MT = TERMS_ROWS / 16, WAVES = TERMS_WAVES;
+    __shared__ float2 part[WAVES][TERMS_ROWS];
+    __shared__ uint32_t largest[WAVES];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
+    const int group = blockIdx.x % (uint32_t)a.groups, share = blockIdx.x / (uint32_t)a.groups;
+    const int64_t n0 = (int64_t)group * TERMS_ROWS, n = n0 + threadIdx.x;
+    auto terms_of = [&](int64_t at) __attribute__((always_inline)) {
+        const int32_t label = at < a.z.N ? a.z.labels[at] : -1;
+        const float l = label >= 0 && label < a.z.V ? a.lse[at] : -__builtin_inff();
+        return l != -__builtin_inff() ? RowTerms{l, 1.f, a.dloss[at], label} : RowTerms{__builtin_inff(), 0.f, 0.f, -1};
+    };
+    // (every eighth workgroup takes its followers' largest along: exchanges on one word go one after the other)
+    const bool tops = a.top && share == 0 && group % WAVES == 0;
+    RowTerms own{};
+    if (w == 0 || tops) own = terms_of(n);
+    if (tops) {
+        uint32_t m = mag_bits(own.weight);
+        for (int d = 32; d; d >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d, 64));
+        if (lane == 0) largest[w] = m;
+    }
+    const int far = w == 0 && fabsf(own.shift) >= XENT_FAR && fabsf(own.shift) < __builtin_inff();
+    const int any = __syncthreads_or(far);
+    if (tops && threadIdx.x == 0) {
+        uint32_t m = largest[0];
+        for (int k = 1; k < WAVES; ++k) m = max(m, largest[k]);
+        if (m) atomicMax(a.top, m);
+    }
+    if (!any) {
+        if (w == 0 && share == 0) a.terms[n] = own;
+        return;
+    }
+    float2 sum[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) sum[i] = float2{-__builtin_inff(), 0.f};
+    const int64_t end = min((share + 1) * a.each, a.z.V);
+    for (int64_t v0 = share * a.each + 16 * w; v0 < end; v0 += 16 * WAVES) {
+        const T *const row = a.W + min(v0 + r, a.z.V - 1) * a.ldw;
+        float4v acc[MT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) acc[i] = float4v{0, 0, 0, 0};
+        auto step = [&](int k, const T (&v)[8]) __attribute__((always_inline)) {
+            half8 b[PLANES], x[PLANES][MT];
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+                    x[p][i] = *reinterpret_cast<const half8 *>(a.X + p * a.plane + (n0 + 16 * i + r) * a.Dp + k);
+            pieces_of<H>(v, b);
+            // (the order of pieces_kernel)
+            constexpr int PRODUCTS = PLANES == 3 ? 6 : 1, PA[6] = {2, 1, 0, 1, 0, 0}, PB[6] = {0, 1, 2, 0, 1, 0};
+#pragma unroll
+            for (int s = 0; s < PRODUCTS; ++s)
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+                    acc[i] = PLANES == 3 ? mma<H>(b[PB[s] % PLANES], x[PA[s] % PLANES][i], acc[i]) : mma<H>(b[0], x[0][i], acc[i]);
+        };
+        int k = 8 * q;
+#pragma unroll 4
+        for (; k < (a.D & ~31); k += 32) {
+            T v[8];
+#pragma unroll
+            for (int c = 0; c < 8 / PIECE<T>; ++c) {
+                const PieceOf<T> piece = row_piece(row + k + c * PIECE<T>);
+#pragma unroll
+                for (int e = 0; e < PIECE<T>; ++e) v[c * PIECE<T> + e] = piece[e];
+            }
+            step(k, v);
+        }
+        if (a.D & 31) {
+            T v[8];
+            load8(row, k, a.D, v);
+            step(k, v);
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            float top = sum[i].x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                acc[i][e] = fmaf(a.z.scale, acc[i][e], a.z.bias_of(v0 + 4 * q + e));
+                top = fmaxf(top, acc[i][e]);
+            }
+            const float shift = top > -__builtin_inff() ? top : 0.f;
+            float t = sum[i].y * exp2_of(sum[i].x - shift);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t += exp2_of(acc[i][e] - shift);
+            sum[i] = float2{top, t};
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+#pragma unroll
+        for (int d = 16; d < 64; d *= 2)
+            sum[i] = SumEnd::joined(sum[i], float2{__shfl_xor(sum[i].x, d, 64), __shfl_xor(sum[i].y, d, 64)});
+        if (q == 0) part[w][16 * i + r] = sum[i];
+    }
+    __syncthreads();
+    if (w) return;
+    float2 p = part[0][lane];
+#pragma unroll
+    for (int k = 1; k < WAVES; ++k) p = SumEnd::joined(p, part[k][lane]);
+    if (a.shares > 1) {
+        uint64_t *const parts = a.parts + (int64_t)group * a.shares * TERMS_ROWS + lane;
+        __hip_atomic_store(&parts[share * TERMS_ROWS], __builtin_bit_cast(uint64_t, p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+        uint32_t ended = 0;
+        if (lane == 0) ended = __hip_atomic_fetch_add(&a.tickets[group], 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+        if (__builtin_amdgcn_readfirstlane(ended) != (uint32_t)a.shares - 1) return;
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+        p = float2{-__builtin_inff(), 0.f};
+        for (int k = 0; k < a.shares; ++k)
+            p = SumEnd::joined(p, __builtin_bit_cast(float2, __hip_atomic_load(&parts[k * TERMS_ROWS], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)));
+    }
+    if (far) {
+        own.shift = p.x;
+        own.sum = p.y;
+        own.weight /= p.y;
+    }
+    a.terms[n] = own;
 }
 
 // ---- calls -----------------------------------------------------------------------------------
@@ -963,7 +1113,8 @@ struct XentPlan {
     struct Cut {
         int tile, splits;
     } logits, rows_grad, classes_grad;
-    size_t X, W, parts, running, label_logit, d, sums, shares, dbias, top, total;
+    size_t X, W, parts, running, label_logit, d, sums, shares, dbias, terms, parts_far, top, total;
+    int shares_far;   // of the classes, where logits are gone through anew for a group of rows
 };
 
 using Large = Shape<8, 4, 2, 4>;   // 256 x 256, eight waves
@@ -1055,7 +1206,8 @@ static XentPlan plan_xent(ftk_dtype dtype, int64_t N, int64_t V, int D, bool gra
     }
     p.X = take((size_t)p.planes * p.rows * p.Dp * 2);
     p.W = direct ? at : take((size_t)p.planes * p.width * p.Dp * 2);
-    p.parts = p.running = p.label_logit = p.d = p.sums = p.shares = p.dbias = p.top = at;
+    p.parts = p.running = p.label_logit = p.d = p.sums = p.shares = p.dbias = p.terms = p.parts_far = p.top = at;
+    p.shares_far = 1;
     if (grad) {
         p.d = take((size_t)p.planes * p.rows * p.width * 2);
         p.sums = dtype == FTK_F32 ? at : take((size_t)N * D * 4);
@@ -1063,7 +1215,12 @@ static XentPlan plan_xent(ftk_dtype dtype, int64_t N, int64_t V, int D, bool gra
         const size_t cs = p.classes_grad.splits > 1 ? (size_t)p.classes_grad.splits * classes * D * 4 : 0;
         p.shares = take(rs > cs ? rs : cs);
         p.dbias = take((size_t)ceil_div(p.rows, XENT_TILE) * p.width * 4);
-        p.top = take(256);
+        p.terms = take((size_t)p.rows * sizeof(RowTerms));
+        // (two workgroups a compute unit, each wave four tiles of classes at least)
+        const int64_t groups = p.rows / TERMS_ROWS, wanted = groups < 512 ? 512 / groups : 1, most = ceil_div(V, 64 * TERMS_WAVES);
+        p.shares_far = (int)(wanted < most ? wanted : most);
+        p.parts_far = take(p.shares_far > 1 ? (size_t)p.rows * p.shares_far * 8 : 0);
+        p.top = take((size_t)(1 + groups) * 4);  // and the groups' tickets
     } else {
         p.tiles = ceil_div(classes, p.logits.tile);
         p.parts = take((size_t)N * p.tiles * 8);
@@ -1121,14 +1278,14 @@ static ftk_status launch_gradient(Product g, const XentPlan::Cut &cut, const Sto
 }
 
 template <typename T, typename H, int PLANES>
-static ftk_status launch_pack(PackJob first, PackJob second, uint32_t *zero, hipStream_t st)
+static ftk_status launch_pack(PackJob first, PackJob second, uint32_t *zero, uint32_t zeros, hipStream_t st)
 {
     for (PackJob *j : {&first, &second}) {
         const int64_t groups = ceil_div(j->rows * (j->Dp / 8), 256);
         j->groups = (uint32_t)(groups < 4096 ? groups : 4096);
     }
     if (first.groups + second.groups == 0) return FTK_OK;
-    pack_kernel<T, H, PLANES><<<first.groups + second.groups, 256, 0, st>>>(first, second, zero);
+    pack_kernel<T, H, PLANES><<<first.groups + second.groups, 256, 0, st>>>(first, second, zero, zeros);
     FTK_TRY_HIP(hipGetLastError());
     return FTK_OK;
 }
@@ -1146,7 +1303,7 @@ struct XentCall {
     PackJob rows_job() const { return PackJob{X, ldx, N, p.rows, D, p.Dp, labels, V, (uint16_t *)(ws + p.X), 0}; }
     // One piece's rows of W: packed, in one launch with `rows` (the first piece: those of X), or where they lie.
     template <typename T, typename H, int PLANES>
-    ftk_status classes(int64_t first, int64_t n, const PackJob &rows, uint32_t *zero, Operand &along, Operand &across) const
+    ftk_status classes(int64_t first, int64_t n, const PackJob &rows, uint32_t *zero, uint32_t zeros, Operand &along, Operand &across) const
     {
         PackJob job{};
         if (p.direct) {
@@ -1160,7 +1317,7 @@ struct XentCall {
             along = Operand{w, p.Dp, rows * p.Dp, n, p.Dp};
             across = Operand{w, p.Dp, rows * p.Dp, p.Dp, rows};
         }
-        return launch_pack<T, H, PLANES>(rows, job, zero, st);
+        return launch_pack<T, H, PLANES>(rows, job, zero, zeros, st);
     }
 };
 
@@ -1219,7 +1376,7 @@ static ftk_status xent_forward(const XentCall &c, float *loss, float *lse)
     for (int64_t first = 0; first < c.V; first += p.width) {
         const int64_t n = c.V - first < p.width ? c.V - first : p.width;
         Operand across;
-        FTK_TRY((c.classes<T, H, PLANES>(first, n, first == 0 && !direct ? c.rows_job() : PackJob{}, nullptr, g.b, across)));
+        FTK_TRY((c.classes<T, H, PLANES>(first, n, first == 0 && !direct ? c.rows_job() : PackJob{}, nullptr, 0, g.b, across)));
         const SumEnd end{Logits{c.bias, c.labels, c.N, first, first + n, c.V, c.scale}, parts, ceil_div(n, tile), label_logit};
         FTK_TRY((launch_product<H, PLANES, false, false>(g, tile, end, c.st)));
         FTK_TRY(launch_loss(c, end, running, first == 0, first + n == c.V, loss, lse));
@@ -1233,23 +1390,28 @@ static ftk_status xent_backward(const XentCall &c, const float *lse, const float
 {
     const XentPlan &p = c.p;
     uint16_t *x = (uint16_t *)(c.ws + p.X), *d = (uint16_t *)(c.ws + p.d);
-    uint32_t *top = std::is_same<T, _Float16>::value ? (uint32_t *)(c.ws + p.top) : nullptr;
+    uint32_t *zeros = (uint32_t *)(c.ws + p.top), *top = std::is_same<T, _Float16>::value ? zeros : nullptr;
+    const int groups = (int)(p.rows / TERMS_ROWS);
     float *parts = (float *)(c.ws + p.dbias), *shares = (float *)(c.ws + p.shares);
+    RowTerms *terms = (RowTerms *)(c.ws + p.terms);
     constexpr int K = stage_of(PLANES);
     for (int64_t first = 0; first < c.V; first += p.width) {
         const int64_t n = c.V - first < p.width ? c.V - first : p.width, np = ceil_div(n, XENT_STAGE) * XENT_STAGE;
         const int64_t plane = p.rows * p.width;
         Operand along, across;
-        FTK_TRY((c.classes<T, H, PLANES>(first, n, first == 0 ? c.rows_job() : PackJob{}, first == 0 ? top : nullptr, along, across)));
-        if (top && first == 0) {
-            const int64_t groups = ceil_div(c.N > 0 ? c.N : 1, 1024);
-            dloss_top_kernel<<<(unsigned)(groups < 256 ? groups : 256), 256, 0, c.st>>>(dloss, c.labels, c.N, c.V, top);
+        FTK_TRY((c.classes<T, H, PLANES>(first, n, first == 0 ? c.rows_job() : PackJob{}, zeros, first == 0 ? 1 + groups : 0, along,
+                                         across)));
+        if (first == 0) {
+            const int64_t each = ceil_div(ceil_div(c.V, p.shares_far), 16 * TERMS_WAVES) * (16 * TERMS_WAVES);
+            const TermsArgs<T> args{Logits{c.bias, c.labels, c.N, 0, c.V, c.V, c.scale}, lse, dloss, x, p.rows * p.Dp, p.Dp, c.D, (const T *)c.W, c.ldw,
+                                    terms, top, groups, p.shares_far, each, (uint64_t *)(c.ws + p.parts_far), zeros + 1};
+            terms_kernel<T, H, PLANES><<<(unsigned)(groups * p.shares_far), 64 * TERMS_WAVES, 0, c.st>>>(args);
             FTK_TRY_HIP(hipGetLastError());
         }
         Product g{Operand{x, p.Dp, p.rows * p.Dp, p.rows, p.Dp}, along, 0, 0, p.Dp / K, 1};
         const int tile = p.logits.tile;
-        const GradEnd<H, PLANES> grad{Logits{c.bias, c.labels, c.N, first, first + n, c.V, c.scale}, lse, dloss, top, d, p.width, plane,
-                                      p.rows, dbias ? parts : nullptr};
+        const GradEnd<H, PLANES> grad{Logits{c.bias, c.labels, c.N, first, first + n, c.V, c.scale}, terms, top, d, p.width, plane, p.rows,
+                                      dbias ? parts : nullptr};
         FTK_TRY((launch_product<H, PLANES, false, false>(g, tile, grad, c.st)));
         BiasJob bias{parts, p.width, (int)ceil_div(p.rows, tile), dbias ? n : 0, dbias ? dbias + first : nullptr};
         if (dX) {

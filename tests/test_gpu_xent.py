@@ -334,3 +334,78 @@ def test_rows_without_open_classes_have_no_gradient(N, V, D, dtype):
     assert (lse[live] == -INF).all()
     for grad in ftk.xent_grad(X, W, labels, lse, dloss, bias=bias, need=(True, True, True)):
         assert (grad == 0).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("low", [torch.finfo(torch.float32).min, -1e9])
+@pytest.mark.parametrize("N,V,D", [(1, 9, 8), (16, 513, 41), (70, 333, 64), (300, 900, 72), (130, 5000, 256), (2500, 4000, 256), (12000, 14000, 16)])
+def test_gradient_of_classes_that_are_all_masked(N, V, D, low, dtype):
+    """A bias so low that 32-bit logits are all alike, the logarithm of their number lost in lse: each class has probability 1 / V."""
+    X, W, labels, _, dloss = problem(N, V, D, dtype)
+    bias = torch.full((V,), low, device=DEV)
+    _, lse = ftk.xent(X, W, labels, bias=bias)
+    grads = ftk.xent_grad(X, W, labels, lse, dloss, bias=bias, need=(True, True, True))
+    live = (labels >= 0) & (labels < V)
+    g = torch.where(live, dloss.double(), 0).unsqueeze(1)
+    d = (g / V).expand(N, V).clone()
+    d.scatter_add_(1, torch.where(live, labels, 0).long().unsqueeze(1), -g)
+    x, w, half, one = X.double(), W.double(), HALF[X.dtype], 2.0 ** -24
+    # the sum of V equal terms and the division by it; d's rounding (fp16: a half step of 2^-38 of the largest dloss at least); the sums
+    for mine, want, size, n, scaled in ((grads[0], d @ w, d.abs() @ w.abs(), V, w), (grads[1], d.t() @ x, d.abs().t() @ x.abs(), N, x),
+                                        (grads[2], d.sum(0), d.abs().sum(0), N, None)):
+        rounding = 0 if scaled is None else 2.0 ** -22 if X.dtype == torch.float32 else half
+        n = n * (6 if X.dtype == torch.float32 else 1) + 8
+        tiny = 2.0 ** -25 + float(g.abs().max()) * 2.0 ** -38 * n * float(scaled.abs().max()) if X.dtype == torch.float16 and scaled is not None else 0
+        last = one if scaled is None else half
+        assert ((mine.double() - want).abs() <= (rounding + (V + n + 8) * one) * size + 1.01 * last * want.abs() + tiny + 1e-37).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [64, 41])
+def test_gradient_of_rows_with_far_logits(D, dtype):
+    """Rows whose logits all lie at 3 * 10^5, steps of 2^-5 apart, among others: their probabilities add up to 1, which exp(z - lse)
+    do not; the other rows' gradients are what they are without them, bit for bit."""
+    N, V = 200, 333
+    X, W, labels, _, dloss = problem(N, V, D, dtype)
+    far = [3, 64, 70, 199]
+    labels = torch.where(labels < 0, 5, labels.clamp(max=V - 1))
+    W[:, 0], X[:, 0], X[far, 0] = 8, 0, 4e4
+    dloss[far] = 1e-4
+    _, lse = ftk.xent(X, W, labels)
+    assert ((lse.abs() > 3e5).nonzero().flatten().cpu() == torch.tensor(far)).all()
+    for n in far:
+        alone = torch.zeros_like(dloss)
+        alone[n] = 1.0
+        db = ftk.xent_grad(X, W, labels, lse, alone, need=(False, False, True))[2]
+        # V terms' sum there and here
+        assert abs(float(db.double().sum())) <= 2 * (V + 20) * 2.0 ** -24
+        assert (db[torch.arange(V, device=DEV) != labels[n]] >= 0).all() and -1 < float(db[labels[n]]) < 0
+    dX = ftk.xent_grad(X, W, labels, lse, dloss)[0]
+    closed = labels.clone()
+    closed[far] = -1
+    others = ftk.xent_grad(X, W, closed, lse, dloss)[0]
+    rest = torch.ones(N, dtype=torch.bool, device=DEV)
+    rest[far] = False
+    assert torch.equal(dX[rest], others[rest]) and (others[far] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_graph_of_far_logits(dtype):
+    """Shares of the classes that count each other's ends, captured and replayed with eager calls between, in a workspace of any content."""
+    N, V, D = 130, 5000, 72
+    X, W, labels, _, dloss = problem(N, V, D, dtype)
+    bias = torch.full((V,), -1e9, device=DEV)
+    _, lse = ftk.xent(X, W, labels, bias=bias)
+    ws = torch.full((ftk.xent_workspace_bytes(ftk._MX_DTYPES[X.dtype], N, V, D, True) + 512,), 255, dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = ftk.xent_grad(X, W, labels, lse, dloss, bias=bias, workspace=ws)
+    for turn in range(4):
+        if turn == 2:
+            ws.fill_(127)
+        dloss.mul_(-0.5)
+        graph.replay()
+        want = ftk.xent_grad(X, W, labels, lse, dloss, bias=bias)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, want))
