@@ -123,15 +123,28 @@ class LearnedExperts(Experts):
     def forward(self, x, training=False):
         """Returns (out [N, F], what gradients of the weights need)."""
         logits = x @ self.gate.t()
-        gate = ftk.route_gate(logits, self.k)
-        out, saved = self.products(x, gate.labels, gate.weights, training)
+        gate, out, saved = self._routed(x, logits, training)
         return out, (logits, gate, saved)
 
-    def loss(self, x, labels, weights=None):
+    def _routed(self, x, logits, training):
+        gate = ftk.route_gate(logits, self.k)
+        return gate, *self.products(x, gate.labels, gate.weights, training)
+
+    def loss(self, x, labels, weights=None, padding=None):
         """Returns (sum of the rows' losses by their weights float [N], by default 1 / N; gradients of it and the balance loss by
-        gate, experts and classes; the Gate).  Rows with a label outside [0, V) are ignored."""
+        gate, experts and classes; the Gate).  Rows with a label outside [0, V) have no loss; they go to their experts and count in
+        the balance loss as the others do.  Rows marked in `padding` (bool [N]) and those without a loss that hold NaN or infinities are no tokens:
+        nothing of them is looked at, and they do not count."""
         N = x.shape[0]
-        out, (logits, gate, saved) = self.forward(x, training=True)
+        logits = x @ self.gate.t()
+        # (such an element makes all logits of its row likewise)
+        closed = ((labels < 0) | (labels >= self.classes.shape[0])) & ~logits[:, 0].isfinite()
+        if padding is not None:
+            closed = closed | padding
+            labels = labels.masked_fill(padding, -1)
+        logits.masked_fill_(closed.unsqueeze(1), float("-inf"))
+        x = x.masked_fill(closed.unsqueeze(1), 0)  # (0 * NaN would reach the gate's gradient)
+        gate, out, saved = self._routed(x, logits, training=True)
         loss, lse = ftk.xent(out, self.classes, labels, bias=self.bias)
         if weights is None:
             weights = torch.full((N,), 1.0 / max(N, 1), device=x.device)
@@ -140,9 +153,9 @@ class LearnedExperts(Experts):
         dlogits = ftk.route_gate_grad(logits, gate, dgates, self.balance)
         return torch.dot(loss, weights), [dlogits.t() @ x, dexperts, dclasses], gate
 
-    def step(self, x, labels, weights=None):
+    def step(self, x, labels, weights=None, padding=None):
         """One update of all weights; returns (loss, Gate)."""
-        loss, grads, gate = self.loss(x, labels, weights)
+        loss, grads, gate = self.loss(x, labels, weights, padding)
         self.count.add_(1)
         ftk.adamw_step(self.state, grads, self.count, **self.options)
         self.pack(self.experts)

@@ -115,3 +115,48 @@ def test_refusals():
                  lambda: LearnedExperts(z(4, 8), z(4, 6, 8), z(5, 6), k=5)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("marked", [True, False])
+def test_padding_takes_no_part(marked, dtype):
+    """Rows that are no tokens, marked or filled with what nobody wrote: gradients, loss and the gate's counts are those of whatever else
+    they hold, and those of the batch without them."""
+    N, E, V, keep = 128, 6, 50, 90
+    weights = torch.full((N,), 0.01, device=DEV)
+    layer, x, labels = layer_of(np.random.default_rng(5), N, 96, 64, E, V, dtype, balance=0.5)
+    labels[keep:] = -1
+    padding = torch.arange(N, device=DEV) >= keep if marked else None
+    if marked:
+        labels[keep + 3] = 7  # (a label does not make it a token)
+    results = []
+    for fill in (float("nan"), float("inf"), -float("inf")) + ((0.0, 3.0) if marked else ()):
+        x[keep:] = fill
+        results.append(layer.loss(x, labels, weights, padding))
+    results.append(layer.loss(x[:keep].contiguous(), labels[:keep].contiguous(), weights[:keep].contiguous()))
+    loss, grads, gate = results[0]
+    assert loss.isfinite() and all(g.isfinite().all() for g in grads) and int(gate.counts[-1]) == keep
+    assert (gate.labels[keep:] == -1).all() and (gate.weights[keep:] == 0).all()
+    for other, others, that in results[1:-1]:
+        assert torch.equal(loss, other) and torch.equal(gate.counts, that.counts) and all(torch.equal(a, b) for a, b in zip(grads, others))
+    # fewer rows may be added up in another order: 32-bit sums, and in 16 bits a step of the result
+    other, others, that = results[-1]
+    assert torch.equal(gate.counts, that.counts) and abs(float(loss - other)) <= 1e-5 * abs(float(other))
+    for a, b in zip(grads, others):
+        assert (f64(a) - f64(b)).__abs__().max() <= (2e-5 if dtype == torch.float32 else 2.0 ** -7) * np.abs(f64(b)).max()
+
+
+def test_rows_without_a_loss_count_in_the_balance():
+    """Tokens without a class are routed like others; one with a class that holds NaN shows in the balance loss and in the gate."""
+    layer, x, labels = layer_of(np.random.default_rng(6), 64, 96, 64, 6, 50, torch.float32)
+    labels[:] = torch.arange(64, device=DEV, dtype=torch.int32) % 50
+    labels[::2] = -1
+    _, _, gate = layer.loss(x, labels)
+    assert int(gate.counts[-1]) == 64 and (gate.labels >= 0).all()
+    x[1] = float("nan")
+    loss, grads, gate = layer.loss(x, labels)
+    assert gate.loss.isnan().all() and grads[0].isnan().any() and int(gate.counts[-1]) == 64
+    padding = torch.zeros(64, dtype=torch.bool, device=DEV)
+    padding[1] = True
+    loss, _ = layer.step(x, labels, padding=padding)
+    assert loss.isfinite() and all(p.isfinite().all() for p in layer.state.params)
