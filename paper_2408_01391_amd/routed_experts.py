@@ -20,16 +20,21 @@ from . import binding as ftk
 class Experts:
     """out[t] = sum over the slots (t, j) of g[t, j] * W[label[t, j]] x[t] with W [E, F, D] packed to 4 bits, once for either direction."""
 
-    def __init__(self, weights):
+    def __init__(self, weights, transposed=True):
         self.E, self.F, self.D = weights.shape
         self.W = self.WT = None
-        self.pack(weights)
+        self.pack(weights, transposed)
 
-    def pack(self, weights):
-        """Packs the matrices anew, where they were packed before: a captured graph finds them there."""
+    def pack(self, weights, transposed=True):
+        """Packs the matrices anew, where they were packed before: a captured graph finds them there.  transposed: those that the rows'
+        gradient is formed with, too."""
         E, F, D = weights.shape
         self.W = ftk.mx4_quantize(weights.reshape(E * F, D), out=self.W)
-        self.WT = ftk.mx4_quantize(weights.transpose(1, 2).reshape(E * D, F), out=self.WT)
+        if transposed:
+            self.WT = ftk.mx4_quantize(weights.transpose(1, 2).reshape(E * D, F), out=self.WT)
+
+    def _transposed(self):
+        return self.WT
 
     def products(self, x, labels, gates, training=False):
         """Returns (out [N, F], what gradients() needs, or None)."""
@@ -38,14 +43,14 @@ class Experts:
         y = ftk.mx4_linear(x, self.W, route=route, gather=True)
         return ftk.route_combine(y, route, gates), (x, y, route, gates) if training else None
 
-    def gradients(self, dout, saved, out_dtype=torch.float32):
+    def gradients(self, dout, saved, out_dtype=torch.float32, rows=True):
         """Gradients (dx [N, D], dgates [N, k], dweights [E, F, D] of out_dtype) of sum(dout * out) with labels and gates held fixed;
-        rounding to 4 bits counts as the identity."""
+        rounding to 4 bits counts as the identity.  Without `rows` dx is not formed, and None."""
         x, y, route, gates = saved
         dy, dgates = ftk.route_combine_grad(dout, y, route, gates)
-        dx = ftk.route_combine(ftk.mx4_linear(dy, self.WT, route=route), route)
-        rows = ftk.route_gather(x, route)
-        dweights = ftk.mx4_outer(ftk.mx4_quantize(dy, transpose=True), ftk.mx4_quantize(rows, transpose=True), route, out_dtype=out_dtype)
+        dx = ftk.route_combine(ftk.mx4_linear(dy, self._transposed(), route=route), route) if rows else None
+        gathered = ftk.route_gather(x, route)
+        dweights = ftk.mx4_outer(ftk.mx4_quantize(dy, transpose=True), ftk.mx4_quantize(gathered, transpose=True), route, out_dtype=out_dtype)
         return dx, dgates, dweights
 
 
@@ -118,7 +123,13 @@ class LearnedExperts(Experts):
         self.state = ftk.AdamW([gate, experts, classes], bits, master=gate.dtype != torch.float32)
         self.count = torch.zeros(1, dtype=torch.int64, device=gate.device)
         self.balance = torch.full((1,), float(balance), device=gate.device)
-        super().__init__(experts)
+        super().__init__(experts, transposed=False)
+
+    def _transposed(self):
+        """Packed when the rows' gradient is asked for: no step of the layer's own weights needs them."""
+        E, F, D = self.experts.shape
+        self.WT = ftk.mx4_quantize(self.experts.transpose(1, 2).reshape(E * D, F), out=self.WT)
+        return self.WT
 
     def forward(self, x, training=False):
         """Returns (out [N, F], what gradients of the weights need)."""
@@ -130,11 +141,12 @@ class LearnedExperts(Experts):
         gate = ftk.route_gate(logits, self.k)
         return gate, *self.products(x, gate.labels, gate.weights, training)
 
-    def loss(self, x, labels, weights=None, padding=None):
+    def loss(self, x, labels, weights=None, padding=None, rows=False):
         """Returns (sum of the rows' losses by their weights float [N], by default 1 / N; gradients of it and the balance loss by
         gate, experts and classes; the Gate).  Rows with a label outside [0, V) have no loss; they go to their experts and count in
         the balance loss as the others do.  Rows marked in `padding` (bool [N]) and those without a loss that hold NaN or infinities are no tokens:
-        nothing of them is looked at, and they do not count."""
+        nothing of them is looked at, and they do not count.
+        rows: a fourth result, the gradient by x [N, D] through experts and gate, for what made the rows."""
         N = x.shape[0]
         logits = x @ self.gate.t()
         # (such an element makes all logits of its row likewise)
@@ -149,16 +161,17 @@ class LearnedExperts(Experts):
         if weights is None:
             weights = torch.full((N,), 1.0 / max(N, 1), device=x.device)
         dout, dclasses, _ = ftk.xent_grad(out, self.classes, labels, lse, weights, bias=self.bias, need=(True, True, False))
-        _, dgates, dexperts = self.gradients(dout, saved, x.dtype)
+        dx, dgates, dexperts = self.gradients(dout, saved, x.dtype, rows)
         dlogits = ftk.route_gate_grad(logits, gate, dgates, self.balance)
-        return torch.dot(loss, weights), [dlogits.t() @ x, dexperts, dclasses], gate
+        results = torch.dot(loss, weights), [dlogits.t() @ x, dexperts, dclasses], gate
+        return (*results, torch.addmm(dx, dlogits, self.gate)) if rows else results
 
     def step(self, x, labels, weights=None, padding=None):
         """One update of all weights; returns (loss, Gate)."""
         loss, grads, gate = self.loss(x, labels, weights, padding)
         self.count.add_(1)
         ftk.adamw_step(self.state, grads, self.count, **self.options)
-        self.pack(self.experts)
+        self.pack(self.experts, transposed=False)
         return loss, gate
 
 

@@ -160,3 +160,43 @@ def test_rows_without_a_loss_count_in_the_balance():
     padding[1] = True
     loss, _ = layer.step(x, labels, padding=padding)
     assert loss.isfinite() and all(p.isfinite().all() for p in layer.state.params)
+
+
+@pytest.mark.parametrize("N,D,F,E,V,k", [(300, 96, 40, 6, 50, 2), (37, 130, 260, 9, 333, 3), (1, 64, 64, 4, 7, 1)])
+def test_gradient_of_the_rows(N, D, F, E, V, k):
+    """What a net in front of the layer gets: through the experts' matrices and through the gate, after a step, in 32 bits."""
+    rng = np.random.default_rng(N + 1)
+    layer, x, labels = layer_of(rng, N, D, F, E, V, torch.float32, k=k, balance=0.5, lr=1e-2)
+    assert layer.WT is None  # (no step asks for it)
+    layer.step(x, labels)
+    plain = layer.loss(x, labels)
+    loss, grads, gate, dx = layer.loss(x, labels, rows=True)
+    assert torch.equal(loss, plain[0]) and all(torch.equal(a, b) for a, b in zip(grads, plain[1]))
+    out, (logits, _, (_, y, route, _)) = layer.forward(x, training=True)
+    _, lse = ftk.xent(out, layer.classes, labels)
+    dout, _, _ = ftk.xent_grad(out, layer.classes, labels, lse, torch.full((N,), 1.0 / N, device=DEV))
+    dy, dg = ftk.route_combine_grad(dout, y, route, gate.weights)
+    WT = values_of(*pack_of(f64(layer.experts).transpose(0, 2, 1).reshape(E * D, F)), F).reshape(E, D, F)
+    slots, off, order = rounded(f64(dy)), route.offsets.cpu().numpy(), route.order.cpu().numpy()
+    want, size = np.zeros((N, D)), np.zeros((N, D))
+    for e in range(E):
+        for row in range(off[e], off[e + 1]):
+            if order[row] >= 0:
+                want[order[row] // k] += WT[e] @ slots[row]
+                size[order[row] // k] += abs(WT[e]) @ abs(slots[row])
+    dz, dsize = gradient(f64(logits), gate.labels.cpu().numpy(), gate.counts.cpu().numpy(), True, f64(dg), 0.5)
+    want, size = want + dz @ f64(layer.gate), size + dsize @ abs(f64(layer.gate))
+    # sums of F and of E products and of the slots; p within (80 + 12 + E) steps, four times
+    assert (abs(f64(dx) - want) <= (F + E + k + 16 + 4 * (92 + E)) * 2.0 ** -24 * size + 1e-30).all()
+    assert (f64(dx)[labels.cpu().numpy() < 0] != 0).any() or N == 1  # (by the balance)
+    # the inherited call has it, too
+    assert torch.equal(layer.gradients(dout, (x, y, route, gate.weights))[0], ftk.route_combine(ftk.mx4_linear(dy, layer.WT, route=route), route))
+
+
+def test_gradient_of_the_rows_in_16_bits():
+    """In the rows' type; rows that are no tokens get zeros."""
+    layer, x, labels = layer_of(np.random.default_rng(9), 70, 96, 40, 6, 50, torch.bfloat16)
+    x[60:] = float("nan")
+    labels[60:] = -1
+    dx = layer.loss(x, labels, rows=True)[3]
+    assert dx.dtype == x.dtype and dx.shape == x.shape and dx.isfinite().all() and (dx[60:] == 0).all() and (dx[:60] != 0).any(1).all()
