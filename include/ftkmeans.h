@@ -482,7 +482,8 @@ ftk_status ftk_xent(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N, cons
                     void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* Gradients of sum(dloss * loss), d_nv = dloss_n (exp(z_nv - lse_n) - [v = label_n]), zero for ignored rows:
- *   dX = scale * d W [N x D], dW = scale * d^T X [V x D] (type of the rows), dbias_v = sum_n d_nv [V]; each may be NULL.
+ *   dX = scale * d W [N x D], dW = scale * d^T X [V x D] (type of the rows), dbias_v = sum_n d_nv [V]; each may be NULL,
+ *   not all of them unless N = 0.
  * lse as ftk_xent left it; exp(z - lse) is off by half a step of lse, 2^-8 at most.  From |lse| = 2^17 on, where that would be more (masks of
  * the type's lowest value on all classes), the row's probabilities are divided by their own sum, which takes another pass over W for
  * every 64 rows that have such a one among them.

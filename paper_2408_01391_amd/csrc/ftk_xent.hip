@@ -1504,7 +1504,7 @@ ftk_status ftk_xent_grad(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N,
                          void *hip_stream)
 {
     FTK_TRY(check_xent(dtype, X, ldx, N, W, ldw, V, D, bias, scale, labels));
-    if (!dX && !dW && !dbias) {
+    if (N > 0 && !dX && !dW && !dbias) {
         set_error("no gradient is asked for");
         return FTK_EINVAL;
     }
@@ -1516,6 +1516,7 @@ ftk_status ftk_xent_grad(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N,
         FTK_TRY(check_ptr(lse, 4, "lse"));
         FTK_TRY(check_ptr(dloss, 4, "dloss"));
     }
+    if (N == 0 && !dW && !dbias) return FTK_OK;  // (an empty dX may have no address)
     if (dX) FTK_TRY(check_ptr(dX, dtype_size(dtype), "dX"));
     if (dW) FTK_TRY(check_ptr(dW, dtype_size(dtype), "dW"));
     if (dbias) FTK_TRY(check_ptr(dbias, 4, "dbias"));

@@ -409,3 +409,15 @@ def test_graph_of_far_logits(dtype):
         want = ftk.xent_grad(X, W, labels, lse, dloss, bias=bias)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(held, want))
+
+
+def test_no_rows_and_their_gradient_alone():
+    X, W, labels, b, dloss = problem(70, 90, 40, "bf16", bias=True)
+    lse = torch.zeros(0, device=DEV)
+    for bias, need in ((None, (True, False, None)), (b, (True, False, False))):
+        dX, dW, db = ftk.xent_grad(X[:0], W, labels[:0], lse, lse, bias=bias, need=need)
+        assert dX.shape == (0, 40) and dX.dtype == X.dtype and dW is None and db is None
+    out = torch.empty(0, 40, dtype=X.dtype, device=DEV)
+    assert ftk.xent_grad(X[:0], W, labels[:0], lse, lse, dX=out, need=(False, False, False))[0] is out
+    with pytest.raises(ftk.FtkError):  # (refused as with rows)
+        ftk.xent_grad(X[:0], W, labels[:0], lse, lse, scale=INF, need=(True, False, False))

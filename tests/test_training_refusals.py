@@ -99,3 +99,11 @@ def test_tensors_on_the_host():
                  lambda: ftk.AdamW([x], bits=4)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_xent_gradients_without_rows():
+    """Nothing is asked for where there are no rows and no classes' gradients: no refusal, and nothing to enqueue."""
+    L = ftk.load()
+    ok = [ftk.BF16, None, 64, 0, P, 64, 1000, 64, None, 1.0, None, None, None, None, 64, None, 64, None, None, 0, None]
+    assert L.ftk_xent_grad(*ok) == 0
+    each("ftk_xent_grad", ok, ((0, ftk.F64, 1), (3, -1, 1), (4, None, 1), (5, 63, 1), (9, math.inf, 1), (17, P + 2, 2)))
