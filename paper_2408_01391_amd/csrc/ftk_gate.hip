@@ -568,13 +568,15 @@ __global__ __launch_bounds__(64 * GATE_GRAD_WAVES, (NP * PIECE<T> > 16 ? 2 : 4))
             p[i] = exp_of(p[i] - shift);
             p[i] = none ? 0.f : p[i];
         }
-        // where half a step of lse is no longer small: by their own sum (a row of masks of the type's lowest value)
-        if (__any(fabsf(shift) > 64.f)) {
+        // where half a step of lse is no longer small: by their own sum (a row of masks of the type's lowest value).  16-bit gradients round
+        // to 2^-11 of themselves at best, what lse is off by below 64 is 2^-19; in 32 bits it would be what bounds them
+        constexpr float FAR = sizeof(T) == 2 ? 64.f : 1.f;
+        if (__any(fabsf(shift) > FAR)) {
             float all = 0.f;
 #pragma unroll
             for (int i = 0; i < R::V; ++i) all += p[i];
             all = group.sum(all);
-            all = none || !(fabsf(shift) > 64.f) ? 1.f : 1.f / all;
+            all = none || !(fabsf(shift) > FAR) ? 1.f : 1.f / all;
 #pragma unroll
             for (int i = 0; i < R::V; ++i) p[i] *= all;
         }

@@ -319,3 +319,23 @@ def test_masks_of_the_lowest_value(N, E, k, dtype, normalise):
     want, size = gradient(z, labels, counts, normalise, f64(dw), 0.7)
     # as elsewhere; a probability divided by the sum of them (E / 16 additions in a lane at most) is off by its rounding besides
     assert (abs(f64(dz) - want) <= (6 * tol + (E / 16 + 16) * 2.0 ** -24) * size + HALF[t] * abs(want) * 1.01 + 2.0 ** -25).all()
+
+
+@pytest.mark.parametrize("N,E,k,lanes", [(300, 8, 2, 4), (200, 16, 4, 4), (70, 64, 8, 16)])
+def test_gradient_of_32_bit_logits_far_from_zero(N, E, k, lanes):
+    """Logits between 33 and 62, where lse is off by up to 2^-19: the balance loss' gradient of a row adds up to 0 within the roundings of
+    its own sums, which are less."""
+    rng = np.random.default_rng(E)
+    z = (rng.uniform(33, 58, (N, 1)) + rng.uniform(0, 2, (N, E))).astype(np.float32)
+    logits = torch.from_numpy(z).to(DEV)
+    gate = ftk.route_gate(logits, k)
+    p, lse = probabilities(z.astype(np.float64))
+    assert (lse > 33).all() and (lse < 64).all()
+    dloss, counts = float(np.float32(0.3 * N)), gate.counts.cpu().numpy()
+    got = f64(ftk.route_gate_grad(logits, gate, None, torch.full((1,), dloss, device=DEV)))
+    mean = (p * (dloss * E * counts[:-1] / (k * N) / N)).sum(1)
+    # p: four terms of a lane and the lanes' are added, divided and multiplied; <p, c>: as many additions; the difference and the last
+    # product: a half step (2^-24) each of p |c - <p, c>|, whose sum is at most twice <p, c>
+    steps = 2 * (4 + np.log2(lanes)) + 2 + 4 + 1
+    assert steps < 32
+    assert (abs(got.sum(1)) <= steps * 2.0 ** -24 * mean).all()
