@@ -8,6 +8,8 @@ fails, an exception is raised.  The calls compute values: torch records nothing 
 from __future__ import annotations
 
 import ctypes
+import itertools
+import operator
 from pathlib import Path
 
 import torch
@@ -900,7 +902,7 @@ class _AdamwOptions(ctypes.Structure):
 
 class AdamW:
     """Weights and their states for adamw_step: contiguous device tensors of one type (float32, bfloat16 or float16), not overlapping,
-    which stay where they are in memory.
+    which stay where they are in memory, as their states do: new values are copied into them.
 
     bits: 32 (m, v float32) or 8 (m, v uint8 codes and a scale byte for every 32 elements).  States that are not given start at
     zero.  master: float32 copies of 16-bit weights; True makes them from the weights."""
@@ -938,6 +940,9 @@ class AdamW:
                 if need:
                     setattr(row, "param" if name == "params" else name, t.data_ptr())
                     spans.append((t.data_ptr(), t.data_ptr() + need * t.element_size()))
+        # (the memory that the table names, held whatever becomes of the states' tensors)
+        self._states = list(self._all_states())
+        self._memory = [t.detach() for t in self._states]
         self._counts = [p.numel() for p in self.params]
         self._places = [p.data_ptr() for p in self.params]
         for n, row in zip(self._counts, self._table):
@@ -946,6 +951,13 @@ class AdamW:
         spans.sort()
         if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
             raise ValueError("weights or states overlap")
+
+    def _all_states(self):
+        return itertools.chain(self.m, self.v, self.m_scales or (), self.v_scales or (), self.master or ())
+
+    def _check_states(self):
+        if not all(map(operator.is_, self._all_states(), self._states)):
+            raise ValueError("states have been replaced since they were given: new values are copied into them")
 
 
 def _alike(tensors, counts, dtype, device):
@@ -973,6 +985,7 @@ def adamw_step(state, grads, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, we
         raise ValueError("gradients must be contiguous tensors of one type with the weights' elements, on their device")
     if list(map(torch.Tensor.data_ptr, state.params)) != state._places:
         raise ValueError("weights have moved since their state was made")
+    state._check_states()
     state._grads[1::8] = [0 if g is None else g.data_ptr() for g in grads]
     code = _MX_DTYPES.get(dtype)
     if code is None:
@@ -993,6 +1006,7 @@ def adamw_moments(state, out=None, dtype=torch.float32):
         raise ValueError("states in 32 bits are their own values")
     if out is None:
         out = [[torch.empty_like(p, dtype=dtype) for p in state.params] for _ in range(2)]
+    state._check_states()
     dtype, device, lists = out[0][0].dtype, state.params[0].get_device(), []
     for ts in out:
         if not _alike(ts, state._counts, dtype, device):

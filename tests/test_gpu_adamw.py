@@ -398,3 +398,28 @@ def test_small_gradients_and_small_eps(eps, bits):
     assert np.isfinite(w).all()
     # a dozen roundings of the change, two of the weight
     assert (abs(numpy(p) - w) <= 40 * 2.0 ** -24 * change + 2 * 2.0 ** -24 * abs(w)).all()
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_states_that_were_replaced(bits):
+    """Other tensors in the lists of states are refused rather than passed over; memory that a state's tensor gave up is not written
+    to once it is another's."""
+    n, step = 1 << 16, torch.ones(1, dtype=torch.int64, device=DEV)
+    p, g = torch.zeros(n, dtype=B, device=DEV), torch.ones(n, dtype=B, device=DEV)
+    for name in ("m", "v", "master") + (("m_scales", "v_scales") if bits == 8 else ()):
+        state = ftk.AdamW([p], bits, master=True)
+        tensors = getattr(state, name)
+        tensors[0] = tensors[0].clone()
+        with pytest.raises(ValueError):
+            ftk.adamw_step(state, [g], step)
+        if bits == 8:
+            with pytest.raises(ValueError):
+                ftk.adamw_moments(state)
+    assert not p.any()
+    state = ftk.AdamW([p], bits, master=True)
+    for tensors in (state.m, state.v, state.master):
+        tensors[0].data = tensors[0].data.clone()
+    torch.cuda.synchronize()
+    others = [torch.full((n,), 3, dtype=t.dtype, device=DEV) for t in (state.m[0], state.v[0], state.master[0]) for _ in range(3)]
+    ftk.adamw_step(state, [g], step)
+    assert all((t == 3).all() for t in others)
