@@ -743,7 +743,7 @@ def mx4_outer(A, B, route=None, out=None, out_dtype=torch.float32):
 
 # ---- a gate that learns ----------------------------------------------------------------------
 
-GATE_FEW = 16384  # logits that need no workspace
+GATE_FEW = 16384  # logits that need no workspace (FTK_ROUTE_GATE_FEW)
 
 
 class Gate:
@@ -795,8 +795,9 @@ def route_gate(logits, k, normalise=True, gate=None, workspace=None):
     else:
         _index(gate.labels, "labels", N, k), _floats(gate.weights, "weights", N, k), _floats(gate.lse, "lse", N)
         _index(gate.counts, "counts", E + 1), _floats(gate.probs, "probs", E), _floats(gate.loss, "loss", 1)
+        _here(gate.labels, gate.weights, gate.lse, gate.counts, gate.probs, gate.loss)
         gate.normalise = normalise
-    _here(logits, gate.labels, workspace)
+    _here(logits, workspace)
     workspace, wp, wn = _workspace(workspace, route_gate_workspace_bytes(N, E) if N * E > GATE_FEW else 0, dev)
     _check(load().ftk_route_gate(code, logits.data_ptr(), ld, N, E, k, 1 if normalise else 0, gate.labels.data_ptr(),
                                  gate.weights.data_ptr(), gate.lse.data_ptr(), gate.counts.data_ptr(), gate.probs.data_ptr(),
@@ -817,7 +818,7 @@ def route_gate_grad(logits, gate, dweights=None, dloss=None, out=None):
     if dloss is not None:
         _floats(dloss, "dloss", 1)
     out, ldo = _new_rows(out, N, E, logits, "out")
-    _here(logits, gate.labels, dweights, dloss, out)
+    _here(logits, gate.labels, gate.weights, gate.lse, gate.counts, dweights, dloss, out)
     _check(load().ftk_route_gate_grad(_row_code(logits, "logits", _MX_DTYPES), logits.data_ptr(), ld, N, E, k,
                                       1 if gate.normalise else 0, gate.labels.data_ptr(), gate.weights.data_ptr(),
                                       gate.lse.data_ptr(), gate.counts.data_ptr(), _ptr(dweights), _ptr(dloss), out.data_ptr(), ldo,

@@ -339,3 +339,30 @@ def test_gradient_of_32_bit_logits_far_from_zero(N, E, k, lanes):
     steps = 2 * (4 + np.log2(lanes)) + 2 + 4 + 1
     assert steps < 32
     assert (abs(got.sum(1)) <= steps * 2.0 ** -24 * mean).all()
+
+
+class Elsewhere(torch.Tensor):
+    """A tensor that says it lives on another device."""
+
+    def get_device(self):
+        return torch.cuda.current_device() + 1
+
+
+def test_arrays_on_another_device():
+    z = torch.randn(300, 70, device=DEV)
+    names = ("labels", "weights", "lse", "counts", "probs", "loss")
+    for name in names:
+        gate = ftk.route_gate(z, 2)
+        setattr(gate, name, getattr(gate, name).as_subclass(Elsewhere))
+        before = getattr(gate, name).clone()
+        with pytest.raises(ValueError, match="device"):
+            ftk.route_gate(-z, 2, normalise=False, gate=gate)
+        assert gate.normalise and torch.equal(getattr(gate, name), before)
+        if name not in ("probs", "loss"):
+            with pytest.raises(ValueError, match="device"):
+                ftk.route_gate_grad(z, gate, torch.ones(300, 2, device=DEV))
+    gate = ftk.route_gate(z, 2)
+    with pytest.raises(ValueError, match="device"):
+        ftk.route_gate(z.as_subclass(Elsewhere), 2)
+    with pytest.raises(ValueError, match="device"):
+        ftk.route_gate_grad(z, gate, torch.ones(300, 2, device=DEV).as_subclass(Elsewhere))

@@ -1,6 +1,8 @@
 """What the gate, the cross entropy and the weights' update refuse, before anything is enqueued (no GPU needed)."""
 import ctypes
 import math
+import re
+from pathlib import Path
 
 import pytest
 import torch
@@ -107,3 +109,9 @@ def test_xent_gradients_without_rows():
     ok = [ftk.BF16, None, 64, 0, P, 64, 1000, 64, None, 1.0, None, None, None, None, 64, None, 64, None, None, 0, None]
     assert L.ftk_xent_grad(*ok) == 0
     each("ftk_xent_grad", ok, ((0, ftk.F64, 1), (3, -1, 1), (4, None, 1), (5, 63, 1), (9, math.inf, 1), (17, P + 2, 2)))
+
+
+def test_gate_without_a_workspace():
+    """The binding's limit is the header's."""
+    header = (Path(ftk.__file__).resolve().parents[1] / "include" / "ftkmeans.h").read_text()
+    assert int(re.search(r"#define FTK_ROUTE_GATE_FEW (\d+)", header).group(1)) == ftk.GATE_FEW
