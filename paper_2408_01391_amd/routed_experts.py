@@ -181,8 +181,8 @@ def main():
     ap.add_argument("--features", type=int, default=1024)
     ap.add_argument("--outputs", type=int, default=2048)
     ap.add_argument("--clusters", type=int, default=15)
-    ap.add_argument("--classes", type=int, default=512)
-    ap.add_argument("--steps", type=int, default=20)
+    ap.add_argument("--classes", type=int, default=512, help="as many as there are tokens at most")
+    ap.add_argument("--steps", type=int, default=20, help="0: no training")
     a = ap.parse_args()
     g = torch.Generator(device="cuda:0").manual_seed(1)
     rand = lambda *s: torch.randn(*s, generator=g, device="cuda:0")  # noqa: E731
@@ -216,8 +216,10 @@ def main():
     print("from 32-bit matrices and rows: %.3f of the output" % float((out.float() - plain).norm() / plain.norm()))
     print("gradients: " + ", ".join("%s %s" % (list(t.shape), str(t.dtype)[6:]) for t in grads))
 
+    if a.steps < 1:
+        return
     # the clusters of a finer fit are the classes that experts with a gate of their own learn to name
-    V = a.classes
+    V = min(a.classes, N)
     fine = ftk.kmeans_fit(x.float(), V, 5, seed=1, want_inertia=False)["C"]
     names = ftk.kmeans_assign(x.float(), fine)[0]
     learner = LearnedExperts((rand(E, D) * D ** -0.5).bfloat16(), weights.bfloat16(), (rand(V, F) * F ** -0.5).bfloat16(), lr=1e-3)

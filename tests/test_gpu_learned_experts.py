@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2408_01391_amd import binding as ftk
+from paper_2408_01391_amd import binding as ftk, routed_experts
 from paper_2408_01391_amd.routed_experts import LearnedExperts
 from tests.gpu_util import DEV
 from tests.test_gpu_adamw import one_step
@@ -200,3 +200,18 @@ def test_gradient_of_the_rows_in_16_bits():
     labels[60:] = -1
     dx = layer.loss(x, labels, rows=True)[3]
     assert dx.dtype == x.dtype and dx.shape == x.shape and dx.isfinite().all() and (dx[60:] == 0).all() and (dx[:60] != 0).any(1).all()
+
+
+@pytest.mark.parametrize("options,trained", [("--tokens 300 --features 64 --outputs 64 --clusters 3 --steps 2", 300),
+                                             ("--tokens 20 --features 64 --outputs 64 --clusters 3 --steps 1", 20),
+                                             ("--tokens 300 --features 64 --outputs 64 --clusters 3 --classes 7 --steps 3", 7),
+                                             ("--tokens 300 --features 64 --outputs 64 --clusters 3 --steps 0", None)])
+def test_command(options, trained, monkeypatch, capsys):
+    """Fewer tokens than there are classes by default, and no steps: what ran without the training runs."""
+    monkeypatch.setattr("sys.argv", ["routed_experts", *options.split()])
+    routed_experts.main()
+    said = capsys.readouterr().out
+    assert "gradients: " in said
+    assert ("a training step" in said) == (trained is not None)
+    if trained and "--steps 1" not in options:
+        assert "towards %d classes" % trained in said
