@@ -421,3 +421,54 @@ def test_no_rows_and_their_gradient_alone():
     assert ftk.xent_grad(X[:0], W, labels[:0], lse, lse, dX=out, need=(False, False, False))[0] is out
     with pytest.raises(ftk.FtkError):  # (refused as with rows)
         ftk.xent_grad(X[:0], W, labels[:0], lse, lse, scale=INF, need=(True, False, False))
+
+
+@pytest.mark.parametrize("N,V,D,dtypes", [
+    # tiles of 256 x 256 for the logits and both gradients, two pieces of the classes; the rows' gradient in four shares of the classes
+    (5001, 33001, 520, ("bf16", "f16")),
+    # the same without shares, where the rows' sums go on from piece to piece, 160 and 157 stages of classes and 128 of rows, rows read
+    # where they lie and packed
+    (8150, 20003, 1096, ("bf16", "f16")), (8150, 20003, 1101, ("bf16",)),
+    # tiles of 128 x 128 for the gradients, of 256 and of 128 for the logits, the classes' gradient in sixteen shares
+    (30001, 1003, 255, ("f16",)), (20001, 1000, 248, ("bf16",)),
+    # three pieces of 16 bits: tiles of 128 x 128, in shares and without, two pieces of the classes
+    (5001, 9001, 333, ("f32",)), (777, 10007, 333, ("f32",))])
+def test_every_stage_of_large_products(N, V, D, dtypes):
+    """Within bounds that a stage of k too many or too few would break, of 64 or 32 terms among thousands: errors of d and of the logits
+    are independent of each other, so that the sum of n terms of size t and relative error e is off by 8 e sqrt(sum t^2), but in one
+    of 10^13 cases (Hoeffding)."""
+    for dtype in dtypes:
+        X, W, labels, b, dloss = problem(N, V, D, dtype, bias=True)
+        live = (labels >= 0) & (labels < V)
+        x, w = torch.where(live.unsqueeze(1), X, 0).double(), W.double()
+        z = (x @ w.t()).add_(b.double())
+        # a logit's D products (times six) are added to partial sums that stay below 4 sqrt(D) times the largest of them or so: 8 is more
+        # than any logit here has
+        logit = 8 * (D * (6 if dtype == "f32" else 1)) ** 0.5 * 2.0 ** -24 * max(8.0, float(z.abs().max())) + 2.0 ** -22
+        lse = torch.logsumexp(z, 1)
+        loss, mine = ftk.xent(X, W, labels, bias=b)
+        at = torch.where(live, labels, 0).long().unsqueeze(1)
+        want = torch.where(live, lse - z.gather(1, at).squeeze(1), 0)
+        for a, c in ((mine, torch.where(live, lse, 0)), (loss, want)):
+            assert ((a.double() - c).abs() <= 2 * logit + 64 * 2.0 ** -24).all()
+        d = z.sub_(lse.unsqueeze(1)).exp_()
+        d.scatter_add_(1, at, torch.full_like(at, -1, dtype=torch.float64))
+        d *= torch.where(live, dloss.double(), 0).unsqueeze(1)
+        dX, dW, db = ftk.xent_grad(X, W, labels, mine, dloss, bias=b)
+        each = logit + (2.0 ** -22 if dtype == "f32" else HALF[X.dtype])
+        least = 2.0 ** -38 * float(dloss.abs().max()) if dtype == "f16" else 0.0  # (half a step of the smallest d)
+        half, common = HALF[X.dtype], 400 * 2.0 ** -24  # lse and its sums err alike for all classes of a row
+        squares = d.square()
+        for got, right, q, u, n in ((dX, d @ w, squares @ w.square(), w, V), (dW, d.t() @ x, squares.t() @ x.square(), x, N)):
+            size = (d.abs() if n == V else d.abs().t()) @ u.abs()
+            tiny = 8 * least * n ** 0.5 * float(u.abs().max()) + (2.0 ** -25 if dtype == "f16" else 1e-37)
+            bound = 8 * each * q.sqrt() + common * size + 1.01 * half * right.abs() + tiny
+            within = bool(((got.double() - right).abs() <= bound).all())
+            assert within, dtype
+            # (the bounds tell: the terms of a stage of 64, or of 32 in three pieces, have that part of the squares)
+            stage = 32 if dtype == "f32" else 64
+            tells = float((bound / (stage / n * q).sqrt().clamp(min=1e-37)).median()) < 1
+            assert tells, dtype
+            del size, bound, q
+        assert ((db.double() - d.sum(0)).abs() <= 8 * logit * squares.sum(0).sqrt() + common * d.abs().sum(0) + 1e-37).all()
+        del x, w, z, d, squares, X, W, dX, dW
