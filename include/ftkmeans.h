@@ -470,7 +470,7 @@ ftk_status ftk_route_gate_grad(ftk_dtype dtype, const void *logits, int64_t ldz,
  *   X [N x D], W [V x D] of `dtype` (FTK_F32, FTK_BF16 or FTK_F16), row strides ldx and ldw; bias [V] or NULL: 0
  *   labels [N]: a row whose label lies outside [0, V) is ignored: nothing of it is looked at, loss and lse are 0
  *   loss, lse [N]
- * Logits and sums are held in 32 bits; FTK_F32 operands (below 2^127) are taken to 24 bits.  W has to be finite.  A bias of
+ * Logits, sums and lse are held in 32 bits (loss is off by half a step of lse); FTK_F32 operands (below 2^127) are taken to 24 bits.  W has to be finite.  A bias of
  * -infinity closes a class.  A row all of whose logits are -infinity has lse -infinity, a NaN loss and no gradient; a NaN or
  * +infinity among its logits makes a row's loss, lse and gradients NaN.  Results are bitwise reproducible.
  * workspace: ftk_xent_workspace_bytes(dtype, N, V, D, grad); it grows with N * max(D, 256), not with N * V: the classes go in pieces
@@ -487,8 +487,8 @@ ftk_status ftk_xent(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N, cons
  * lse as ftk_xent left it; exp(z - lse) is off by half a step of lse, 2^-8 at most.  From |lse| = 2^17 on, where that would be more (masks of
  * the type's lowest value on all classes), the row's probabilities are divided by their own sum, which takes another pass over W for
  * every 64 rows that have such a one among them.
- * d is rounded to the rows' type (FTK_F32: not at all) before the products; every gradient is written
- * once, in whole, and must not overlap an input. */
+ * d is rounded to the rows' type (FTK_F32: not at all) before the products, and the gradients after them, which leaves those of 16-bit rows
+ * off by 1.4 times a single rounding on average.  Every gradient is written once, in whole, and must not overlap an input. */
 ftk_status ftk_xent_grad(ftk_dtype dtype, const void *X, int64_t ldx, int64_t N, const void *W, int64_t ldw, int64_t V, int32_t D,
                          const float *bias /* nullable */, double scale, const int32_t *labels, const float *lse,
                          const float *dloss, void *dX /* nullable */, int64_t lddx, void *dW /* nullable */, int64_t lddw,

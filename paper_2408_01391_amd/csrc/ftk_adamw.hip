@@ -7,7 +7,7 @@
 // tensor, a lane eight consecutive ones at a time; the tensors' addresses travel as the kernel's arguments, so that a call
 // needs no table in device memory and nothing waits for one.
 // 50 M bf16 weights with 32-bit states and masters, 30 bytes an element: three launches (as many tensors as the arguments hold) of together
-// 272 to 312 us, 4.8 to 5.5 TB/s; 134 M with 8-bit states, 10 bytes: 288 to 302 us, 4.5 to 4.7 TB/s; a copy reaches 5.0.
+// 314 us, 4.8 TB/s; 134 M with 8-bit states, 10 bytes: 290 to 308 us, 4.4 to 4.6 TB/s; a copy reaches 5.0.
 //
 // 8-bit states (ftkmeans.h has the format): the lanes that have a block of 32 exchange its largest magnitude.
 #include <math.h>

@@ -314,8 +314,9 @@ constexpr int GATE_WAVES = L > 64 || NP * PIECE<T> > 16 ? 8 : 16;
 
 // One pass: largest logit and sum of exponentials in registers, the k best beside them, the next row under way meanwhile.
 // Reading the logits is the bound, with the exponentials and the lists close behind: 65536 rows of 256 in bf16, the eight best
-// (34 MB read, 5 written): 22 us, 1.7 TB/s; 16384 rows of 4096 in fp16, the two best (134 MB): 47 us, 2.9 TB/s.  There sixteen pieces of a
-// row (64 logits a lane) leave registers for eight waves a compute unit.
+// (34 MB read, 5 written): 22 us, 1.7 TB/s; 16384 rows of 4096 in fp16, the two best (134 MB): 47 us, 2.9 TB/s.  There eight pieces of a
+// row (64 logits a lane) leave registers for two waves a SIMD, so that reading and arithmetic (27 us each) hardly overlap; a row by 256
+// lanes of 16 logits, as in the gradient, was not tried.
 template <typename T, int L, int NP, int K>
 __global__ __launch_bounds__((64 * GATE_WAVES<T, L, NP>), (NP * PIECE<T> > 16 ? 2 : 4)) void gate_kernel(GateArgs a)
 {
@@ -448,8 +449,9 @@ __global__ __launch_bounds__((64 * GATE_WAVES<T, L, NP>), (NP * PIECE<T> > 16 ? 
 }
 
 // The lines of all workgroups together: 32 experts a workgroup, a 32nd of the lines half a wave, sixteen of them under way at a
-// time.  The last workgroup to end adds the parts of the loss up, in order.  (A launch of its own, as the order of the lines must not
-// depend on which workgroup ends first; 256 lines of 256 experts take 5.3 us, of 4096 8.1 us, a launch alone 4.2 us.)
+// time.  The last workgroup to end adds the parts of the loss up, in order.  A launch of its own, for the bandwidth of many
+// workgroups: 256 lines of 4096 experts (8 MB) take 7.8 us.  The last workgroup of gate_kernel could add small tables up by itself, in the same
+// order: 256 lines of 256 experts take 5.2 us here, of which a launch alone is 4.2.
 constexpr int GATE_END_EXPERTS = 32, GATE_END_SHARES = 32, GATE_END_THREADS = GATE_END_EXPERTS * GATE_END_SHARES;
 __global__ __launch_bounds__(GATE_END_THREADS) void gate_end_kernel(GateArgs a, int lines, double *parts)
 {
@@ -509,7 +511,7 @@ __global__ __launch_bounds__(GATE_END_THREADS) void gate_end_kernel(GateArgs a, 
     }
 }
 
-// One pass again: probabilities from lse, which needs one sum over the row (<p, c>) rather than two.  Memory is the bound: 65536 rows of
+// One pass again: probabilities from lse, which needs one sum over the row (<p, c>) rather than two, as 32-bit logits do.  Memory is the bound: 65536 rows of
 // 256 in bf16 (67 MB and the labels' 8 MB): 20 us, 3.8 TB/s.
 // What the labels add to a row's gradient goes through a row of LDS of the group's own, whose zeros are put back.
 constexpr int GATE_GRAD_WAVES = 4;

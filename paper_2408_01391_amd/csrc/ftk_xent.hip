@@ -11,7 +11,9 @@
 // What lies across k is read from LDS by ds_read_b64_tr_b16, which gives a lane four elements from four of LDS's rows, so that
 // nothing is transposed in memory.
 // 16-bit rows use the 16-bit matrix instructions, sums in 32 bits; d is rounded to the rows' type like any operand of theirs (for
-// fp16 times a power of two that brings the largest dloss to 2^14, where no probability that counts is lost).
+// fp16 times a power of two that brings the largest dloss to 2^14, where no probability that counts is lost).  With the
+// result's own rounding that leaves gradients off by 1.4 times what the result's alone would (2.4e-3 against 1.7e-3 of the norm in bf16,
+// 2.9e-4 against 2.1e-4 in fp16); a second piece of d would double the gradients' products.
 // 32-bit rows are split into three bf16 pieces each (24 bits), of whose products the six largest are
 // added: what is left out is below 2^-24 of the magnitudes.
 #include <math.h>
@@ -210,7 +212,7 @@ __device__ __forceinline__ Run run_of(const Product &g, int split)
 // 16-bit rows.  Stages of 64 elements of k, two in LDS, copied there without passing through registers.  Tiles of 256 x 256 by
 // eight waves need 128 KB of LDS, of which 64 KB pass for 8.4 MF: matrix instructions are the bound, with what a tile's begin
 // and end take (10 and 5 of 47 us at 32 stages), when none are issued.  8192 rows x 65536 classes x 2048, bf16: the sums 1716 to
-// 1775 us, 1.24 to 1.28 PF; d and its store in 16 bits 1892 to 1957; rows' and classes' gradient 1680 to 1736 each, up to 1.31 PF.
+// 1775 us, 1.24 to 1.28 PF; d and its store in 16 bits 1860 to 1957; rows' and classes' gradient 1680 to 1736 each, up to 1.31 PF.
 // The instruction alone, fed from registers, reaches 1.95 PF on such numbers, a library's large product 1.40 to 1.48.  Slower: five
 // stages of 32 in a ring (by 20 %), workgroups that go on to further tiles (26 %), four waves of 128 x 128 (45 %), tiles of
 // 128 x 128 (30 %), the 32 x 32 x 16 instruction (its own rate is 10 % less).
@@ -324,8 +326,8 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product g, End e
 // Rows of three bf16 pieces, all of whole stages: a stage holds 32 elements of all pieces, so that six products are formed of what
 // is read once.
 // While a stage's products are formed, the next one's fragments come from LDS, the one after that is under way, and the third begins
-// to come into the place that this one's fragments have left: one meeting a stage.  777 rows x 10007 classes x 333: the sums 54 us,
-// d 63, the rows' and the classes' gradient 37 each (31 GF each by six products, 0.84 PF); matrix instructions are busy for 60 % of
+// to come into the place that this one's fragments have left: one meeting a stage.  777 rows x 10007 classes x 333: the sums 55 us,
+// d 63, the rows' and the classes' gradient 38 each (31 GF each by six products, 0.84 PF); matrix instructions are busy for 60 % of
 // that, the rest is begin, end and a last round of tiles that does not fill the card.  (One piece's product after the other reads
 // LDS twice as often: 63, 70, 56 and 69 us.)
 template <typename S, bool AT, bool BT, typename End>

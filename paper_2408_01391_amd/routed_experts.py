@@ -111,7 +111,8 @@ class LearnedExperts(Experts):
 
     gate [E, D], experts [E, F, D], classes [V, F]: weights of one type, float32 or bfloat16, which the layer updates in place
     (AdamW; 16-bit weights beside 32-bit masters, states of `bits` bits).  bias [V] float: of the classes' logits.
-    balance: weight of the balance loss."""
+    balance: weight of the balance loss.
+    The gate's logits come in the rows' type, which near ties of 16-bit rows do not outlast: the lower index is chosen."""
 
     def __init__(self, gate, experts, classes, k=2, balance=0.01, bits=8, bias=None, **options):
         E, F, D = experts.shape
